@@ -9,12 +9,16 @@
 #include <new>
 #include <string>
 
+#include "gsq_host.h"
 #include "gsq_internal.h"
-#include "gsq_pool.h"
+
+namespace gsq {
 
 namespace {
-
 thread_local std::string g_err;
+}
+
+void clear_error() { g_err.clear(); }
 
 gsq_status fail(gsq_status st, const char* fmt, ...) {
   char buf[512];
@@ -30,20 +34,7 @@ gsq_status hip_fail(hipError_t e, const char* what) {
   return fail(GSQ_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-#define GSQ_HIP(call)                                  \
-  do {                                                 \
-    hipError_t e_ = (call);                            \
-    if (e_ != hipSuccess) return hip_fail(e_, #call);  \
-  } while (0)
-
-int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
-
 int code_bits(int n) { return n <= 2 ? 1 : n <= 4 ? 2 : n <= 8 ? 3 : 4; }
-
-int logits_per_coord(const gsq_config& c) {
-  return c.relaxation == GSQ_RELAX_SHIFT ? GSQ_SHIFT_WINDOW
-         : c.relaxation == GSQ_RELAX_TERNARY ? 2 : c.n_levels;
-}
 
 gsq_status validate_config(const gsq_config* c) {
   if (!c) return fail(GSQ_EINVAL, "config is NULL");
@@ -90,7 +81,26 @@ gsq_status validate_config(const gsq_config* c) {
   return GSQ_OK;
 }
 
-gsq::DevicePool g_pool;   // at process exit the runtime frees device memory itself
+DevicePool g_pool;   // at process exit the runtime frees device memory itself
+
+}  // namespace gsq
+
+namespace {
+
+using gsq::code_bits;
+using gsq::fail;
+using gsq::g_err;
+using gsq::g_pool;
+using gsq::hip_fail;
+using gsq::validate_config;
+
+int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+int logits_per_coord(const gsq_config& c) {
+  return c.relaxation == GSQ_RELAX_SHIFT ? GSQ_SHIFT_WINDOW
+         : c.relaxation == GSQ_RELAX_TERNARY ? 2 : c.n_levels;
+}
+
 
 // Free a handle nothing on its device uses any more (`idle`; else its memory is not kept).
 void free_layer(gsq::Layer* L, bool idle) {
