@@ -16,7 +16,7 @@ RELAX_GRID, RELAX_SHIFT, RELAX_TERNARY = 0, 1, 2
 MAX_LEVELS = 16             # GSQ_MAX_LEVELS
 SHIFT_WINDOW = 5            # GSQ_SHIFT_WINDOW
 PREC_FP32, PREC_BF16 = 0, 1
-DT_FP32, DT_BF16 = 0, 1
+DT_FP32, DT_BF16, DT_FP16 = 0, 1, 2
 OPT_ADAM, OPT_LION = 0, 1
 MAX_SAMPLES = 16            # GSQ_MAX_SAMPLES
 STATUS_NAMES = {0: "GSQ_OK", -1: "GSQ_EINVAL", -2: "GSQ_ENOMEM", -3: "GSQ_EHIP",
@@ -24,7 +24,10 @@ STATUS_NAMES = {0: "GSQ_OK", -1: "GSQ_EINVAL", -2: "GSQ_ENOMEM", -3: "GSQ_EHIP",
 
 EXPORTS = ("gsq_layer_init", "gsq_step", "gsq_step_static", "gsq_harden", "gsq_packed_size",
            "gsq_pack", "gsq_get_state", "gsq_set_state", "gsq_get_intermediates", "gsq_gumbel", "gsq_check",
-           "gsq_layer_destroy", "gsq_release_cached", "gsq_last_error", "gsq_timing", "gsq_timing_read")
+           "gsq_layer_destroy", "gsq_release_cached", "gsq_last_error", "gsq_timing", "gsq_timing_read",
+           "gsq_grouped_forward", "gsq_grouped_input_grad", "gsq_grouped_weight_grad", "gsq_gram",
+           "gsq_quantize_rows", "gsq_grouped_forward_i8", "gsq_linear_init", "gsq_linear_forward",
+           "gsq_linear_destroy")
 KERNEL_NAMES = ("init", "forward", "contract", "reduce", "backward", "harden", "pack")
 
 
@@ -50,6 +53,11 @@ class CStepParams(ctypes.Structure):
                 ("tau_next", ctypes.c_float), ("kappa_next", ctypes.c_float),
                 ("optimizer", ctypes.c_int32), ("weight_decay", ctypes.c_float),
                 ("samples", ctypes.c_int32)]
+
+
+class CGrouped(ctypes.Structure):
+    _fields_ = [("groups", ctypes.c_int32), ("out_features", ctypes.c_int32),
+                ("in_features", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rows", ctypes.c_int64)]
 
 
 @dataclass
@@ -142,6 +150,20 @@ def load(path=None):
     lib.gsq_last_error.restype = ctypes.c_char_p
     lib.gsq_timing.argtypes = [vp, i32]
     lib.gsq_timing_read.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i64), i32, vp]
+    gp = ctypes.POINTER(CGrouped)
+    lib.gsq_grouped_forward.argtypes = [gp, vp, vp, vp, vp, vp]
+    lib.gsq_grouped_input_grad.argtypes = [gp, vp, vp, vp, vp, vp]
+    lib.gsq_grouped_weight_grad.argtypes = [gp, vp, vp, vp, vp, i32, i32, vp]
+    lib.gsq_gram.argtypes = [gp, vp, vp, vp, i32, vp]
+    lib.gsq_quantize_rows.argtypes = [vp, i32, i64, i32, vp, vp, vp]
+    lib.gsq_grouped_forward_i8.argtypes = [gp, vp, vp, vp, vp, vp, vp, vp]
+    lib.gsq_linear_init.argtypes = [ctypes.POINTER(CConfig), vp, sz, vp, ctypes.POINTER(vp)]
+    lib.gsq_linear_forward.argtypes = [vp, vp, i32, i64, vp, vp, vp]
+    lib.gsq_linear_destroy.argtypes = [vp]
+    for name in ("gsq_grouped_forward", "gsq_grouped_input_grad", "gsq_grouped_weight_grad",
+                 "gsq_gram", "gsq_quantize_rows", "gsq_grouped_forward_i8", "gsq_linear_init",
+                 "gsq_linear_forward", "gsq_linear_destroy"):
+        getattr(lib, name).restype = ctypes.c_int
     for name in ("gsq_layer_init", "gsq_step", "gsq_step_static", "gsq_harden", "gsq_pack",
                  "gsq_get_state", "gsq_set_state", "gsq_get_intermediates", "gsq_gumbel", "gsq_check",
                  "gsq_layer_destroy", "gsq_release_cached", "gsq_timing", "gsq_timing_read"):
@@ -315,6 +337,160 @@ class Layer:
     def destroy(self):
         if self._h is not None:
             load().gsq_layer_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+# ---- products of grouped rows: x is rows x I with the rows of all groups sorted by group, w is groups x
+# O x I (or O x I for one group), and ``offsets`` a device int64 tensor of groups + 1 row offsets (None
+# for one group that has every row).
+
+def _grouped(tensors, groups, rows, out_features, in_features, dtype, offsets):
+    """The sizes as the library takes them, after checks of the tensors ({name: (tensor, shapes,
+    dtypes)}): on the current device, dense, of one of the shapes and types."""
+    import torch
+    codes = {torch.bfloat16: DT_BF16, torch.float16: DT_FP16}
+    if dtype not in codes:
+        raise TypeError(f"rows must be bfloat16 or float16, got {dtype}")
+    if offsets is None:
+        if groups != 1:
+            raise ValueError(f"{groups} groups need offsets")
+    else:
+        tensors = dict(tensors, offsets=(offsets, [(groups + 1,)], (torch.int64,)))
+    for name, (t, shapes, dtypes) in tensors.items():
+        if tuple(t.shape) not in shapes:
+            raise ValueError(f"{name} must have the shape {' or '.join(map(str, shapes))}, got "
+                             f"{tuple(t.shape)}")
+    for name, (t, _, dtypes) in tensors.items():
+        _on_current_device(t, name)
+        _arg(t, name, t.numel(), dtypes)
+    return CGrouped(groups, out_features, in_features, codes[dtype], rows)
+
+
+def _on_current_device(t, name):
+    import torch
+    if t.is_cuda and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, but device {torch.cuda.current_device()} is current")
+
+
+def _weight_sizes(w):
+    if w.dim() not in (2, 3):
+        raise ValueError(f"w must be groups x O x I or O x I, got {tuple(w.shape)}")
+    return (1, *w.shape) if w.dim() == 2 else tuple(w.shape)
+
+
+def _row_count(x, name):
+    if x.dim() != 2:
+        raise ValueError(f"{name} must be rows x features, got {tuple(x.shape)}")
+    return x.shape[0]
+
+
+def grouped_forward(x, w, out, offsets=None, stream=None):
+    """out = x W_e^T for the rows of each group (x, w, out: bfloat16 or float16)."""
+    (n, o, i), r = _weight_sizes(w), _row_count(x, "x")
+    g = _grouped({"x": (x, [(r, i)], (x.dtype,)), "w": (w, [tuple(w.shape)], (x.dtype,)),
+                  "out": (out, [(r, o)], (x.dtype,))}, n, r, o, i, x.dtype, offsets)
+    _check(load().gsq_grouped_forward(ctypes.byref(g), _ptr(x), _ptr(w), _ptr(offsets), _ptr(out),
+                                      _stream(stream)))
+
+
+def grouped_input_grad(dy, w, out, offsets=None, stream=None):
+    """out = dy W_e, the gradient of grouped_forward's x."""
+    (n, o, i), r = _weight_sizes(w), _row_count(dy, "dy")
+    g = _grouped({"dy": (dy, [(r, o)], (dy.dtype,)), "w": (w, [tuple(w.shape)], (dy.dtype,)),
+                  "out": (out, [(r, i)], (dy.dtype,))}, n, r, o, i, dy.dtype, offsets)
+    _check(load().gsq_grouped_input_grad(ctypes.byref(g), _ptr(dy), _ptr(w), _ptr(offsets), _ptr(out),
+                                         _stream(stream)))
+
+
+def grouped_weight_grad(dy, x, out, offsets=None, accumulate=False, stream=None):
+    """out_e = sum of dy[r]^T x[r] over the rows of group e, the gradient of grouped_forward's w, in the
+    type of x or in float32; ``accumulate`` adds to a float32 out."""
+    import torch
+    (n, o, i), r = _weight_sizes(out), _row_count(dy, "dy")
+    g = _grouped({"dy": (dy, [(r, o)], (dy.dtype,)), "x": (x, [(r, i)], (dy.dtype,)),
+                  "out": (out, [tuple(out.shape)], (dy.dtype, torch.float32))}, n, r, o, i, dy.dtype, offsets)
+    dt = DT_FP32 if out.dtype == torch.float32 else g.dtype
+    _check(load().gsq_grouped_weight_grad(ctypes.byref(g), _ptr(dy), _ptr(x), _ptr(offsets), _ptr(out), dt,
+                                          1 if accumulate else 0, _stream(stream)))
+
+
+def gram(x, out, offsets=None, accumulate=False, stream=None):
+    """out_e = X_e^T X_e in float32 (groups x I x I or I x I), the H of ``Layer``; ``accumulate`` adds to it."""
+    import torch
+    (n, i, i2), r = _weight_sizes(out), _row_count(x, "x")
+    if i != i2:
+        raise ValueError(f"out must be square, got {tuple(out.shape)}")
+    g = _grouped({"x": (x, [(r, i)], (x.dtype,)), "out": (out, [tuple(out.shape)], (torch.float32,))},
+                 n, r, 0, i, x.dtype, offsets)
+    _check(load().gsq_gram(ctypes.byref(g), _ptr(x), _ptr(offsets), _ptr(out), 1 if accumulate else 0,
+                           _stream(stream)))
+
+
+def quantize_rows(x, q, scales, stream=None):
+    """Rows of x (rows x cols; float32, bfloat16 or float16) as int8 ``q`` and a float32 scale each: tokens
+    of activations, or output channels of weights (a groups x O x I tensor has groups * O rows)."""
+    import torch
+    codes = {torch.float32: DT_FP32, torch.bfloat16: DT_BF16, torch.float16: DT_FP16}
+    if x.dim() < 2:
+        raise ValueError(f"x must be rows x columns, got {tuple(x.shape)}")
+    if tuple(q.shape) != tuple(x.shape) or tuple(scales.shape) != tuple(x.shape[:-1]):
+        raise ValueError(f"q must have the shape of x and scales that of its rows, got {tuple(q.shape)} and "
+                         f"{tuple(scales.shape)} for {tuple(x.shape)}")
+    for name, t, dtypes in (("x", x, tuple(codes)), ("q", q, (torch.int8,)),
+                            ("scales", scales, (torch.float32,))):
+        _on_current_device(t, name)
+        _arg(t, name, t.numel(), dtypes)
+    _check(load().gsq_quantize_rows(_ptr(x), codes[x.dtype], scales.numel(), x.shape[-1], _ptr(q),
+                                    _ptr(scales), _stream(stream)))
+
+
+def grouped_forward_i8(x, x_scales, w, w_scales, out, offsets=None, stream=None):
+    """out[r, n] = x_scales[r] w_scales[e, n] sum_k x[r, k] w[e, n, k] for int8 x and w."""
+    import torch
+    (n, o, i), r = _weight_sizes(w), _row_count(x, "x")
+    g = _grouped({"x": (x, [(r, i)], (torch.int8,)), "x_scales": (x_scales, [(r,)], (torch.float32,)),
+                  "w": (w, [tuple(w.shape)], (torch.int8,)),
+                  "w_scales": (w_scales, [tuple(w.shape[:-1])], (torch.float32,)),
+                  "out": (out, [(r, o)], (out.dtype,))}, n, r, o, i, out.dtype, offsets)
+    _check(load().gsq_grouped_forward_i8(ctypes.byref(g), _ptr(x), _ptr(x_scales), _ptr(w), _ptr(w_scales),
+                                         _ptr(offsets), _ptr(out), _stream(stream)))
+
+
+class Linear:
+    """A packed layer in use (gsq_linear*): ``packed`` holds what Layer.pack wrote for ``cfg``."""
+
+    def __init__(self, cfg, packed, stream=None):
+        self._h = None
+        self.cfg = cfg
+        if not (packed.is_cuda and packed.is_contiguous()):
+            raise ValueError("packed must be a contiguous device tensor")
+        _on_current_device(packed, "packed")
+        h = ctypes.c_void_p()
+        _check(load().gsq_linear_init(ctypes.byref(cfg.to_c()), _ptr(packed),
+                                      packed.numel() * packed.element_size(), _stream(stream),
+                                      ctypes.byref(h)))
+        self._h = h
+
+    def forward(self, x, out, offsets=None, stream=None):
+        """out = x W_e^T with the packed weights (x, out: bfloat16 or float16)."""
+        if self._h is None:
+            raise RuntimeError("layer destroyed")
+        c, r = self.cfg, _row_count(x, "x")
+        g = _grouped({"x": (x, [(r, c.in_features)], (x.dtype,)),
+                      "out": (out, [(r, c.out_features)], (x.dtype,))}, c.batch, r, c.out_features,
+                     c.in_features, x.dtype, offsets)
+        _check(load().gsq_linear_forward(self._h, _ptr(x), g.dtype, r, _ptr(offsets), _ptr(out),
+                                         _stream(stream)))
+
+    def destroy(self):
+        if self._h is not None:
+            load().gsq_linear_destroy(self._h)
             self._h = None
 
     def __del__(self):

@@ -1,0 +1,150 @@
+"""What the products refuse, and in what words, before anything reaches the device."""
+import ctypes
+import os
+
+import pytest
+
+from paper_2604_18556_amd import binding as B
+
+torch = pytest.importorskip("torch")
+P = ctypes.c_void_p
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(B._LIB_PATH):
+        pytest.skip("libgsq.so not built (run __graft_entry__.build())")
+    return B.load()
+
+
+def sizes(groups=2, out=8, inn=16, dtype=B.DT_BF16, rows=4):
+    return B.CGrouped(groups, out, inn, dtype, rows)
+
+
+BAD_SIZES = [dict(groups=0), dict(groups=65536), dict(out=0), dict(out=(1 << 21) + 1), dict(inn=0),
+             dict(inn=(1 << 21) + 1), dict(dtype=B.DT_FP32), dict(dtype=9), dict(rows=-1),
+             dict(rows=(1 << 29) + 1)]
+
+
+@pytest.mark.parametrize("bad", BAD_SIZES)
+def test_sizes_are_checked(lib, bad):
+    g, a = ctypes.byref(sizes(**bad)), P(64)
+    calls = [lambda: lib.gsq_grouped_forward(g, a, a, a, a, None),
+             lambda: lib.gsq_grouped_input_grad(g, a, a, a, a, None),
+             lambda: lib.gsq_grouped_weight_grad(g, a, a, a, a, B.DT_FP32, 0, None),
+             lambda: lib.gsq_grouped_forward_i8(g, a, a, a, a, a, a, None)]
+    if "out" not in bad:                       # the Gram matrix has no output features
+        calls.append(lambda: lib.gsq_gram(g, a, a, a, 0, None))
+    for call in calls:
+        assert call() == B.GSQ_EINVAL
+        assert lib.gsq_last_error()
+
+
+def test_arrays_are_checked(lib):
+    g, a, no, odd = ctypes.byref(sizes()), P(64), None, P(65)
+    E = B.GSQ_EINVAL
+    assert lib.gsq_grouped_forward(None, a, a, a, a, None) == E
+    for bad in (no, odd):
+        assert lib.gsq_grouped_forward(g, bad, a, a, a, None) == E
+        assert lib.gsq_grouped_forward(g, a, bad, a, a, None) == E
+        assert lib.gsq_grouped_forward(g, a, a, bad, a, None) == E      # two groups need offsets
+        assert lib.gsq_grouped_forward(g, a, a, a, bad, None) == E
+        assert lib.gsq_grouped_input_grad(g, bad, a, a, a, None) == E
+        assert lib.gsq_grouped_input_grad(g, a, bad, a, a, None) == E
+        assert lib.gsq_grouped_input_grad(g, a, a, a, bad, None) == E
+        assert lib.gsq_grouped_weight_grad(g, bad, a, a, a, B.DT_BF16, 0, None) == E
+        assert lib.gsq_grouped_weight_grad(g, a, bad, a, a, B.DT_BF16, 0, None) == E
+        assert lib.gsq_grouped_weight_grad(g, a, a, a, bad, B.DT_BF16, 0, None) == E
+        assert lib.gsq_gram(g, bad, a, a, 0, None) == E
+        assert lib.gsq_gram(g, a, a, bad, 0, None) == E
+        assert lib.gsq_grouped_forward_i8(g, a, bad, a, a, a, a, None) == E
+        assert lib.gsq_grouped_forward_i8(g, a, a, a, bad, a, a, None) == E
+        assert lib.gsq_grouped_forward_i8(g, a, a, a, a, a, bad, None) == E
+        assert lib.gsq_quantize_rows(bad, B.DT_BF16, 1, 8, a, a, None) == E
+        assert lib.gsq_quantize_rows(a, B.DT_BF16, 1, 8, a, bad, None) == E
+    assert lib.gsq_gram(g, a, a, P(66), 0, None) == E                    # fp32 needs 4 bytes
+    assert lib.gsq_grouped_weight_grad(g, a, a, a, P(66), B.DT_FP32, 0, None) == E
+    assert lib.gsq_grouped_forward_i8(g, None, a, a, a, a, a, None) == E
+    assert lib.gsq_quantize_rows(a, B.DT_BF16, 1, 8, None, a, None) == E
+
+
+def test_weight_grad_types(lib):
+    g, a = ctypes.byref(sizes()), P(64)
+    assert lib.gsq_grouped_weight_grad(g, a, a, a, a, B.DT_FP16, 0, None) == B.GSQ_EINVAL
+    assert lib.gsq_grouped_weight_grad(g, a, a, a, a, B.DT_BF16, 1, None) == B.GSQ_EINVAL
+    assert b"FP32" in lib.gsq_last_error()
+
+
+def test_integer_sums_stay_exact(lib):
+    a = P(64)
+    assert lib.gsq_grouped_forward_i8(ctypes.byref(sizes(inn=131072)), a, a, a, a, a, a, None) == B.GSQ_EINVAL
+    assert b"131071" in lib.gsq_last_error()
+    assert 128 * 128 * 131071 < 2 ** 31
+
+
+def test_quantize_sizes(lib):
+    a = P(64)
+    for dtype, rows, cols in ((7, 1, 8), (0, -1, 8), (0, (1 << 23) + 1, 8), (0, 1, 0), (0, 1, (1 << 21) + 1)):
+        assert lib.gsq_quantize_rows(a, dtype, rows, cols, a, a, None) == B.GSQ_EINVAL
+
+
+def test_no_rows_need_no_arrays(lib):
+    """A batch without a row is no error, whatever its row arrays' addresses are."""
+    g, a = ctypes.byref(sizes(groups=1, rows=0)), P(64)
+    assert lib.gsq_grouped_forward(g, None, a, None, None, None) == B.GSQ_OK
+    assert lib.gsq_grouped_input_grad(g, None, a, None, None, None) == B.GSQ_OK
+    assert lib.gsq_grouped_forward_i8(g, None, None, a, a, None, None, None) == B.GSQ_OK
+    assert lib.gsq_quantize_rows(None, B.DT_BF16, 0, 8, None, None, None) == B.GSQ_OK
+
+
+def test_linear_refusals(lib):
+    h = P()
+    cfg = B.LayerConfig(8, 256, (-1.0, 0.0, 1.0))
+    need = B.packed_size(cfg)
+    c = cfg.to_c()
+    E = B.GSQ_EINVAL
+    assert lib.gsq_linear_init(None, P(64), need, None, ctypes.byref(h)) == E
+    assert lib.gsq_linear_init(ctypes.byref(c), None, need, None, ctypes.byref(h)) == E
+    assert lib.gsq_linear_init(ctypes.byref(c), P(64), need - 1, None, ctypes.byref(h)) == E
+    assert lib.gsq_linear_init(ctypes.byref(c), P(64), need, None, None) == E
+    bad = B.LayerConfig(8, 200, (-1.0, 0.0, 1.0)).to_c()
+    assert lib.gsq_linear_init(ctypes.byref(bad), P(64), need, None, ctypes.byref(h)) == E
+    for big in (B.LayerConfig((1 << 21) + 1, 16, (-1.0, 1.0), 16),
+                B.LayerConfig(1, (1 << 21) + 16, (-1.0, 1.0), 16),
+                B.LayerConfig(1, 16, (-1.0, 1.0), 16, batch=65536)):
+        b = big.to_c()
+        assert lib.gsq_linear_init(ctypes.byref(b), P(64), 1 << 40, None, ctypes.byref(h)) == E
+    assert h.value is None
+    assert lib.gsq_linear_forward(None, P(64), B.DT_BF16, 1, None, P(64), None) == E
+    assert lib.gsq_linear_destroy(None) == B.GSQ_OK
+
+
+def test_c_struct_layout():
+    assert ctypes.sizeof(B.CGrouped) == 24 and B.CGrouped.rows.offset == 16
+
+
+def test_binding_checks_tensors_before_the_library():
+    """Host tensors, wrong shapes and wrong types raise before a pointer is passed on."""
+    x, w, y = torch.zeros(3, 8, dtype=torch.bfloat16), torch.zeros(2, 4, 8, dtype=torch.bfloat16), \
+        torch.zeros(3, 4, dtype=torch.bfloat16)
+    off = torch.zeros(3, dtype=torch.int64)
+    with pytest.raises(ValueError, match="device tensor"):
+        B.grouped_forward(x, w, y, offsets=off)
+    with pytest.raises(ValueError, match="need offsets"):
+        B.grouped_forward(x, w, y)
+    with pytest.raises(ValueError, match="shape"):
+        B.grouped_forward(x[:, :4], w, y, offsets=off)
+    with pytest.raises(ValueError, match="shape"):
+        B.grouped_forward(x, w, y, offsets=off[:2])
+    with pytest.raises(TypeError, match="bfloat16 or float16"):
+        B.grouped_forward(x.float(), w.float(), y.float(), offsets=off)
+    with pytest.raises(ValueError, match="square"):
+        B.gram(x, torch.zeros(4, 8))
+    with pytest.raises(ValueError, match="rows x features"):
+        B.gram(x[0], torch.zeros(8, 8))
+    with pytest.raises(ValueError, match="groups x O x I"):
+        B.grouped_input_grad(y, w[0, 0], x)
+    with pytest.raises(ValueError, match="shape"):
+        B.quantize_rows(x, torch.zeros(3, 7, dtype=torch.int8), torch.zeros(3))
+    with pytest.raises(ValueError, match="device tensor"):
+        B.Linear(B.LayerConfig(4, 16, (-1.0, 1.0), 16), torch.zeros(64, dtype=torch.uint8))
