@@ -1,0 +1,89 @@
+// Device parts of the kernels whose operands move as slabs through a ring in LDS: the order of the tiles,
+// the slab's layout, and the waits.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace gsq {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int ROW_BYTES = 128;       // a slab's row (64 16-bit elements): a full cache line
+constexpr int GROUP_M = 8;           // tile rows swept together for L2 reuse
+constexpr size_t LDS_BYTES = 160 * 1024;
+
+// Position of block `bid` of nblk in the tile order.  Workgroups are handed to the 8 XCDs
+// round-robin; renumbering so each XCD owns a contiguous range of the blocks keeps the R and H
+// panels a group of tiles shares in the same XCD's L2.
+__device__ __forceinline__ int lin_of(int bid, int nblk) {
+  const int x = bid & 7, base = nblk >> 3, rem = nblk & 7;
+  return x * base + min(x, rem) + (bid >> 3);
+}
+
+// Tile at position `lin`: GROUP_M tile rows are swept together, column by column.
+__device__ __forceinline__ void tile_at(int lin, int tiles_m, int tiles_n, int& tm, int& tn) {
+  const int per_group = GROUP_M * tiles_n;
+  const int first_m = (lin / per_group) * GROUP_M;
+  const int gsz = min(tiles_m - first_m, GROUP_M);
+  const int r = lin % per_group;
+  tm = first_m + r % gsz;
+  tn = r / gsz;
+}
+
+// LDS layout of a slab: row r occupies 128 bytes as eight 16-byte chunks, chunk c stored at
+// position c ^ f(r), f(r) = (r / 2) & 7; two rows span the 64 banks.  A fragment read takes 16 rows,
+// chunk c in one 16 lanes and c ^ 1 in the next, and the hardware serves lanes 0-3, 12-15 and 20-27
+// together, then the others (measured: with f(r) = (r ^ (r / 8)) & 7, which is free of conflicts for
+// 16 consecutive lanes, every read took 4 cycles more).  With this f both sets, and consecutive lanes
+// too, fall on distinct banks.
+__device__ __forceinline__ int swz(int r) { return (r >> 1) & 7; }
+
+// Global->LDS copy of a wavefront's share of one operand slab: n instructions of eight rows, 16
+// bytes per lane.  `src` is wave-uniform (the slab's first column); off[j] is the lane's element
+// offset of instruction j, fixed for the whole K loop.
+__device__ __forceinline__ void load_rows(const uint16_t* src, uint8_t* lds) {
+  __builtin_amdgcn_global_load_lds(src, lds, 16, 0, 0);
+}
+
+template <class F>
+__device__ __forceinline__ F read_frag(const uint8_t* lds, int row, int chunk) {
+  return *reinterpret_cast<const F*>(lds + row * ROW_BYTES + ((chunk ^ swz(row)) << 4));
+}
+
+// Wait until at most n of this wavefront's vector-memory loads are outstanding (loads complete
+// in issue order), leaving LDS and scalar counters alone.
+template <int n>
+__device__ __forceinline__ void wait_vm() {
+  static_assert(n >= 0 && n < 64, "six bits");
+  __builtin_amdgcn_s_waitcnt((n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14));
+}
+
+// Workgroup barrier for the slab ring: this wavefront's LDS reads are drained (its own
+// global->LDS loads were waited for with wait_vm), then a plain s_barrier.  The signal fences
+// keep the compiler from moving memory accesses across it; the waits are real instructions, so
+// the compiler's own wait bookkeeping sees them.
+__device__ __forceinline__ void slab_barrier() {
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  __builtin_amdgcn_s_waitcnt((15) | (7 << 4) | (0 << 8) | (3 << 14));   // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+}
+
+// Waits until accumulators can be read by anything but another product (see the products).
+template <class A, int MI, int NJ>
+__device__ __forceinline__ void acc_settled(A (&acc)[MI][NJ]) {
+  // accumulators written before this are written before the wait, and read after it
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) asm volatile("" : "+a"(acc[i][j]));
+  asm volatile("s_nop 15\n\ts_nop 15");
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) asm volatile("" : "+a"(acc[i][j]));
+}
+
+}  // namespace
+}  // namespace gsq
