@@ -140,10 +140,10 @@ __global__ __launch_bounds__(256) void k_packed_any(PackedLayer L, GroupRows row
                                                     const typename T::elem* __restrict__ x,
                                                     typename T::elem* __restrict__ y) {
   using E = typename T::elem;
-  int e;
-  int64_t first, end;
-  if (!find_panel(rows, kAnyTile, blockIdx.x, e, first, end)) return;
-  const int ms = (int)(end - first);
+  PanelPlace at;
+  if (!find_panel(rows, kAnyTile, blockIdx.x, at)) return;
+  const int64_t first = at.first + (int64_t)at.panel * kAnyTile;
+  const int e = at.group, ms = (int)min(at.end - first, (int64_t)kAnyTile);
   const AlongK<E> a{x + first * L.I, L.I, ms, L.I};
   tile_any<T>(a, PackedWeights<E>{L, (int64_t)e * L.tiles}, 0, blockIdx.y * kAnyTile, L.I,
               [&](int m, int n, float v) {

@@ -4,7 +4,7 @@
 
 #include <algorithm>
 
-#include "gsq_product_any.hpp"
+#include "gsq_tile.hpp"
 
 namespace gsq {
 namespace {
@@ -13,10 +13,11 @@ namespace {
 template <class T, int kForm>
 __global__ __launch_bounds__(256) void k_rows_any(ProductArgs p) {
   using E = typename T::elem;
-  int e;
-  int64_t first, end;
-  if (!find_panel(p.rows, kAnyTile, blockIdx.x, e, first, end)) return;
-  const int n0 = blockIdx.y * kAnyTile, ms = (int)(end - first);
+  PanelPlace at;
+  if (!find_panel(p.rows, kAnyTile, blockIdx.x, at)) return;
+  const int64_t first = at.first + (int64_t)at.panel * kAnyTile;
+  const int e = at.group, ms = (int)min(at.end - first, (int64_t)kAnyTile);
+  const int n0 = blockIdx.y * kAnyTile;
   const int ks = kForm == kForward ? p.I : p.O, ns = kForm == kForward ? p.O : p.I;
   const E* w = static_cast<const E*>(p.b) + (int64_t)e * p.O * p.I;
   const AlongK<E> a{static_cast<const E*>(p.a) + first * ks, ks, ms, ks};
@@ -50,6 +51,155 @@ __global__ __launch_bounds__(256) void k_weight_grad_any(ProductArgs p) {
     store_out(p.out, p.out_dtype, at, v);
   };
   tile_any<T>(a, b, blockIdx.y * kAnyTile, blockIdx.x * kAnyTile, ks, store);
+}
+
+// Four consecutive output elements, together where `four` says that they are whole and aligned.
+__device__ __forceinline__ void store_four(void* out, int dtype, int64_t at, f32x4 v, int count, bool four) {
+  if (!four) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (c < count) store_out(out, dtype, at + c, v[c]);
+    return;
+  }
+  if (dtype == GSQ_DT_FP32) {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = v;
+  } else if (dtype == GSQ_DT_BF16) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(out) + at) = __builtin_convertvector(v, bf16x4);
+  } else {
+    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<f16x4*>(static_cast<_Float16*>(out) + at) = __builtin_convertvector(v, f16x4);
+  }
+}
+
+// The whole tile uses all the LDS; panels with fewer rows take lower ones, whose slabs last less long and
+// are loaded further ahead.
+using Whole = TileShape<256, 256, 2>;
+using Half = TileShape<128, 256, 3>;
+using Low = TileShape<64, 256, 3>;
+
+// One tile of y or dx: rows m0 .. of a group, columns n0 .. .
+template <class T, int kForm, class S>
+__device__ __forceinline__ void rows_tile(const ProductArgs& p, const PanelPlace& at, int64_t first, int ms, int n0,
+                                          uint8_t* smem) {
+  using E = typename T::elem;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int ks = kForm == kForward ? p.I : p.O, ns = kForm == kForward ? p.O : p.I;
+  const int nk = (int)(((int64_t)ks * sizeof(E) + ROW_BYTES - 1) / ROW_BYTES);
+  const E* w = static_cast<const E*>(p.b) + (int64_t)at.group * p.O * p.I;
+  const SlabAlong<S::TM> a(static_cast<const E*>(p.a) + first * ks, (int64_t)ks * sizeof(E), ms, wave, lane);
+  typename T::acc acc[S::MI][S::NJ];
+  if constexpr (kForm == kForward) {
+    const SlabAlong<S::TN> b(w + (int64_t)n0 * ks, (int64_t)ks * sizeof(E), ns - n0, wave, lane);
+    tile_ring<T, S>(a, b, nk, acc, smem);
+  } else {
+    const SlabAcross<S::TN> b(w + n0, (int64_t)ns * sizeof(E), ns - n0, ks, wave, lane);
+    tile_ring<T, S>(a, b, nk, acc, smem);
+  }
+  const bool four = p.vector_out;
+  tile_results<S>(acc, [&](int m, int n, auto v) {
+    if (m >= ms || n0 + n >= ns) return;
+    f32x4 y;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) y[c] = (float)v[c];
+    if constexpr (T::kDtype < 0) {   // 8-bit integers: the sum is exact in 32 bits
+      const float* bs = p.b_scales + (int64_t)at.group * p.O + n0 + n;
+      const float as = p.a_scales[first + m];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) y[c] = y[c] * as * bs[min(c, ns - n0 - n - 1)];
+    }
+    store_four(p.out, p.out_dtype, (first + m) * ns + n0 + n, y, ns - n0 - n, four);
+  });
+}
+
+// y or dx.  A group's tiles follow each other and are spread over the XCDs so that each has a contiguous
+// part of the group's tile order.
+template <class T, int kForm>
+__global__ __launch_bounds__(256, 1) void k_rows_tile(ProductArgs p) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  const int ns = kForm == kForward ? p.O : p.I, tiles_n = (ns + Whole::TN - 1) / Whole::TN;
+  PanelPlace at;
+  if (!find_panel(p.rows, Whole::TM, blockIdx.x / (unsigned)tiles_n, at)) return;
+  int tm, tn;
+  tile_at(lin_of((int)(blockIdx.x - at.before * tiles_n), at.panels * tiles_n), at.panels, tiles_n, tm, tn);
+  const int64_t first = at.first + (int64_t)tm * Whole::TM;
+  const int ms = (int)min(at.end - first, (int64_t)Whole::TM), n0 = tn * Whole::TN;
+  if (ms > Half::TM)
+    rows_tile<T, kForm, Whole>(p, at, first, ms, n0, smem);
+  else if (ms > Low::TM)
+    rows_tile<T, kForm, Half>(p, at, first, ms, n0, smem);
+  else
+    rows_tile<T, kForm, Low>(p, at, first, ms, n0, smem);
+}
+
+// One tile of a sum over a group's rows: out[m0 .., n0 ..] (+)= sum_r a[r, m] b[r, n], and with `mirror` its
+// transpose too.
+template <class T>
+__device__ __forceinline__ void sum_tile(const ProductArgs& p, int e, int m0, int n0, bool mirror, uint8_t* smem) {
+  using E = typename T::elem;
+  using S = Whole;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int64_t first, end;
+  group_rows(p.rows, e, first, end);
+  const int ks = (int)(end - first), nk = (ks + kSlabRows - 1) / kSlabRows;
+  // a group without rows reads zeros only: its addresses are not used
+  const SlabAcross<S::TM> a(static_cast<const E*>(p.a) + first * p.O + m0, (int64_t)p.O * 2, p.O - m0, ks, wave, lane);
+  const SlabAcross<S::TN> b(static_cast<const E*>(p.b) + first * p.I + n0, (int64_t)p.I * 2, p.I - n0, ks, wave, lane);
+  typename T::acc acc[S::MI][S::NJ];
+  tile_ring<T, S>(a, b, nk, acc, smem);
+  const int64_t out0 = (int64_t)e * p.O * p.I;
+  tile_results<S>(acc, [&](int m, int n, f32x4 v) {
+    m += m0;
+    n += n0;
+    if (m >= p.O || n >= p.I) return;
+    const int64_t at = out0 + (int64_t)m * p.I + n;
+    if (p.accumulate) {
+      const float* sums = static_cast<const float*>(p.out) + at;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[c] += n + c < p.I ? sums[c] : 0.f;
+    }
+    store_four(p.out, p.out_dtype, at, v, p.I - n, p.vector_out);
+  });
+  if (!mirror) return;
+  tile_results<S>(acc, [&](int m, int n, f32x4 v) {   // 16 lanes hold 16 neighbours of a transposed row
+    m += m0;
+    n += n0;
+    if (m >= p.O) return;
+    float* sums = static_cast<float*>(p.out) + out0 + (int64_t)n * p.I + m;
+#pragma unroll
+    for (int c = 0; c < 4; ++c, sums += p.I)
+      if (n + c < p.I) *sums = p.accumulate ? *sums + v[c] : v[c];
+  });
+}
+
+// dW of every group, each group's tiles spread over the XCDs.
+template <class T>
+__global__ __launch_bounds__(256, 1) void k_weight_grad_tile(ProductArgs p) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  const int tiles_m = (p.O + Whole::TM - 1) / Whole::TM, tiles_n = (p.I + Whole::TN - 1) / Whole::TN;
+  const int tiles = tiles_m * tiles_n, e = blockIdx.x / (unsigned)tiles;
+  int tm, tn;
+  tile_at(lin_of(blockIdx.x - e * tiles, tiles), tiles_m, tiles_n, tm, tn);
+  sum_tile<T>(p, e, tm * Whole::TM, tn * Whole::TN, false, smem);
+}
+
+// H of every group: the tiles on and above the diagonal, and their transposes.  Of T tile rows, row r (T - r
+// tiles) and row T - 1 - r (r + 1) are taken as one row of T + 1, so that the order of a rectangle serves;
+// an odd T's middle row has the second half of its own empty.
+template <class T>
+__global__ __launch_bounds__(256, 1) void k_gram_tile(ProductArgs p) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  const int side = (p.I + Whole::TM - 1) / Whole::TM, pairs = (side + 1) / 2;
+  const int tiles = pairs * (side + 1), e = blockIdx.x / (unsigned)tiles;
+  int r, c;
+  tile_at(lin_of(blockIdx.x - e * tiles, tiles), pairs, side + 1, r, c);
+  int tm = r, tn = r + c;
+  if (c >= side - r) {
+    tm = side - 1 - r;
+    tn = tm + c - (side - r);
+    if (tm == r) return;
+  }
+  sum_tile<T>(p, e, tm * Whole::TM, tn * Whole::TN, tm != tn, smem);
 }
 
 // Rows in 8-bit integers: s = max |x| / 127 in fp32, q = x / s to the nearest integer, ties to even.  A
@@ -96,40 +246,67 @@ __global__ __launch_bounds__(256) void k_quantize_rows(const E* __restrict__ x, 
   }
 }
 
+// A kernel that uses the whole LDS needs leave for it, once on each device.
+template <class... Args>
+hipError_t launch_ring(void (*kernel)(Args...), int64_t blocks, hipStream_t s, Args... args) {
+  if (blocks >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;   // 2^32 threads in grid.x
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS_BYTES);
+  if (e != hipSuccess) return e;
+  kernel<<<(unsigned)blocks, 256, LDS_BYTES, s>>>(args...);
+  return hipGetLastError();
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+int tiles_of(int n, int tile) { return (n + tile - 1) / tile; }
+
+// Results can be stored four at a time: whole rows of them, at aligned addresses.
+bool four_at_once(const void* out, int32_t dtype, int32_t cols) {
+  const uintptr_t bytes = dtype == GSQ_DT_FP32 ? 16 : 8;
+  return cols % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & (bytes - 1)) == 0;
+}
+
+template <class T, int kForm>
+hipError_t launch_rows(ProductArgs p, hipStream_t s) {
+  if (p.rows.rows == 0) return hipSuccess;
+  const int ns = kForm == kForward ? p.O : p.I;
+  const int64_t unit = 16 / (int64_t)sizeof(typename T::elem);
+  if (p.O % (kForm == kForward ? 1 : unit) == 0 && p.I % unit == 0 && aligned16(p.a) && aligned16(p.b)) {
+    p.vector_out = four_at_once(p.out, p.out_dtype, ns);
+    return launch_ring(k_rows_tile<T, kForm>, most_panels(p.rows, Whole::TM) * tiles_of(ns, Whole::TN), s, p);
+  }
+  const dim3 grid(most_panels(p.rows, kAnyTile), tiles_of(ns, kAnyTile));
+  k_rows_any<T, kForm><<<grid, 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t launch_sums(ProductArgs p, bool gram, hipStream_t s) {
+  if (p.O % 8 == 0 && p.I % 8 == 0 && aligned16(p.a) && aligned16(p.b)) {
+    p.vector_out = four_at_once(p.out, p.out_dtype, p.I);
+    const int64_t tm = tiles_of(p.O, Whole::TM), tn = tiles_of(p.I, Whole::TN);
+    if (gram) return launch_ring(k_gram_tile<T>, p.rows.groups * ((tn + 1) / 2 * (tn + 1)), s, p);
+    return launch_ring(k_weight_grad_tile<T>, p.rows.groups * tm * tn, s, p);
+  }
+  const dim3 grid(tiles_of(p.I, kAnyTile), tiles_of(p.O, kAnyTile), p.rows.groups);
+  k_weight_grad_any<T><<<grid, 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_product(int form, int dtype, const ProductArgs& p, hipStream_t s) {
-  if (form == kWeightGrad) {
-    const dim3 grid((p.I + kAnyTile - 1) / kAnyTile, (p.O + kAnyTile - 1) / kAnyTile, p.rows.groups);
-    if (dtype == GSQ_DT_BF16)
-      k_weight_grad_any<Bf16><<<grid, 256, 0, s>>>(p);
-    else
-      k_weight_grad_any<F16><<<grid, 256, 0, s>>>(p);
-    return hipGetLastError();
-  }
-  if (p.rows.rows == 0) return hipSuccess;
-  const int ns = form == kForward ? p.O : p.I;
-  const dim3 grid(most_panels(p.rows, kAnyTile), (ns + kAnyTile - 1) / kAnyTile);
-  if (form == kForward && dtype == GSQ_DT_BF16)
-    k_rows_any<Bf16, kForward><<<grid, 256, 0, s>>>(p);
-  else if (form == kForward)
-    k_rows_any<F16, kForward><<<grid, 256, 0, s>>>(p);
-  else if (dtype == GSQ_DT_BF16)
-    k_rows_any<Bf16, kInputGrad><<<grid, 256, 0, s>>>(p);
-  else
-    k_rows_any<F16, kInputGrad><<<grid, 256, 0, s>>>(p);
-  return hipGetLastError();
+  const bool bf16 = dtype == GSQ_DT_BF16;
+  if (form == kForward) return bf16 ? launch_rows<Bf16, kForward>(p, s) : launch_rows<F16, kForward>(p, s);
+  if (form == kInputGrad) return bf16 ? launch_rows<Bf16, kInputGrad>(p, s) : launch_rows<F16, kInputGrad>(p, s);
+  return bf16 ? launch_sums<Bf16>(p, false, s) : launch_sums<F16>(p, false, s);
 }
 
-hipError_t launch_product_i8(const ProductArgs& p, hipStream_t s) {
-  if (p.rows.rows == 0) return hipSuccess;
-  const dim3 grid(most_panels(p.rows, kAnyTile), (p.O + kAnyTile - 1) / kAnyTile);
-  k_rows_any<I8, kForward><<<grid, 256, 0, s>>>(p);
-  return hipGetLastError();
-}
+hipError_t launch_product_i8(const ProductArgs& p, hipStream_t s) { return launch_rows<I8, kForward>(p, s); }
 
 hipError_t launch_gram(int dtype, const ProductArgs& p, hipStream_t s) {
-  return launch_product(kWeightGrad, dtype, p, s);
+  return dtype == GSQ_DT_BF16 ? launch_sums<Bf16>(p, true, s) : launch_sums<F16>(p, true, s);
 }
 
 hipError_t launch_quantize_rows(const void* x, int dtype, int64_t rows, int64_t cols, int8_t* q,

@@ -54,11 +54,19 @@ __device__ __forceinline__ void group_rows(const GroupRows& g, int e, int64_t& f
   }
 }
 
-// Panel `index` when every group's rows are cut into panels of `height`: its group, first row and end.
-// False: there are fewer panels.  The whole wavefront calls it; 64 groups are counted at a time.
-__device__ __forceinline__ bool find_panel(const GroupRows& g, int height, int64_t index, int& group,
-                                           int64_t& first, int64_t& end) {
+// Where a workgroup stands when every group's rows are cut into panels of equal height.
+struct PanelPlace {
+  int group;
+  int panel, panels;        // in the group
+  int64_t first, end;       // rows of the group
+  int64_t before;           // panels of the groups before it
+};
+
+// Panel `index` of all groups.  False: there are fewer.  The whole wavefront calls it; 64 groups are counted
+// at a time.
+__device__ __forceinline__ bool find_panel(const GroupRows& g, int height, int64_t index, PanelPlace& at) {
   const int lane = threadIdx.x & 63;
+  int64_t before = 0;
   for (int e0 = 0; e0 < g.groups; e0 += 64) {
     int64_t a = 0, b = 0;
     if (e0 + lane < g.groups) group_rows(g, e0 + lane, a, b);
@@ -70,16 +78,20 @@ __device__ __forceinline__ bool find_panel(const GroupRows& g, int height, int64
       if (lane >= d) upto += x;
     }
     const int all = __shfl(upto, 63, 64);
-    if (index < all) {
-      const uint64_t past = __ballot(index < upto);
-      const int src = __builtin_ctzll(past);
-      const int k = (int)index - __shfl(upto - mine, src, 64);
-      group = __builtin_amdgcn_readfirstlane(e0 + src);
-      first = __shfl(a, src, 64) + (int64_t)k * height;
-      end = min(__shfl(b, src, 64), first + height);
+    if (index - before < all) {
+      const int src = __builtin_ctzll(__ballot((int)(index - before) < upto));
+      const auto of_src = [&](int v) {
+        return __builtin_amdgcn_readfirstlane(__shfl(v, src, 64));
+      };
+      at.group = __builtin_amdgcn_readfirstlane(e0 + src);
+      at.panels = of_src(mine);
+      at.before = before + of_src(upto - mine);
+      at.panel = (int)(index - at.before);
+      at.first = (int64_t)(((uint64_t)(uint32_t)of_src((int)(a >> 32)) << 32) | (uint32_t)of_src((int)a));
+      at.end = (int64_t)(((uint64_t)(uint32_t)of_src((int)(b >> 32)) << 32) | (uint32_t)of_src((int)b));
       return true;
     }
-    index -= all;
+    before += all;
   }
   return false;
 }

@@ -1,0 +1,270 @@
+// The product of one output tile from two operands that move as slabs through a ring in LDS.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gsq_product_any.hpp"
+#include "gsq_slab.hpp"
+
+namespace gsq {
+namespace {
+
+constexpr int kSlabRows = 64;        // rows of a slab that is read across k
+
+// What lanes read where an operand has ended: zeros, in global memory so that it takes the same path.
+__device__ const uint4 g_zeros[1] = {};
+__device__ __forceinline__ const uint8_t* zeros() { return reinterpret_cast<const uint8_t*>(g_zeros); }
+
+// A workgroup's tile: TM x TN outputs by four wavefronts (a quarter each), and slabs loaded AHEAD ahead of
+// the one in use.  LDS holds a ring of AHEAD + 1 slabs of A and AHEAD of B.
+template <int TM_, int TN_, int AHEAD_>
+struct TileShape {
+  static constexpr int TM = TM_, TN = TN_, AHEAD = AHEAD_;
+  static constexpr int A_STAGES = AHEAD + 1, B_STAGES = AHEAD;
+  static constexpr int A_SLAB = TM * ROW_BYTES, B_SLAB = TN * ROW_BYTES;
+  static constexpr int B_BASE = A_STAGES * A_SLAB;
+  static constexpr int A_LOADS = TM / 32, B_LOADS = TN / 32;   // 1 KB loads per wavefront and slab
+  static constexpr int MI = TM / 32, NJ = TN / 32;             // 16 x 16 blocks per wavefront
+  static_assert(B_BASE + B_STAGES * B_SLAB <= (int)LDS_BYTES, "the ring fits the LDS");
+};
+
+// One block's product: B's columns are the instruction's rows, so that a lane's four results are four
+// consecutive columns of a row.  The instruction is written out because the builtin gives its result other
+// registers than its accumulator input once there are 64 of these, and moves them around.  The compiler
+// then does not see when an accumulator can be read: acc_settled() waits for it.  The operands come from
+// LDS reads, whose waits the compiler sets; no vector instruction writes them.
+template <class T>
+__device__ __forceinline__ void mfma_block(typename T::acc& acc, const i32x4& b, const i32x4& a) {
+  if constexpr (T::kDtype == GSQ_DT_BF16)
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(b), "v"(a));
+  else if constexpr (T::kDtype == GSQ_DT_FP16)
+    asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(b), "v"(a));
+  else
+    asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(acc) : "v"(b), "v"(a));
+}
+
+// Global->LDS copies of 16 bytes per lane, to `lds` + 16 lane.  Written out, so that the compiler does not
+// make every transposing LDS read wait for all of them: the loop's own wait_vm() and barrier order them, and
+// they return nothing to a register.  Addresses: a uniform base with 32-bit lane offsets, or one per lane.
+// M0 holds the LDS address; nothing else in these kernels uses it (it is no register that the compiler keeps
+// values in).
+__device__ __forceinline__ uint32_t lds_address(const uint8_t* lds) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)lds;
+}
+__device__ __forceinline__ void copy_to_lds(const uint8_t* base, uint32_t off, const uint8_t* lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds_address(lds))), "v"(off), "s"(base)
+               : "memory");
+}
+__device__ __forceinline__ void copy_to_lds(const uint8_t* src, const uint8_t* lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds_address(lds))), "v"(src)
+               : "memory");
+}
+
+// An address that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ const uint8_t* uniform(const void* p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return reinterpret_cast<const uint8_t*>((uint64_t)hi << 32 | lo);
+}
+
+// An operand whose rows (of the output's side) run along k: a slab is 128 bytes of each of its rows, row r
+// at r ROW_BYTES, chunks swizzled as swz() says.  Rows beyond the last one are read as the last one (their
+// outputs are not stored), chunks beyond the end of k as zeros.
+template <int ROWS>
+struct SlabAlong {
+  static constexpr int LOADS = ROWS / 32;
+  const uint8_t* base;       // the tile's first row
+  uint32_t off[LOADS];       // bytes; below 256 x 2^22
+  int bytes;                 // of a row
+  int chunk[LOADS];
+
+  __device__ __forceinline__ SlabAlong(const void* first, int64_t row_bytes, int rows, int wave, int lane)
+      : base(uniform(first)), bytes((int)row_bytes) {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int row = wave * (LOADS * 8) + j * 8 + (lane >> 3);
+      chunk[j] = ((lane & 7) ^ swz(row)) * 16;
+      off[j] = (uint32_t)min(row, rows - 1) * (uint32_t)row_bytes + chunk[j];
+    }
+  }
+  template <bool kEnd>
+  __device__ __forceinline__ void load(int k, int j, uint8_t* lds) const {
+    const uint8_t* slab = base + (int64_t)k * ROW_BYTES;
+    if constexpr (kEnd)
+      copy_to_lds((int64_t)k * ROW_BYTES + chunk[j] < bytes ? slab + off[j] : zeros(), lds + j * 8 * ROW_BYTES);
+    else
+      copy_to_lds(slab, off[j], lds + j * 8 * ROW_BYTES);
+  }
+  // 16 rows from `row0`, k of half a slab
+  static __device__ __forceinline__ i32x4 frag(const uint8_t* slab, int row0, int half, int lane) {
+    return read_frag<i32x4>(slab, row0 + (lane & 15), half * 4 + (lane >> 4));
+  }
+};
+
+// An operand whose rows are k (16-bit elements, the output's side is contiguous): a slab is 64 rows of COLS
+// elements.  The reads transpose: 16 lanes take four rows of 16 columns (32 bytes each) and each gets the
+// four k of one column.  32 lanes read rows r .. r + 3 and r + 8 .. r + 11 at once: the 32-byte granules of
+// a row are stored at granule ^ f(row), so that those eight rows fall on distinct banks.
+// Rows beyond the end of k are read as zeros, columns beyond the last 16 bytes as those.
+template <int COLS>
+struct SlabAcross {
+  static constexpr int LOADS = COLS / 32;
+  static constexpr int PITCH = COLS * 2, PER_ROW = COLS / 8;   // bytes; 16-byte chunks
+  static_assert(PITCH >= 256, "eight granules of a row to swizzle");
+  const uint8_t* base;       // row 0 of k, the tile's first column
+  uint32_t off[LOADS];       // bytes; below 64 x 2^22
+  int64_t slab_bytes;        // from one slab to the next
+  int rows;                  // of k
+  int row[LOADS];
+
+  static __device__ __forceinline__ int turn(int r) { return (r & 3) | ((r >> 1) & 4); }
+
+  __device__ __forceinline__ SlabAcross(const void* first, int64_t row_bytes, int cols, int rows_, int wave,
+                                        int lane)
+      : base(uniform(first)), slab_bytes(row_bytes * kSlabRows), rows(rows_) {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int at = (wave * LOADS + j) * 64 + lane, c = at % PER_ROW;
+      row[j] = at / PER_ROW;
+      const int chunk = ((c >> 1) ^ turn(row[j])) * 2 + (c & 1);
+      off[j] = (uint32_t)row[j] * (uint32_t)row_bytes + (uint32_t)min(chunk * 16, cols * 2 - 16);
+    }
+  }
+  template <bool kEnd>
+  __device__ __forceinline__ void load(int k, int j, uint8_t* lds) const {
+    const uint8_t* slab = base + k * slab_bytes;
+    if constexpr (kEnd)
+      copy_to_lds(k * kSlabRows + row[j] < rows ? slab + off[j] : zeros(), lds + j * 1024);
+    else
+      copy_to_lds(slab, off[j], lds + j * 1024);
+  }
+  static __device__ __forceinline__ i32x4 frag(const uint8_t* slab, int col0, int half, int lane) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+    const int r = half * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2);
+    const uint8_t* at = slab + r * PITCH + (((col0 >> 4) ^ turn(r)) << 5) + (lane & 3) * 8;
+    union { s16x4 s[2]; i32x4 v; } u;
+    u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at);
+    u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * PITCH));   // the same turn
+    return u.v;
+  }
+};
+
+// The tile: slabs 0 .. nk - 1, of which the last may end early (those past nk, for short sums, are zeros).
+// 64 of k (128 of 8-bit integers) at a time move by direct global->LDS loads into the two rings.  A's extra
+// buffer lets its slab k + AHEAD be loaded during the first half of slab k, B's during the second.  Fragment
+// reads of the next half and slab loads are issued between the products, a load after every two reads.
+// Blocks are walked back and forth: one operand of each product is the last one's.
+template <class T, class S, class A, class B>
+__device__ __forceinline__ void tile_ring(const A& a, const B& b, int nk,
+                                          typename T::acc (&acc)[S::MI][S::NJ], uint8_t* smem) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+#pragma unroll
+  for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j) acc[i][j] = typename T::acc{};
+  acc_settled(acc);
+
+  uint8_t* const a_wave = smem + wave * (S::A_SLAB / 4);
+  uint8_t* const b_wave = smem + S::B_BASE + wave * (S::B_SLAB / 4);
+  const int row_a = wm * (S::TM / 2), row_b = wn * (S::TN / 2);
+
+  constexpr int kMfma = S::MI * S::NJ, kReads = S::MI + S::NJ;
+  constexpr int kLess = S::MI < S::NJ ? S::MI : S::NJ;
+  const auto read = [&](i32x4 (&fa)[S::MI], i32x4 (&fb)[S::NJ], int k, int half, int n) {
+    // one of each in turn, then the rest of the longer side
+    const bool of_b = n < 2 * kLess ? n % 2 == 1 : S::NJ > S::MI;
+    const int i = n < 2 * kLess ? n / 2 : n - kLess;
+    if (of_b)
+      fb[i] = B::frag(smem + S::B_BASE + (k % S::B_STAGES) * S::B_SLAB, row_b + i * 16, half, lane);
+    else
+      fa[i] = A::frag(smem + (k % S::A_STAGES) * S::A_SLAB, row_a + i * 16, half, lane);
+  };
+  const auto half_slab = [&](const i32x4 (&fa)[S::MI], const i32x4 (&fb)[S::NJ], int n_reads, int n_loads,
+                             auto&& next_read, auto&& next_load) {
+    constexpr int kLoads = S::A_LOADS > S::B_LOADS ? S::A_LOADS : S::B_LOADS;
+    constexpr int kOps = kReads + kReads / 2 > 3 * kLoads ? kReads + kReads / 2 : 3 * kLoads;
+    constexpr int kStep = kMfma / kOps > 0 ? kMfma / kOps : 1;
+    const auto op = [&](int o) {
+      if (o % 3 == 2) { if (o / 3 < n_loads) next_load(o / 3); }
+      else if (o - o / 3 < n_reads) next_read(o - o / 3);
+    };
+#pragma unroll
+    for (int n = 0; n < kMfma; ++n) {
+      const int i = n / S::NJ, j = i % 2 ? S::NJ - 1 - n % S::NJ : n % S::NJ;
+      mfma_block<T>(acc[i][j], fb[j], fa[i]);
+      if (n % kStep == 0) op(n / kStep);
+    }
+#pragma unroll
+    for (int o = (kMfma + kStep - 1) / kStep; o < kOps; ++o) op(o);
+  };
+  const auto none = [](int) {};
+
+  // p: first half of the current slab; q: second half
+  i32x4 pa[S::MI], pb[S::NJ], qa[S::MI], qb[S::NJ];
+#pragma unroll
+  for (int k = 0; k < S::AHEAD; ++k) {
+#pragma unroll
+    for (int j = 0; j < S::A_LOADS; ++j) a.template load<true>(k, j, a_wave + k * S::A_SLAB);
+#pragma unroll
+    for (int j = 0; j < S::B_LOADS; ++j) b.template load<true>(k, j, b_wave + k * S::B_SLAB);
+  }
+  constexpr int kSlabLoads = S::A_LOADS + S::B_LOADS;
+  wait_vm<(S::AHEAD - 1) * kSlabLoads>();
+  slab_barrier();
+#pragma unroll
+  for (int n = 0; n < kReads; ++n) read(pa, pb, 0, 0, n);
+  nk = max(nk, S::AHEAD);
+  // one slab while AHEAD more are on their way; `end`: the one loaded may end early
+  const auto step = [&](int kt, auto end) {
+    constexpr bool kEnd = decltype(end)::value;
+    half_slab(pa, pb, kReads, S::A_LOADS, [&](int n) { read(qa, qb, kt, 1, n); },
+              [&](int j) {
+                a.template load<kEnd>(kt + S::AHEAD, j, a_wave + ((kt + S::AHEAD) % S::A_STAGES) * S::A_SLAB);
+              });
+    __builtin_amdgcn_sched_barrier(0);   // every product of this half is issued before the wait
+    // slab kt + 1 has landed (later ones, of kt + AHEAD only A's, may be in flight), and every
+    // wavefront has read slab kt
+    wait_vm<(S::AHEAD - 2) * kSlabLoads + S::A_LOADS>();
+    slab_barrier();
+    half_slab(qa, qb, kReads, S::B_LOADS, [&](int n) { read(pa, pb, kt + 1, 0, n); },
+              [&](int j) {
+                b.template load<kEnd>(kt + S::AHEAD, j, b_wave + ((kt + S::AHEAD) % S::B_STAGES) * S::B_SLAB);
+              });
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  int kt = 0;
+  for (; kt < nk - S::AHEAD - 1; ++kt) step(kt, std::false_type{});
+  if (kt < nk - S::AHEAD) step(kt++, std::true_type{});
+  // the last slabs: nothing more to load
+  for (; kt < nk - 1; ++kt) {
+    half_slab(pa, pb, kReads, 0, [&](int n) { read(qa, qb, kt, 1, n); }, none);
+    wait_vm<0>();
+    slab_barrier();
+    half_slab(qa, qb, kReads, 0, [&](int n) { read(pa, pb, kt + 1, 0, n); }, none);
+  }
+  half_slab(pa, pb, kReads, 0, [&](int n) { read(qa, qb, nk - 1, 1, n); }, none);
+  half_slab(qa, qb, 0, 0, none, none);
+  acc_settled(acc);
+}
+
+// The tile's results: store(row, column, four consecutive columns' values) for every block.  Lane l of a
+// block has row l % 16 and columns 4 (l / 16) .. + 3.
+template <class S, class Acc, class Store>
+__device__ __forceinline__ void tile_results(const Acc (&acc)[S::MI][S::NJ], Store store) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int m = (wave >> 1) * (S::TM / 2) + (lane & 15), n = (wave & 1) * (S::TN / 2) + 4 * (lane >> 4);
+#pragma unroll
+  for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j) store(m + i * 16, n + j * 16, acc[i][j]);
+}
+
+}  // namespace
+}  // namespace gsq
