@@ -15,7 +15,7 @@ namespace {
 //   2 bits: word j / 16, bits 8 (j % 4) + 2 (j / 4 % 4)
 //   3 bits: the lower two as for 2 bits, the third in word 2 as for 1 bit
 //   4 bits: word j / 8, bits 8 (j % 4) + 4 (j / 4 % 2)
-__host__ __device__ __forceinline__ void place_code(uint32_t* words, int bits, int j, uint32_t code) {
+__device__ __forceinline__ void place_code(uint32_t* words, int bits, int j, uint32_t code) {
   const int byte = 8 * (j & 3), quad = j >> 2;
   if (bits == 1) {
     words[0] |= code << (byte + quad);
@@ -26,14 +26,6 @@ __host__ __device__ __forceinline__ void place_code(uint32_t* words, int bits, i
     if (bits == 3) words[2] |= (code >> 2) << (byte + quad);
   }
 }
-__device__ __forceinline__ uint32_t code_at(const uint32_t* words, int bits, int j) {
-  const int byte = 8 * (j & 3), quad = j >> 2;
-  if (bits == 1) return words[0] >> (byte + quad) & 1;
-  if (bits == 4) return words[quad >> 1] >> (byte + 4 * (quad & 1)) & 15;
-  const uint32_t low = words[quad >> 2] >> (byte + 2 * (quad & 3)) & 3;
-  return bits == 2 ? low : low | (words[2] >> (byte + quad) & 1) << 2;
-}
-
 // A field of at most 8 bits from little-endian bits; the next byte is read only if the field reaches it.
 __device__ __forceinline__ uint32_t bit_field(const uint8_t* p, int64_t bit, int width) {
   const int64_t at = bit >> 3;
@@ -77,15 +69,33 @@ __global__ __launch_bounds__(256) void k_unpack_codes(const uint8_t* __restrict_
   for (int k = 0; k < L.bits; ++k) codes[at * L.bits + k] = words[k];
 }
 
-// One thread per kept scale (groups x tiles x per x 16 channels), zero where there is no channel or group.
+// Where the scale of channel n of a tile and inputs 16 j .. is kept: for groups of 16 with the unit's lanes,
+// the two of a lane side by side; else by group, 16 channels side by side.
+__device__ __forceinline__ void place_of_scale(const PackedLayer& L, bool fine, int64_t at, int64_t& tile, int& n,
+                                               int& group) {
+  if (fine) {
+    const int64_t unit = at >> 7;
+    const int lane = (int)(at >> 1) & 63;
+    tile = unit / L.blocks;
+    n = lane & 15;
+    group = (int)(unit % L.blocks) * 8 + (lane >> 4) * 2 + (int)(at & 1);
+  } else {
+    tile = at / 16 / L.scale_groups;
+    n = (int)(at & 15);
+    group = (int)(at / 16 % L.scale_groups);
+  }
+}
+
+// One thread per kept scale, zero where there is no channel or group.
 __global__ __launch_bounds__(256) void k_unpack_scales(const uint8_t* __restrict__ packed, int layout,
                                                        PackedLayer L, int64_t at_byte, int64_t count,
                                                        uint16_t* __restrict__ scales) {
   const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (at >= count) return;
-  const int64_t tile = at / 16 / L.scale_groups;
-  const int64_t g = at / 16 % L.scale_groups;
-  const int64_t e = tile / L.tiles, o = (tile % L.tiles) * 16 + (at & 15);
+  int64_t tile;
+  int n, g;
+  place_of_scale(L, L.gs == 16, at, tile, n, g);
+  const int64_t e = tile / L.tiles, o = (tile % L.tiles) * 16 + n;
   uint16_t v = 0;
   if (o < L.O && g < L.I / L.gs) {
     const int64_t k = (e * L.O + o) * (L.I / L.gs) + g;
@@ -98,9 +108,10 @@ __global__ __launch_bounds__(256) void k_unpack_sub(const uint8_t* __restrict__ 
                                                     int64_t count, uint8_t* __restrict__ sub) {
   const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (at >= count) return;
-  const int64_t per = L.scale_groups * 16;
-  const int64_t tile = at / 16 / per, g = at / 16 % per;
-  const int64_t e = tile / L.tiles, o = (tile % L.tiles) * 16 + (at & 15);
+  int64_t tile;
+  int n, g;
+  place_of_scale(L, true, at, tile, n, g);
+  const int64_t e = tile / L.tiles, o = (tile % L.tiles) * 16 + n;
   uint32_t v = 0;
   if (o < L.O && g < L.I / 16) {
     const int64_t rec = (e * L.O + o) * (L.I / 256) + g / 16;
@@ -117,38 +128,187 @@ __device__ __forceinline__ float scaled_level(float scale, float level) {
   return p;
 }
 
-// Weight (n, k) of one group: scale * level in fp32, rounded to the type of x.
-template <class E>
-struct PackedWeights {
-  const PackedLayer& L;
-  int64_t tile0;       // first tile of the group
-  static constexpr bool kFast = true;
-  __device__ __forceinline__ E at(int n, int k) const {
-    if (n >= L.O || k >= L.I) return (E)0;
-    const int64_t tile = tile0 + n / 16;
-    const int lane = (k % 128) / 32 * 16 + n % 16;
-    const uint32_t* words = L.codes + ((tile * L.blocks + k / 128) * 64 + lane) * L.bits;
-    const uint32_t c = code_at(words, L.bits, k % 32);
-    float s = (float)__builtin_bit_cast(_Float16, L.scales[(tile * L.scale_groups + k / L.gs) * 16 + n % 16]);
-    if (L.sub) s *= (float)L.sub[(tile * L.scale_groups * 16 + k / 16) * 16 + n % 16];
-    return (E)scaled_level(s, L.levels[c]);
+// ---- from codes to weights.  Scales of one group of inputs give a table of all 2^BITS weights; a lane's
+// codes pick from it.  v_perm_b32 picks four bytes of eight by four selectors, so the table is kept as its low
+// bytes and its high bytes, four codes are four selectors, and two more picks put the bytes together:
+// 1.5 instructions per weight at 2 bits, 2 at 3 bits, 3.3 at 4 bits.
+template <class T, int BITS>
+struct WeightTable {
+  static constexpr int N = 1 << BITS, WORDS = (N + 3) / 4;
+  uint32_t lo[WORDS], hi[WORDS];
+
+  static __device__ __forceinline__ uint32_t pair(float a, float b) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef typename T::elem e2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), e2));
+  }
+  __device__ __forceinline__ WeightTable(float scale, const float* levels) {
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+      float v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = 4 * w + k < N ? scaled_level(scale, levels[4 * w + k]) : 0.f;
+      const uint32_t p01 = pair(v[0], v[1]), p23 = N > 2 ? pair(v[2], v[3]) : 0;
+      lo[w] = __builtin_amdgcn_perm(p23, p01, 0x06040200);
+      hi[w] = __builtin_amdgcn_perm(p23, p01, 0x07050301);
+    }
+  }
+  // Weights 4 q .. 4 q + 3 of a lane's 32 as two words.
+  __device__ __forceinline__ void pick(const uint32_t* words, int q, uint32_t& d0, uint32_t& d1) const {
+    uint32_t l, h;
+    if constexpr (BITS == 1) {
+      const uint32_t sel = words[0] >> q & 0x01010101u;
+      l = __builtin_amdgcn_perm(hi[0], lo[0], sel);
+      h = __builtin_amdgcn_perm(lo[0], hi[0], sel);
+    } else if constexpr (BITS == 2) {
+      const uint32_t sel = words[q >> 2] >> (2 * (q & 3)) & 0x03030303u;
+      l = __builtin_amdgcn_perm(hi[0], lo[0], sel);
+      h = __builtin_amdgcn_perm(lo[0], hi[0], sel);
+    } else if constexpr (BITS == 3) {
+      const uint32_t top = q < 2 ? words[2] << (2 - q) : words[2] >> (q - 2);
+      const uint32_t sel = (words[q >> 2] >> (2 * (q & 3)) & 0x03030303u) | (top & 0x04040404u);
+      l = __builtin_amdgcn_perm(lo[1], lo[0], sel);
+      h = __builtin_amdgcn_perm(hi[1], hi[0], sel);
+    } else {
+      const uint32_t nibbles = words[q >> 1] >> (4 * (q & 1));
+      const uint32_t sel = nibbles & 0x07070707u;
+      // selectors 12 and 13 give 0 and 255: the mask of the upper eight
+      const uint32_t mask = __builtin_amdgcn_perm(0, 0, (nibbles >> 3 & 0x01010101u) | 0x0c0c0c0cu);
+      const uint32_t l0 = __builtin_amdgcn_perm(lo[1], lo[0], sel), l1 = __builtin_amdgcn_perm(lo[3], lo[2], sel);
+      const uint32_t h0 = __builtin_amdgcn_perm(hi[1], hi[0], sel), h1 = __builtin_amdgcn_perm(hi[3], hi[2], sel);
+      l = (l1 & mask) | (l0 & ~mask);
+      h = (h1 & mask) | (h0 & ~mask);
+    }
+    d0 = __builtin_amdgcn_perm(h, l, 0x05010400);
+    d1 = __builtin_amdgcn_perm(h, l, 0x07030602);
   }
 };
 
-template <class T>
-__global__ __launch_bounds__(256) void k_packed_any(PackedLayer L, GroupRows rows,
-                                                    const typename T::elem* __restrict__ x,
-                                                    typename T::elem* __restrict__ y) {
+// What one lane holds of a unit: its 32 codes, and the scales of their first and second half.
+template <int BITS, bool kFine>
+struct LaneCodes {
+  uint32_t words[BITS];
+  uint32_t scales;          // fp16: one, or two for groups of 16 (kFine); sub-block scales: two bytes
+  uint32_t d;               // SUPERBLOCK: fp16
+
+  // of lane slot `slot` (16 g + n) of unit (tile, kb)
+  __device__ __forceinline__ void load(const PackedLayer& L, int64_t tile, int kb, int slot) {
+    const int64_t unit = tile * L.blocks + kb;
+    const uint32_t* p = L.codes + (unit * 64 + slot) * BITS;
+#pragma unroll
+    for (int k = 0; k < BITS; ++k) words[k] = p[k];
+    d = 0;
+    if constexpr (kFine) {
+      if (L.sub) {
+        scales = reinterpret_cast<const uint16_t*>(L.sub)[unit * 64 + slot];
+        d = L.scales[(tile * L.scale_groups + (kb >> 1)) * 16 + (slot & 15)];
+      } else {
+        scales = reinterpret_cast<const uint32_t*>(L.scales)[unit * 64 + slot];
+      }
+    } else {
+      const int group = (kb * 128 + (slot >> 4) * 32) / L.gs;
+      scales = L.scales[(tile * L.scale_groups + group) * 16 + (slot & 15)];
+    }
+  }
+  __device__ __forceinline__ float scale(const PackedLayer& L, int half) const {
+    const auto f16 = [](uint32_t v) { return (float)__builtin_bit_cast(_Float16, (uint16_t)v); };
+    if constexpr (!kFine) return f16(scales);
+    if (L.sub) return f16(d) * (float)(half ? scales >> 8 : scales & 255);
+    return f16(half ? scales >> 16 : scales);
+  }
+};
+
+// ---- few rows: each workgroup has 16 output channels, its wavefronts share the inputs between them, and the
+// partial sums are added in LDS in a fixed order.
+constexpr int kMostWaves = 16;
+
+// 16 MI rows: y[r, n] for the 16 channels of `tile`.
+template <class T, int BITS, bool kFine, int MI>
+__device__ __forceinline__ void few_rows(const PackedLayer& L, const typename T::elem* x, typename T::elem* y,
+                                         int64_t first, int ms, int64_t tile, int n0, f32x4* part) {
   using E = typename T::elem;
-  PanelPlace at;
-  if (!find_panel(rows, kAnyTile, blockIdx.x, at)) return;
-  const int64_t first = at.first + (int64_t)at.panel * kAnyTile;
-  const int e = at.group, ms = (int)min(at.end - first, (int64_t)kAnyTile);
-  const AlongK<E> a{x + first * L.I, L.I, ms, L.I};
-  tile_any<T>(a, PackedWeights<E>{L, (int64_t)e * L.tiles}, 0, blockIdx.y * kAnyTile, L.I,
-              [&](int m, int n, float v) {
-                if (m < ms && n < L.O) y[(first + m) * L.O + n] = (E)v;
-              });
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int g = lane >> 4;
+  f32x4 acc[MI] = {};
+  constexpr int U = MI <= 2 ? 2 : 1;      // units in flight
+  LaneCodes<BITS, kFine> now[U], next[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    next[u].load(L, tile, min(wave + u * waves, L.blocks - 1), lane);
+  for (int kb0 = wave; kb0 < L.blocks; kb0 += U * waves) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) now[u] = next[u];
+#pragma unroll
+    for (int u = 0; u < U; ++u)   // past the end: the last unit again, not used
+      next[u].load(L, tile, min(kb0 + (U + u) * waves, L.blocks - 1), lane);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int kb = kb0 + u * waves;
+      if (kb >= L.blocks) break;
+      const int k0 = kb * 128 + g * 32;
+      typename T::frag a[MI][4] = {};
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+        if (i * 16 + (lane & 15) < ms) {
+          const E* row = x + (first + i * 16 + (lane & 15)) * L.I + k0;
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+            if (k0 + 8 * s < L.I) __builtin_memcpy(&a[i][s], row + 8 * s, 16);
+        }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const WeightTable<T, BITS> table(now[u].scale(L, kFine ? h : 0), L.levels);
+#pragma unroll
+        for (int s = 2 * h; s < 2 * h + 2; ++s) {
+          union { uint32_t d[4]; typename T::frag f; } w;
+          table.pick(now[u].words, 2 * s, w.d[0], w.d[1]);
+          table.pick(now[u].words, 2 * s + 1, w.d[2], w.d[3]);
+#pragma unroll
+          for (int i = 0; i < MI; ++i) acc[i] = T::mfma(w.f, a[i][s], acc[i]);
+        }
+      }
+    }
+  }
+  // acc: row of x lane % 16, channels 4 (lane / 16) .. + 3
+  if (waves > 1) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) part[(wave * MI + i) * 64 + lane] = acc[i];
+    __syncthreads();
+  }
+  for (int i = wave; i < MI; i += waves) {
+    f32x4 v = waves > 1 ? part[i * 64 + lane] : acc[0];
+    for (int w = 1; w < waves; ++w) v += part[(w * MI + i) * 64 + lane];
+    if (waves == 1)
+#pragma unroll
+      for (int k = 1; k < MI; ++k)
+        if (k == i) v = acc[k];
+    const int m = i * 16 + (lane & 15);
+    if (m < ms)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (n0 + 4 * g + c < L.O) y[(first + m) * L.O + n0 + 4 * g + c] = (E)v[c];
+  }
+  __syncthreads();   // `part` is free again
+}
+
+template <class T, int BITS, bool kFine>
+__global__ __launch_bounds__(64 * kMostWaves) void k_packed_few(PackedLayer L, GroupRows rows,
+                                                               const typename T::elem* __restrict__ x,
+                                                               typename T::elem* __restrict__ y) {
+  extern __shared__ __attribute__((aligned(16))) f32x4 part[];
+  int64_t first, end;
+  group_rows(rows, blockIdx.y, first, end);
+  const int64_t tile = (int64_t)blockIdx.y * L.tiles + blockIdx.x;
+  const int n0 = blockIdx.x * 16;
+  for (; first < end; first += 64) {
+    const int ms = (int)min(end - first, (int64_t)64);
+    if (ms <= 16)
+      few_rows<T, BITS, kFine, 1>(L, x, y, first, ms, tile, n0, part);
+    else if (ms <= 32)
+      few_rows<T, BITS, kFine, 2>(L, x, y, first, ms, tile, n0, part);
+    else
+      few_rows<T, BITS, kFine, 4>(L, x, y, first, ms, tile, n0, part);
+  }
 }
 
 }  // namespace
@@ -158,26 +318,51 @@ hipError_t launch_unpack_layer(const gsq_config& cfg, const uint8_t* packed, con
   const auto blocks = [](int64_t n) { return (unsigned)((n + 255) / 256); };
   const int64_t tiles = (int64_t)cfg.batch * L.tiles, weights = (int64_t)cfg.batch * L.O * L.I;
   const int packed_bits = cfg.layout == GSQ_LAYOUT_SUPERBLOCK ? 3 : L.bits;
-  const int64_t lanes = tiles * L.blocks * 64, scales = tiles * L.scale_groups * 16;
+  const int64_t lanes = tiles * L.blocks * 64;
+  const int64_t scales = tiles * (L.gs == 16 ? (int64_t)L.blocks * 128 : (int64_t)L.scale_groups * 16);
   k_unpack_codes<<<blocks(lanes), 256, 0, s>>>(packed, cfg.layout, packed_bits, L, lanes,
                                                const_cast<uint32_t*>(L.codes));
   const int64_t at_byte = cfg.layout == GSQ_LAYOUT_BASE3 ? (weights + 4) / 5 : weights * packed_bits / 8;
   k_unpack_scales<<<blocks(scales), 256, 0, s>>>(packed, cfg.layout, L, at_byte, scales,
                                                  const_cast<uint16_t*>(L.scales));
-  if (L.sub)
-    k_unpack_sub<<<blocks(scales * 16), 256, 0, s>>>(packed, L, scales * 16, const_cast<uint8_t*>(L.sub));
+  if (L.sub) k_unpack_sub<<<blocks(lanes * 2), 256, 0, s>>>(packed, L, lanes * 2, const_cast<uint8_t*>(L.sub));
   return hipGetLastError();
 }
+
+namespace {
+
+template <class T, int BITS, bool kFine>
+hipError_t launch_packed(const PackedLayer& L, const GroupRows& rows, const void* x, void* y, hipStream_t s) {
+  using E = typename T::elem;
+  const int waves = std::max(1, std::min(kMostWaves, L.blocks));
+  const dim3 grid(L.tiles, rows.groups);
+  k_packed_few<T, BITS, kFine><<<grid, 64 * waves, waves * 4 * 64 * sizeof(f32x4), s>>>(
+      L, rows, static_cast<const E*>(x), static_cast<E*>(y));
+  return hipGetLastError();
+}
+
+template <class T, int BITS>
+hipError_t launch_packed(const PackedLayer& L, const GroupRows& rows, const void* x, void* y, hipStream_t s) {
+  return L.sub || L.gs == 16 ? launch_packed<T, BITS, true>(L, rows, x, y, s)
+                             : launch_packed<T, BITS, false>(L, rows, x, y, s);
+}
+
+template <class T>
+hipError_t launch_packed(const PackedLayer& L, const GroupRows& rows, const void* x, void* y, hipStream_t s) {
+  switch (L.bits) {
+    case 1: return launch_packed<T, 1>(L, rows, x, y, s);
+    case 2: return launch_packed<T, 2>(L, rows, x, y, s);
+    case 3: return launch_packed<T, 3>(L, rows, x, y, s);
+    default: return launch_packed<T, 4>(L, rows, x, y, s);
+  }
+}
+
+}  // namespace
 
 hipError_t launch_packed_product(const PackedLayer& L, int dtype, const GroupRows& rows, const void* x,
                                  void* y, hipStream_t s) {
   if (rows.rows == 0) return hipSuccess;
-  const dim3 grid(most_panels(rows, kAnyTile), (L.O + kAnyTile - 1) / kAnyTile);
-  if (dtype == GSQ_DT_BF16)
-    k_packed_any<Bf16><<<grid, 256, 0, s>>>(L, rows, static_cast<const __bf16*>(x), static_cast<__bf16*>(y));
-  else
-    k_packed_any<F16><<<grid, 256, 0, s>>>(L, rows, static_cast<const _Float16*>(x), static_cast<_Float16*>(y));
-  return hipGetLastError();
+  return dtype == GSQ_DT_BF16 ? launch_packed<Bf16>(L, rows, x, y, s) : launch_packed<F16>(L, rows, x, y, s);
 }
 
 }  // namespace gsq

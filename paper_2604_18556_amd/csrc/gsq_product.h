@@ -37,13 +37,14 @@ struct ProductArgs {
 // 32-bit words of them (word_of_codes).  Channels beyond O and inputs beyond I have scale zero.
 struct PackedLayer {
   const uint32_t* codes;      // groups x tiles x blocks x 64 lanes x bits
-  const uint16_t* scales;     // fp16: groups x tiles x scale groups x 16 channels (SUPERBLOCK: d per 256)
-  const uint8_t* sub;         // SUPERBLOCK: groups x tiles x I / 16 x 16 channels, else NULL
+  const uint16_t* scales;     // fp16 (SUPERBLOCK: d): groups x tiles x scale groups x 16 channels, or for
+                              // groups of 16 inputs, two for each lane of each unit
+  const uint8_t* sub;         // SUPERBLOCK: the 6-bit scales, two for each lane of each unit; else NULL
   int32_t O, I, bits, gs;     // gs: inputs per fp16 scale
   int32_t tiles, blocks;      // of 16 channels, of 128 inputs
   int32_t scale_groups;       // per channel
   int32_t n_levels;
-  float levels[GSQ_MAX_LEVELS];
+  float levels[GSQ_MAX_LEVELS];   // those past n_levels repeat the last
 };
 
 hipError_t launch_product(int form, int dtype, const ProductArgs& p, hipStream_t s);

@@ -208,7 +208,7 @@ gsq_status gsq_linear_init(const gsq_config* cfg, const void* packed, size_t pac
   L.tiles = (L.O + 15) / 16;
   L.blocks = (L.I + 127) / 128;
   L.scale_groups = (L.blocks * 128 + L.gs - 1) / L.gs;
-  for (int k = 0; k < L.n_levels; ++k) L.levels[k] = cfg->levels[k];
+  for (int k = 0; k < GSQ_MAX_LEVELS; ++k) L.levels[k] = cfg->levels[k < L.n_levels ? k : L.n_levels - 1];
   h->groups = cfg->batch;
   hipError_t e = hipGetDevice(&h->device);
   if (e != hipSuccess) {
@@ -216,8 +216,9 @@ gsq_status gsq_linear_init(const gsq_config* cfg, const void* packed, size_t pac
     return gsq::hip_fail(e, "hipGetDevice");
   }
   const int64_t tiles = (int64_t)cfg->batch * L.tiles;
-  const size_t bytes[3] = {(size_t)tiles * L.blocks * 64 * L.bits * 4, (size_t)tiles * L.scale_groups * 16 * 2,
-                           super ? (size_t)tiles * L.scale_groups * 16 * 16 : 0};
+  const size_t lanes = (size_t)tiles * L.blocks * 64;
+  const size_t bytes[3] = {lanes * L.bits * 4, L.gs == 16 ? lanes * 2 * 2 : (size_t)tiles * L.scale_groups * 16 * 2,
+                           super ? lanes * 2 : 0};
   for (int i = 0; i < 3; ++i) {
     if (!bytes[i]) continue;
     void* p = nullptr;
