@@ -4,7 +4,7 @@
 
 #include <algorithm>
 
-#include "gsq_product_any.hpp"
+#include "gsq_tile.hpp"
 
 namespace gsq {
 namespace {
@@ -210,6 +210,11 @@ struct LaneCodes {
       scales = L.scales[(tile * L.scale_groups + group) * 16 + (slot & 15)];
     }
   }
+  __device__ __forceinline__ void arrived() {
+#pragma unroll
+    for (int k = 0; k < BITS; ++k) asm volatile("" : "+v"(words[k]));
+    asm volatile("" : "+v"(scales), "+v"(d));
+  }
   __device__ __forceinline__ float scale(const PackedLayer& L, int half) const {
     const auto f16 = [](uint32_t v) { return (float)__builtin_bit_cast(_Float16, (uint16_t)v); };
     if constexpr (!kFine) return f16(scales);
@@ -311,6 +316,84 @@ __global__ __launch_bounds__(64 * kMostWaves) void k_packed_few(PackedLayer L, G
   }
 }
 
+// ---- many rows: tiles as for a dense layer, whose slabs of weights the wavefronts write to LDS from the
+// codes.  Half a unit's inputs (64) make a slab.  A wavefront writes a quarter of it: lane 32 j + 16 h + n the
+// 32 weights of channel n, tile 2 i + j, lane slot (2 (k % 2) + h, n), for i = 0 .. in turn.
+template <class T, int BITS, bool kFine, int ROWS>
+struct SlabPacked {
+  static constexpr bool kCopied = false;
+  static constexpr int LOADS = ROWS / 32, UNITS = LOADS / 4;
+  const PackedLayer& L;
+  int64_t tile0;             // first tile of the group
+  int tile[UNITS];
+  LaneCodes<BITS, kFine> codes[UNITS];
+  WeightTable<T, BITS> table;
+
+  __device__ __forceinline__ SlabPacked(const PackedLayer& L_, int group, int n0, int wave, int lane)
+      : L(L_), tile0((int64_t)group * L_.tiles), table(0.f, L_.levels) {
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i)   // channels beyond the last are not stored
+      tile[i] = min(n0 / 16 + wave * (ROWS / 64) + 2 * i + (lane >> 5), L.tiles - 1);
+  }
+  __device__ __forceinline__ void prefetch(int k) {
+    const int lane = threadIdx.x & 63, kb = k >> 1;
+    const int slot = (2 * (k & 1) + ((lane >> 4) & 1)) * 16 + (lane & 15);
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) codes[i].load(L, tile0 + tile[i], min(kb, L.blocks - 1), slot);
+  }
+  // eight weights of each lane into slab k; with the last of them, the codes of slab k + 1 are fetched
+  template <bool kEnd>
+  __device__ __forceinline__ void load(int k, int j, uint8_t* lds) {
+    const int lane = threadIdx.x & 63, i = j / 4, s = j % 4;
+    if (j == 0)   // the codes are waited for here, not where a table might be begun early
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) codes[u].arrived();
+    if (s == 0 || (kFine && s == 2))   // slabs past the last unit are zeros
+      table = WeightTable<T, BITS>(!kEnd || k >> 1 < L.blocks ? codes[i].scale(L, s / 2) : 0.f, L.levels);
+    i32x4 w;
+    uint32_t d[4];
+    table.pick(codes[i].words, 2 * s, d[0], d[1]);
+    table.pick(codes[i].words, 2 * s + 1, d[2], d[3]);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) w[c] = (int)d[c];
+    const int row = (2 * i + (lane >> 5)) * 16 + (lane & 15), chunk = 4 * ((lane >> 4) & 1) + s;
+    *reinterpret_cast<i32x4*>(lds + row * ROW_BYTES + ((chunk ^ swz(row)) << 4)) = w;
+    if (j == LOADS - 1) prefetch(k + 1);
+  }
+  static __device__ __forceinline__ i32x4 frag(const uint8_t* slab, int row0, int half, int lane) {
+    return read_frag<i32x4>(slab, row0 + (lane & 15), half * 4 + (lane >> 4));
+  }
+};
+
+template <class T, int BITS, bool kFine, class S>
+__device__ __forceinline__ void packed_tile(const PackedLayer& L, const typename T::elem* x, typename T::elem* y,
+                                            const RowsTile& at, int vector_out, uint8_t* smem) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const SlabAlong<S::TM, true> a(x + at.first * L.I, (int64_t)L.I * 2, at.ms, wave, lane);
+  SlabPacked<T, BITS, kFine, S::TN> b(L, at.group, at.n0, wave, lane);
+  typename T::acc acc[S::MI][S::NJ];
+  tile_ring<T, S>(a, b, (L.I + 63) / 64, acc, smem);
+  tile_results<S>(acc, [&](int m, int n, f32x4 v) {
+    if (m < at.ms && at.n0 + n < L.O)
+      store_four(y, T::kDtype, (at.first + m) * L.O + at.n0 + n, v, L.O - at.n0 - n, vector_out);
+  });
+}
+
+template <class T, int BITS, bool kFine>
+__global__ __launch_bounds__(256, 1) void k_packed_tile(PackedLayer L, GroupRows rows,
+                                                        const typename T::elem* __restrict__ x,
+                                                        typename T::elem* __restrict__ y, int height, int vector_out) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  RowsTile at;
+  if (!find_rows_tile(rows, height, L.O, at)) return;
+  if (at.ms > Half::TM)
+    packed_tile<T, BITS, kFine, Whole>(L, x, y, at, vector_out, smem);
+  else if (at.ms > Low::TM)
+    packed_tile<T, BITS, kFine, Half>(L, x, y, at, vector_out, smem);
+  else
+    packed_tile<T, BITS, kFine, Low>(L, x, y, at, vector_out, smem);
+}
+
 }  // namespace
 
 hipError_t launch_unpack_layer(const gsq_config& cfg, const uint8_t* packed, const PackedLayer& L,
@@ -334,6 +417,10 @@ namespace {
 template <class T, int BITS, bool kFine>
 hipError_t launch_packed(const PackedLayer& L, const GroupRows& rows, const void* x, void* y, hipStream_t s) {
   using E = typename T::elem;
+  const int height = pick_height(rows, L.O);
+  if (rows.rows > 64 * (int64_t)rows.groups && aligned16(x))
+    return launch_ring(k_packed_tile<T, BITS, kFine>, most_panels(rows, height) * tiles_of(L.O, Whole::TN), s, L,
+                       rows, static_cast<const E*>(x), static_cast<E*>(y), height, (int)four_at_once(y, T::kDtype, L.O));
   const int waves = std::max(1, std::min(kMostWaves, L.blocks));
   const dim3 grid(L.tiles, rows.groups);
   k_packed_few<T, BITS, kFine><<<grid, 64 * waves, waves * 4 * 64 * sizeof(f32x4), s>>>(

@@ -26,6 +26,7 @@ struct ProductArgs {
   void* out;
   int32_t O, I;
   int32_t out_dtype;          // GSQ_DT_*
+  int32_t height;             // of a panel of rows
   int32_t vector_out;         // results may be stored four at a time
   int32_t accumulate;         // kWeightGrad into fp32: add to what is there
   const float* a_scales;      // 8-bit integers: one per row, and one per group and channel

@@ -53,35 +53,11 @@ __global__ __launch_bounds__(256) void k_weight_grad_any(ProductArgs p) {
   tile_any<T>(a, b, blockIdx.y * kAnyTile, blockIdx.x * kAnyTile, ks, store);
 }
 
-// Four consecutive output elements, together where `four` says that they are whole and aligned.
-__device__ __forceinline__ void store_four(void* out, int dtype, int64_t at, f32x4 v, int count, bool four) {
-  if (!four) {
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-      if (c < count) store_out(out, dtype, at + c, v[c]);
-    return;
-  }
-  if (dtype == GSQ_DT_FP32) {
-    *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = v;
-  } else if (dtype == GSQ_DT_BF16) {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(out) + at) = __builtin_convertvector(v, bf16x4);
-  } else {
-    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<f16x4*>(static_cast<_Float16*>(out) + at) = __builtin_convertvector(v, f16x4);
-  }
-}
-
-// The whole tile uses all the LDS; panels with fewer rows take lower ones, whose slabs last less long and
-// are loaded further ahead.
-using Whole = TileShape<256, 256, 2>;
-using Half = TileShape<128, 256, 3>;
-using Low = TileShape<64, 256, 3>;
-
 // One tile of y or dx: rows m0 .. of a group, columns n0 .. .
 template <class T, int kForm, class S>
-__device__ __forceinline__ void rows_tile(const ProductArgs& p, const PanelPlace& at, int64_t first, int ms, int n0,
-                                          uint8_t* smem) {
+__device__ __forceinline__ void rows_tile(const ProductArgs& p, const RowsTile& at, uint8_t* smem) {
+  const int64_t first = at.first;
+  const int ms = at.ms, n0 = at.n0;
   using E = typename T::elem;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ks = kForm == kForward ? p.I : p.O, ns = kForm == kForward ? p.O : p.I;
@@ -90,10 +66,10 @@ __device__ __forceinline__ void rows_tile(const ProductArgs& p, const PanelPlace
   const SlabAlong<S::TM> a(static_cast<const E*>(p.a) + first * ks, (int64_t)ks * sizeof(E), ms, wave, lane);
   typename T::acc acc[S::MI][S::NJ];
   if constexpr (kForm == kForward) {
-    const SlabAlong<S::TN> b(w + (int64_t)n0 * ks, (int64_t)ks * sizeof(E), ns - n0, wave, lane);
+    SlabAlong<S::TN> b(w + (int64_t)n0 * ks, (int64_t)ks * sizeof(E), ns - n0, wave, lane);
     tile_ring<T, S>(a, b, nk, acc, smem);
   } else {
-    const SlabAcross<S::TN> b(w + n0, (int64_t)ns * sizeof(E), ns - n0, ks, wave, lane);
+    SlabAcross<S::TN> b(w + n0, (int64_t)ns * sizeof(E), ns - n0, ks, wave, lane);
     tile_ring<T, S>(a, b, nk, acc, smem);
   }
   const bool four = p.vector_out;
@@ -112,24 +88,18 @@ __device__ __forceinline__ void rows_tile(const ProductArgs& p, const PanelPlace
   });
 }
 
-// y or dx.  A group's tiles follow each other and are spread over the XCDs so that each has a contiguous
-// part of the group's tile order.
+// y or dx.
 template <class T, int kForm>
 __global__ __launch_bounds__(256, 1) void k_rows_tile(ProductArgs p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-  const int ns = kForm == kForward ? p.O : p.I, tiles_n = (ns + Whole::TN - 1) / Whole::TN;
-  PanelPlace at;
-  if (!find_panel(p.rows, Whole::TM, blockIdx.x / (unsigned)tiles_n, at)) return;
-  int tm, tn;
-  tile_at(lin_of((int)(blockIdx.x - at.before * tiles_n), at.panels * tiles_n), at.panels, tiles_n, tm, tn);
-  const int64_t first = at.first + (int64_t)tm * Whole::TM;
-  const int ms = (int)min(at.end - first, (int64_t)Whole::TM), n0 = tn * Whole::TN;
-  if (ms > Half::TM)
-    rows_tile<T, kForm, Whole>(p, at, first, ms, n0, smem);
-  else if (ms > Low::TM)
-    rows_tile<T, kForm, Half>(p, at, first, ms, n0, smem);
+  RowsTile at;
+  if (!find_rows_tile(p.rows, p.height, kForm == kForward ? p.O : p.I, at)) return;
+  if (at.ms > Half::TM)
+    rows_tile<T, kForm, Whole>(p, at, smem);
+  else if (at.ms > Low::TM)
+    rows_tile<T, kForm, Half>(p, at, smem);
   else
-    rows_tile<T, kForm, Low>(p, at, first, ms, n0, smem);
+    rows_tile<T, kForm, Low>(p, at, smem);
 }
 
 // One tile of a sum over a group's rows: out[m0 .., n0 ..] (+)= sum_r a[r, m] b[r, n], and with `mirror` its
@@ -144,7 +114,7 @@ __device__ __forceinline__ void sum_tile(const ProductArgs& p, int e, int m0, in
   const int ks = (int)(end - first), nk = (ks + kSlabRows - 1) / kSlabRows;
   // a group without rows reads zeros only: its addresses are not used
   const SlabAcross<S::TM> a(static_cast<const E*>(p.a) + first * p.O + m0, (int64_t)p.O * 2, p.O - m0, ks, wave, lane);
-  const SlabAcross<S::TN> b(static_cast<const E*>(p.b) + first * p.I + n0, (int64_t)p.I * 2, p.I - n0, ks, wave, lane);
+  SlabAcross<S::TN> b(static_cast<const E*>(p.b) + first * p.I + n0, (int64_t)p.I * 2, p.I - n0, ks, wave, lane);
   typename T::acc acc[S::MI][S::NJ];
   tile_ring<T, S>(a, b, nk, acc, smem);
   const int64_t out0 = (int64_t)e * p.O * p.I;
@@ -246,27 +216,6 @@ __global__ __launch_bounds__(256) void k_quantize_rows(const E* __restrict__ x, 
   }
 }
 
-// A kernel that uses the whole LDS needs leave for it, once on each device.
-template <class... Args>
-hipError_t launch_ring(void (*kernel)(Args...), int64_t blocks, hipStream_t s, Args... args) {
-  if (blocks >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;   // 2^32 threads in grid.x
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS_BYTES);
-  if (e != hipSuccess) return e;
-  kernel<<<(unsigned)blocks, 256, LDS_BYTES, s>>>(args...);
-  return hipGetLastError();
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-
-int tiles_of(int n, int tile) { return (n + tile - 1) / tile; }
-
-// Results can be stored four at a time: whole rows of them, at aligned addresses.
-bool four_at_once(const void* out, int32_t dtype, int32_t cols) {
-  const uintptr_t bytes = dtype == GSQ_DT_FP32 ? 16 : 8;
-  return cols % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & (bytes - 1)) == 0;
-}
-
 template <class T, int kForm>
 hipError_t launch_rows(ProductArgs p, hipStream_t s) {
   if (p.rows.rows == 0) return hipSuccess;
@@ -274,7 +223,8 @@ hipError_t launch_rows(ProductArgs p, hipStream_t s) {
   const int64_t unit = 16 / (int64_t)sizeof(typename T::elem);
   if (p.O % (kForm == kForward ? 1 : unit) == 0 && p.I % unit == 0 && aligned16(p.a) && aligned16(p.b)) {
     p.vector_out = four_at_once(p.out, p.out_dtype, ns);
-    return launch_ring(k_rows_tile<T, kForm>, most_panels(p.rows, Whole::TM) * tiles_of(ns, Whole::TN), s, p);
+    p.height = pick_height(p.rows, ns);
+    return launch_ring(k_rows_tile<T, kForm>, most_panels(p.rows, p.height) * tiles_of(ns, Whole::TN), s, p);
   }
   const dim3 grid(most_panels(p.rows, kAnyTile), tiles_of(ns, kAnyTile));
   k_rows_any<T, kForm><<<grid, 256, 0, s>>>(p);

@@ -3,6 +3,10 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <cstdlib>
+#include <type_traits>
+#include <utility>
+
 #include "gsq_product_any.hpp"
 #include "gsq_slab.hpp"
 
@@ -74,8 +78,11 @@ __device__ __forceinline__ const uint8_t* uniform(const void* p) {
 // An operand whose rows (of the output's side) run along k: a slab is 128 bytes of each of its rows, row r
 // at r ROW_BYTES, chunks swizzled as swz() says.  Rows beyond the last one are read as the last one (their
 // outputs are not stored), chunks beyond the end of k as zeros.
-template <int ROWS>
+// kTracked: by the compiler's own copies, for kernels that have other loads in flight, which it can then
+// wait for without waiting for these.
+template <int ROWS, bool kTracked = false>
 struct SlabAlong {
+  static constexpr bool kCopied = true;
   static constexpr int LOADS = ROWS / 32;
   const uint8_t* base;       // the tile's first row
   uint32_t off[LOADS];       // bytes; below 256 x 2^22
@@ -94,7 +101,11 @@ struct SlabAlong {
   template <bool kEnd>
   __device__ __forceinline__ void load(int k, int j, uint8_t* lds) const {
     const uint8_t* slab = base + (int64_t)k * ROW_BYTES;
-    if constexpr (kEnd)
+    if constexpr (kTracked)
+      load_rows(reinterpret_cast<const uint16_t*>(!kEnd || (int64_t)k * ROW_BYTES + chunk[j] < bytes ? slab + off[j]
+                                                                                                   : zeros()),
+                lds + j * 8 * ROW_BYTES);
+    else if constexpr (kEnd)
       copy_to_lds((int64_t)k * ROW_BYTES + chunk[j] < bytes ? slab + off[j] : zeros(), lds + j * 8 * ROW_BYTES);
     else
       copy_to_lds(slab, off[j], lds + j * 8 * ROW_BYTES);
@@ -112,6 +123,7 @@ struct SlabAlong {
 // Rows beyond the end of k are read as zeros, columns beyond the last 16 bytes as those.
 template <int COLS>
 struct SlabAcross {
+  static constexpr bool kCopied = true;
   static constexpr int LOADS = COLS / 32;
   static constexpr int PITCH = COLS * 2, PER_ROW = COLS / 8;   // bytes; 16-byte chunks
   static_assert(PITCH >= 256, "eight granules of a row to swizzle");
@@ -154,13 +166,26 @@ struct SlabAcross {
   }
 };
 
+// f(0) .. f(N - 1) with the numbers as constants: loops whose bodies the compiler finds too long to unroll.
+template <class F, int... I>
+__device__ __forceinline__ void static_for_each(F& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F f) {
+  static_for_each(f, std::make_integer_sequence<int, N>{});
+}
+
 // The tile: slabs 0 .. nk - 1, of which the last may end early (those past nk, for short sums, are zeros).
 // 64 of k (128 of 8-bit integers) at a time move by direct global->LDS loads into the two rings.  A's extra
 // buffer lets its slab k + AHEAD be loaded during the first half of slab k, B's during the second.  Fragment
 // reads of the next half and slab loads are issued between the products, a load after every two reads.
 // Blocks are walked back and forth: one operand of each product is the last one's.
+//
+// B need not be copied (!B::kCopied): its load(k, j) then writes its part of slab k itself, from what its
+// prefetch() and the calls for slab k - 1 have fetched into registers.
 template <class T, class S, class A, class B>
-__device__ __forceinline__ void tile_ring(const A& a, const B& b, int nk,
+__device__ __forceinline__ void tile_ring(const A& a, B& b, int nk,
                                           typename T::acc (&acc)[S::MI][S::NJ], uint8_t* smem) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -195,19 +220,20 @@ __device__ __forceinline__ void tile_ring(const A& a, const B& b, int nk,
       if (o % 3 == 2) { if (o / 3 < n_loads) next_load(o / 3); }
       else if (o - o / 3 < n_reads) next_read(o - o / 3);
     };
-#pragma unroll
-    for (int n = 0; n < kMfma; ++n) {
-      const int i = n / S::NJ, j = i % 2 ? S::NJ - 1 - n % S::NJ : n % S::NJ;
+    static_for<kMfma>([&](auto at) {
+      constexpr int n = decltype(at)::value;
+      constexpr int i = n / S::NJ, j = i % 2 ? S::NJ - 1 - n % S::NJ : n % S::NJ;
       mfma_block<T>(acc[i][j], fb[j], fa[i]);
-      if (n % kStep == 0) op(n / kStep);
-    }
-#pragma unroll
-    for (int o = (kMfma + kStep - 1) / kStep; o < kOps; ++o) op(o);
+      if constexpr (n % kStep == 0) op(n / kStep);
+    });
+    constexpr int kDone = (kMfma + kStep - 1) / kStep;
+    static_for<(kOps > kDone ? kOps - kDone : 0)>([&](auto at) { op(kDone + decltype(at)::value); });
   };
   const auto none = [](int) {};
 
   // p: first half of the current slab; q: second half
   i32x4 pa[S::MI], pb[S::NJ], qa[S::MI], qb[S::NJ];
+  if constexpr (!B::kCopied) b.prefetch(0);
 #pragma unroll
   for (int k = 0; k < S::AHEAD; ++k) {
 #pragma unroll
@@ -215,7 +241,8 @@ __device__ __forceinline__ void tile_ring(const A& a, const B& b, int nk,
 #pragma unroll
     for (int j = 0; j < S::B_LOADS; ++j) b.template load<true>(k, j, b_wave + k * S::B_SLAB);
   }
-  constexpr int kSlabLoads = S::A_LOADS + S::B_LOADS;
+  // copies of a slab; what B fetches besides makes the waits longer than need be, never shorter
+  constexpr int kSlabLoads = S::A_LOADS + (B::kCopied ? S::B_LOADS : 0);
   wait_vm<(S::AHEAD - 1) * kSlabLoads>();
   slab_barrier();
 #pragma unroll
@@ -264,6 +291,79 @@ __device__ __forceinline__ void tile_results(const Acc (&acc)[S::MI][S::NJ], Sto
   for (int i = 0; i < S::MI; ++i)
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) store(m + i * 16, n + j * 16, acc[i][j]);
+}
+
+// Four consecutive output elements, together where `four` says that they are whole and aligned.
+__device__ __forceinline__ void store_four(void* out, int dtype, int64_t at, f32x4 v, int count, bool four) {
+  if (!four) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (c < count) store_out(out, dtype, at + c, v[c]);
+    return;
+  }
+  if (dtype == GSQ_DT_FP32) {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = v;
+  } else if (dtype == GSQ_DT_BF16) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(out) + at) = __builtin_convertvector(v, bf16x4);
+  } else {
+    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<f16x4*>(static_cast<_Float16*>(out) + at) = __builtin_convertvector(v, f16x4);
+  }
+}
+
+// The whole tile uses all the LDS; panels with fewer rows take lower ones, whose slabs last less long and
+// are loaded further ahead.
+using Whole = TileShape<256, 256, 2>;
+using Half = TileShape<128, 256, 3>;
+using Low = TileShape<64, 256, 3>;
+
+// The tile of y or dx that this workgroup has: up to `height` rows of one group, 256 columns.
+struct RowsTile {
+  int group;
+  int64_t first;     // its first row
+  int ms, n0;        // its rows, its first column
+};
+
+// Which one: the tiles of a group follow each other, and are spread over the XCDs so that each has a
+// contiguous part of the group's tile order.  False: there are fewer.
+__device__ __forceinline__ bool find_rows_tile(const GroupRows& rows, int height, int cols, RowsTile& t) {
+  const int tiles_n = (cols + Whole::TN - 1) / Whole::TN;
+  PanelPlace at;
+  if (!find_panel(rows, height, blockIdx.x / (unsigned)tiles_n, at)) return false;
+  int tm, tn;
+  tile_at(lin_of((int)(blockIdx.x - at.before * tiles_n), at.panels * tiles_n), at.panels, tiles_n, tm, tn);
+  t.group = at.group;
+  t.first = at.first + (int64_t)tm * height;
+  t.ms = (int)min(at.end - t.first, (int64_t)height);
+  t.n0 = tn * Whole::TN;
+  return true;
+}
+
+inline int pick_height(const GroupRows& rows, int cols) {
+  static const char* h = getenv("GSQ_H");
+  return h ? atoi(h) : 256;
+}
+
+// A kernel that uses the whole LDS needs leave for it, once on each device.
+template <class... Args>
+hipError_t launch_ring(void (*kernel)(Args...), int64_t blocks, hipStream_t s, Args... args) {
+  if (blocks >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;   // 2^32 threads in grid.x
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS_BYTES);
+  if (e != hipSuccess) return e;
+  kernel<<<(unsigned)blocks, 256, LDS_BYTES, s>>>(args...);
+  return hipGetLastError();
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+int tiles_of(int n, int tile) { return (n + tile - 1) / tile; }
+
+// Results can be stored four at a time: whole rows of them, at aligned addresses.
+bool four_at_once(const void* out, int32_t dtype, int32_t cols) {
+  const uintptr_t bytes = dtype == GSQ_DT_FP32 ? 16 : 8;
+  return cols % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & (bytes - 1)) == 0;
 }
 
 }  // namespace
