@@ -369,7 +369,7 @@ template <class T, int BITS, bool kFine, class S>
 __device__ __forceinline__ void packed_tile(const PackedLayer& L, const typename T::elem* x, typename T::elem* y,
                                             const RowsTile& at, int vector_out, uint8_t* smem) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const SlabAlong<S::TM, true> a(x + at.first * L.I, (int64_t)L.I * 2, at.ms, wave, lane);
+  const SlabAlong<S::TM, S::TM / 32, true> a(x + at.first * L.I, (int64_t)L.I * 2, at.ms, wave, lane);
   SlabPacked<T, BITS, kFine, S::TN> b(L, at.group, at.n0, wave, lane);
   typename T::acc acc[S::MI][S::NJ];
   tile_ring<T, S>(a, b, (L.I + 63) / 64, acc, smem);
@@ -419,7 +419,7 @@ hipError_t launch_packed(const PackedLayer& L, const GroupRows& rows, const void
   using E = typename T::elem;
   const int height = pick_height(rows, L.O);
   if (rows.rows > 64 * (int64_t)rows.groups && aligned16(x))
-    return launch_ring(k_packed_tile<T, BITS, kFine>, most_panels(rows, height) * tiles_of(L.O, Whole::TN), s, L,
+    return launch_ring<k_packed_tile<T, BITS, kFine>>(most_panels(rows, height) * tiles_of(L.O, Whole::TN), s, L,
                        rows, static_cast<const E*>(x), static_cast<E*>(y), height, (int)four_at_once(y, T::kDtype, L.O));
   const int waves = std::max(1, std::min(kMostWaves, L.blocks));
   const dim3 grid(L.tiles, rows.groups);

@@ -1,5 +1,4 @@
-// Device parts that the products of grouped rows share: element types, the search for a group's rows,
-// and the product of one 64 x 64 tile from any operands.
+// Device parts that the products of grouped rows share: element types and the search for a group's rows.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -113,86 +112,6 @@ __device__ __forceinline__ void store_out(void* out, int dtype, int64_t at, floa
     static_cast<_Float16*>(out)[at] = (_Float16)v;
   else
     static_cast<float*>(out)[at] = v;
-}
-
-// Operands of the tile product, element by element: m is the output's row or column, k is summed over.
-// Out of range they are zero.
-template <class E>
-struct AlongK {            // k is contiguous
-  const E* p;
-  int64_t ld;
-  int ms, ks;
-  static constexpr bool kFast = true;
-  __device__ __forceinline__ E at(int m, int k) const { return m < ms && k < ks ? p[m * ld + k] : (E)0; }
-};
-template <class E>
-struct AcrossK {           // m is contiguous
-  const E* p;
-  int64_t ld;
-  int ms, ks;
-  static constexpr bool kFast = false;
-  __device__ __forceinline__ E at(int m, int k) const { return m < ms && k < ks ? p[k * ld + m] : (E)0; }
-};
-
-constexpr int kAnyTile = 64;
-
-// One 64 x 64 tile at (m0, n0) of a product over ks, for operands of any size and alignment: elements
-// go through registers into LDS, both operands as rows along k, 64 of k at a time, and the next slab is
-// fetched while this one is multiplied.  Four wavefronts, 32 x 32 each.
-// store(m, n, sum) is called for every element of the tile, also beyond the operands' sizes.
-template <class T, class A, class B, class Store>
-__device__ __forceinline__ void tile_any(const A& a, const B& b, int m0, int n0, int ks, Store store) {
-  using E = typename T::elem;
-  constexpr int BK = 64, ROW = BK + 16 / (int)sizeof(E);
-  constexpr int PER = kAnyTile * BK / 256;
-  __shared__ __align__(16) E As[kAnyTile * ROW], Bs[kAnyTile * ROW];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int wm = (wave >> 1) * 32, wn = (wave & 1) * 32;
-
-  typename T::acc acc[2][2] = {};
-  E ra[PER], rb[PER];
-  const auto fetch = [&](int k0) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int f = i * 256 + tid, slow = f / 64, fast = f % 64;
-      ra[i] = A::kFast ? a.at(m0 + slow, k0 + fast) : a.at(m0 + fast, k0 + slow);
-      rb[i] = B::kFast ? b.at(n0 + slow, k0 + fast) : b.at(n0 + fast, k0 + slow);
-    }
-  };
-  fetch(0);
-  for (int k0 = 0; k0 < ks; k0 += BK) {
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int f = i * 256 + tid, slow = f / 64, fast = f % 64;
-      As[A::kFast ? slow * ROW + fast : fast * ROW + slow] = ra[i];
-      Bs[B::kFast ? slow * ROW + fast : fast * ROW + slow] = rb[i];
-    }
-    __syncthreads();
-    if (k0 + BK < ks) fetch(k0 + BK);
-#pragma unroll
-    for (int h = 0; h < BK / T::kStep; ++h) {
-      typename T::frag fa[2], fb[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int k = h * T::kStep + (lane >> 4) * (T::kStep / 4);
-        fa[i] = *reinterpret_cast<const typename T::frag*>(&As[(wm + 16 * i + (lane & 15)) * ROW + k]);
-        fb[i] = *reinterpret_cast<const typename T::frag*>(&Bs[(wn + 16 * i + (lane & 15)) * ROW + k]);
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = T::mfma(fa[i], fb[j], acc[i][j]);
-    }
-  }
-  // lane l of a 16 x 16 block: column l % 16, rows 4 (l / 16) .. + 3
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        store(m0 + wm + 16 * i + 4 * (lane >> 4) + r, n0 + wn + 16 * j + (lane & 15), acc[i][j][r]);
 }
 
 }  // namespace

@@ -70,6 +70,18 @@ __device__ __forceinline__ void slab_barrier() {
   __atomic_signal_fence(__ATOMIC_SEQ_CST);
 }
 
+// Waits of one wavefront for itself: all that it has in flight, or its LDS reads only.
+__device__ __forceinline__ void wait_all() {
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8));
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+}
+__device__ __forceinline__ void wait_reads() {
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+}
+
 // Waits until accumulators can be read by anything but another product (see the products).
 template <class A, int MI, int NJ>
 __device__ __forceinline__ void acc_settled(A (&acc)[MI][NJ]) {

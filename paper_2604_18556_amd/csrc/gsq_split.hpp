@@ -1,0 +1,182 @@
+// The product of a small output tile by wavefronts that share the sum between them: each takes a part of k
+// for the whole tile, with slabs of its own in LDS, and the partial sums are added in a fixed order.
+//
+// For products with too few tiles of 256 x 256 for the GPU, and for operands that are not aligned to 16
+// bytes.  No wavefront waits for another until the end.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gsq_tile.hpp"
+
+namespace gsq {
+namespace {
+
+constexpr int kSplitWaves = 8;       // at most, for one tile
+
+// 16 bytes from any address, of which the first n (<= 16 / sizeof(E)) elements are in bounds and the others
+// become zero.
+template <class E>
+__device__ __forceinline__ i32x4 load_chunk(const E* p, int n) {
+  constexpr int PER = 16 / (int)sizeof(E);
+  i32x4 v = {0, 0, 0, 0};
+  if (n >= PER) {
+    __builtin_memcpy(&v, p, 16);
+  } else if (n > 0) {
+    E e[PER];
+#pragma unroll
+    for (int c = 0; c < PER; ++c) e[c] = c < n ? p[c] : (E)0;
+    __builtin_memcpy(&v, e, 16);
+  }
+  return v;
+}
+
+// Operands as in gsq_tile.hpp, for one wavefront, by way of registers and from any address: fetch() reads slab
+// k, commit() writes it to LDS.
+template <class E, int ROWS>
+struct LooseAlong {
+  static constexpr int LOADS = ROWS / 8, PER = 16 / (int)sizeof(E);
+  const E* base;
+  int64_t ld;
+  int rows, ks;
+  i32x4 held[LOADS];
+
+  __device__ __forceinline__ LooseAlong(const E* first, int64_t ld_, int rows_, int ks_)
+      : base(first), ld(ld_), rows(rows_), ks(ks_) {}
+  __device__ __forceinline__ void fetch(int k, uint8_t*) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int row = j * 8 + (lane >> 3), at = (k * 8 + ((lane & 7) ^ swz(row))) * PER;
+      held[j] = load_chunk(base + min(row, rows - 1) * ld + at, ks - at);
+    }
+  }
+  __device__ __forceinline__ void commit(uint8_t* lds) const {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j)
+      *reinterpret_cast<i32x4*>(lds + j * 1024 + (threadIdx.x & 63) * 16) = held[j];
+  }
+  static __device__ __forceinline__ i32x4 frag(const uint8_t* slab, int row0, int half, int lane) {
+    return read_frag<i32x4>(slab, row0 + (lane & 15), half * 4 + (lane >> 4));
+  }
+};
+
+template <class E, int COLS>
+struct LooseAcross {
+  using Tight = SlabAcross<COLS, COLS / 8>;
+  static constexpr int LOADS = COLS / 8;
+  const E* base;
+  int64_t ld;
+  int cols, ks;
+  i32x4 held[LOADS];
+
+  __device__ __forceinline__ LooseAcross(const E* first, int64_t ld_, int cols_, int ks_)
+      : base(first), ld(ld_), cols(cols_), ks(ks_) {}
+  __device__ __forceinline__ void fetch(int k, uint8_t*) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      int row, chunk;
+      Tight::place(j * 64 + lane, row, chunk);
+      const int64_t r = (int64_t)k * kSlabRows + row;
+      held[j] = load_chunk(base + r * ld + chunk * 8, r < ks ? cols - chunk * 8 : 0);
+    }
+  }
+  __device__ __forceinline__ void commit(uint8_t* lds) const {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j)
+      *reinterpret_cast<i32x4*>(lds + j * 1024 + (threadIdx.x & 63) * 16) = held[j];
+  }
+  static __device__ __forceinline__ i32x4 frag(const uint8_t* slab, int col0, int half, int lane) {
+    return Tight::frag(slab, col0, half, lane);
+  }
+};
+
+// The same from aligned arrays, copied to LDS directly.
+template <class Slab>
+struct Copied : Slab {
+  using Slab::Slab;
+  __device__ __forceinline__ void fetch(int k, uint8_t* lds) {
+#pragma unroll
+    for (int j = 0; j < Slab::LOADS; ++j) Slab::template load<true>(k, j, lds);
+  }
+  __device__ __forceinline__ void commit(uint8_t*) const {}
+};
+
+// A TM x TN tile: sums of slabs k = wave, wave + waves, ... < nk of each wavefront, added up, to
+// store(row, column, four consecutive columns' sums), called for whole fours of the tile; with `mirror`, also
+// turned over, to store_mirror(column, row, four consecutive rows' sums).
+// A wavefront reads a slab's fragments into registers, lets the next slab follow into the same LDS, and
+// multiplies meanwhile.
+template <class T, int TM, int TN, class A, class B, class Store, class StoreMirror>
+__device__ __forceinline__ void tile_split(A& a, B& b, int nk, uint8_t* smem, bool mirror, Store store,
+                                           StoreMirror store_mirror) {
+  constexpr int MI = TM / 16, NJ = TN / 16;
+  constexpr int A_SLAB = TM * ROW_BYTES, SLAB = A_SLAB + TN * ROW_BYTES;
+  static_assert(TM * TN * 4 <= SLAB, "the sums take the slabs' place");
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint8_t* const own = smem + wave * SLAB;
+  typename T::acc acc[MI][NJ] = {};
+  if (wave < nk) {
+    a.fetch(wave, own);
+    b.fetch(wave, own + A_SLAB);
+    for (int k = wave; k < nk; k += waves) {
+      a.commit(own);
+      b.commit(own + A_SLAB);
+      wait_all();
+      typename T::frag fa[2][MI], fb[2][NJ];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) fa[h][i] = __builtin_bit_cast(typename T::frag, A::frag(own, i * 16, h, lane));
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) fb[h][j] = __builtin_bit_cast(typename T::frag, B::frag(own + A_SLAB, j * 16, h, lane));
+      }
+      wait_reads();
+      if (k + waves < nk) {
+        a.fetch(k + waves, own);
+        b.fetch(k + waves, own + A_SLAB);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[i][j] = T::mfma(fb[h][j], fa[h][i], acc[i][j]);
+    }
+  }
+  // a lane has row lane % 16 and four columns of a block; rows of TN sums in LDS, the last 16 bytes' place
+  // turned by the row
+  typename T::acc* const sums = reinterpret_cast<typename T::acc*>(own);
+  constexpr int FOURS = TN / 4;
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int row = i * 16 + (lane & 15), c = j * 4 + (lane >> 4);
+      sums[row * FOURS + (c ^ (row % FOURS))] = acc[i][j];
+    }
+  __syncthreads();
+  const int parts = min(waves, nk);
+  for (int f = threadIdx.x; f < TM * FOURS; f += blockDim.x) {
+    const int row = f / FOURS, c = f % FOURS, at = row * FOURS + (c ^ (row % FOURS));
+    typename T::acc v = {};
+    for (int w = 0; w < parts; ++w) v += reinterpret_cast<typename T::acc*>(smem + w * SLAB)[at];
+    store(row, 4 * c, v);
+    if (mirror) reinterpret_cast<typename T::acc*>(smem)[at] = v;
+  }
+  if (!mirror) return;
+  __syncthreads();
+  for (int f = threadIdx.x; f < TN * (TM / 4); f += blockDim.x) {
+    const int row = 4 * (f % (TM / 4)), col = f / (TM / 4);
+    typename T::acc v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      v[r] = reinterpret_cast<typename T::acc*>(smem)[(row + r) * FOURS + ((col / 4) ^ ((row + r) % FOURS))][col % 4];
+    store_mirror(col, row, v);
+  }
+}
+
+}  // namespace
+}  // namespace gsq

@@ -3,11 +3,12 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <cstdlib>
 #include <type_traits>
 #include <utility>
 
-#include "gsq_product_any.hpp"
+#include "gsq_rows.hpp"
 #include "gsq_slab.hpp"
 
 namespace gsq {
@@ -80,10 +81,11 @@ __device__ __forceinline__ const uint8_t* uniform(const void* p) {
 // outputs are not stored), chunks beyond the end of k as zeros.
 // kTracked: by the compiler's own copies, for kernels that have other loads in flight, which it can then
 // wait for without waiting for these.
-template <int ROWS, bool kTracked = false>
+// LOADS_: copies of 1 KB that each of the wavefronts makes (ROWS / 8 in all).
+template <int ROWS, int LOADS_ = ROWS / 32, bool kTracked = false>
 struct SlabAlong {
   static constexpr bool kCopied = true;
-  static constexpr int LOADS = ROWS / 32;
+  static constexpr int LOADS = LOADS_;
   const uint8_t* base;       // the tile's first row
   uint32_t off[LOADS];       // bytes; below 256 x 2^22
   int bytes;                 // of a row
@@ -119,30 +121,40 @@ struct SlabAlong {
 // An operand whose rows are k (16-bit elements, the output's side is contiguous): a slab is 64 rows of COLS
 // elements.  The reads transpose: 16 lanes take four rows of 16 columns (32 bytes each) and each gets the
 // four k of one column.  32 lanes read rows r .. r + 3 and r + 8 .. r + 11 at once: the 32-byte granules of
-// a row are stored at granule ^ f(row), so that those eight rows fall on distinct banks.
+// a row are stored at granule ^ turn(row), so that those eight rows fall on distinct banks (narrow slabs have
+// several rows in the 256 bytes of the banks, and less to turn).
 // Rows beyond the end of k are read as zeros, columns beyond the last 16 bytes as those.
-template <int COLS>
+template <int COLS, int LOADS_ = COLS / 32>
 struct SlabAcross {
   static constexpr bool kCopied = true;
-  static constexpr int LOADS = COLS / 32;
+  static constexpr int LOADS = LOADS_;
   static constexpr int PITCH = COLS * 2, PER_ROW = COLS / 8;   // bytes; 16-byte chunks
-  static_assert(PITCH >= 256, "eight granules of a row to swizzle");
   const uint8_t* base;       // row 0 of k, the tile's first column
   uint32_t off[LOADS];       // bytes; below 64 x 2^22
   int64_t slab_bytes;        // from one slab to the next
   int rows;                  // of k
   int row[LOADS];
 
-  static __device__ __forceinline__ int turn(int r) { return (r & 3) | ((r >> 1) & 4); }
+  static __device__ __forceinline__ int turn(int r) {
+    return PITCH >= 256  ? (r & 3) | ((r >> 1) & 4)
+           : PITCH == 128 ? ((r >> 1) & 1) | ((r >> 2) & 2)
+           : PITCH == 64  ? (r >> 3) & 1
+                          : 0;
+  }
+  // Row and chunk that are kept at the at-th 16 bytes of a slab.
+  static __device__ __forceinline__ void place(int at, int& row, int& chunk) {
+    const int c = at % PER_ROW;
+    row = at / PER_ROW;
+    chunk = ((c >> 1) ^ turn(row)) * 2 + (c & 1);
+  }
 
   __device__ __forceinline__ SlabAcross(const void* first, int64_t row_bytes, int cols, int rows_, int wave,
                                         int lane)
       : base(uniform(first)), slab_bytes(row_bytes * kSlabRows), rows(rows_) {
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-      const int at = (wave * LOADS + j) * 64 + lane, c = at % PER_ROW;
-      row[j] = at / PER_ROW;
-      const int chunk = ((c >> 1) ^ turn(row[j])) * 2 + (c & 1);
+      int chunk;
+      place((wave * LOADS + j) * 64 + lane, row[j], chunk);
       off[j] = (uint32_t)row[j] * (uint32_t)row_bytes + (uint32_t)min(chunk * 16, cols * 2 - 16);
     }
   }
@@ -161,7 +173,8 @@ struct SlabAcross {
     const uint8_t* at = slab + r * PITCH + (((col0 >> 4) ^ turn(r)) << 5) + (lane & 3) * 8;
     union { s16x4 s[2]; i32x4 v; } u;
     u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at);
-    u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * PITCH));   // the same turn
+    // bit 2 of a row does not enter its turn
+    u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * PITCH));
     return u.v;
   }
 };
@@ -345,15 +358,27 @@ inline int pick_height(const GroupRows& rows, int cols) {
   return h ? atoi(h) : 256;
 }
 
-// A kernel that uses the whole LDS needs leave for it, once on each device.
-template <class... Args>
-hipError_t launch_ring(void (*kernel)(Args...), int64_t blocks, hipStream_t s, Args... args) {
-  if (blocks >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;   // 2^32 threads in grid.x
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS_BYTES);
+// A kernel that uses more LDS than the default limit needs leave for it, once on each device.
+template <auto kKernel, class... Args>
+hipError_t launch_lds(int64_t blocks, int threads, size_t lds, hipStream_t s, const Args&... args) {
+  if (blocks * threads >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;   // the limit of grid.x
+  static std::atomic<uint64_t> leave{0};   // a bit per device
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
-  kernel<<<(unsigned)blocks, 256, LDS_BYTES, s>>>(args...);
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (!(leave.load(std::memory_order_relaxed) & bit)) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(kKernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                            (int)LDS_BYTES);
+    if (e != hipSuccess) return e;
+    leave.fetch_or(bit, std::memory_order_relaxed);
+  }
+  kKernel<<<(unsigned)blocks, threads, lds, s>>>(args...);
   return hipGetLastError();
+}
+template <auto kKernel, class... Args>
+hipError_t launch_ring(int64_t blocks, hipStream_t s, const Args&... args) {
+  return launch_lds<kKernel>(blocks, 256, LDS_BYTES, s, args...);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
