@@ -350,116 +350,131 @@ class Layer:
 # O x I (or O x I for one group), and ``offsets`` a device int64 tensor of groups + 1 row offsets (None
 # for one group that has every row).
 
-def _grouped(tensors, groups, rows, out_features, in_features, dtype, offsets):
-    """The sizes as the library takes them, after checks of the tensors ({name: (tensor, shapes,
-    dtypes)}): on the current device, dense, of one of the shapes and types."""
+def _checked(args, offsets, groups):
+    """Check tensor arguments, (name, tensor, shape, dtypes) each, and the offsets: dense, of that shape and
+    one of those types, and on the current device, which is returned.  These calls take microseconds, so
+    the checks are made without building anything unless one fails."""
     import torch
-    codes = {torch.bfloat16: DT_BF16, torch.float16: DT_FP16}
-    if dtype not in codes:
-        raise TypeError(f"rows must be bfloat16 or float16, got {dtype}")
-    if offsets is None:
-        if groups != 1:
-            raise ValueError(f"{groups} groups need offsets")
-    else:
-        tensors = dict(tensors, offsets=(offsets, [(groups + 1,)], (torch.int64,)))
-    for name, (t, shapes, dtypes) in tensors.items():
-        if tuple(t.shape) not in shapes:
-            raise ValueError(f"{name} must have the shape {' or '.join(map(str, shapes))}, got "
-                             f"{tuple(t.shape)}")
-    for name, (t, _, dtypes) in tensors.items():
-        _on_current_device(t, name)
+    device = torch.cuda.current_device() if torch.cuda.is_initialized() else -1
+    if offsets is not None:
+        args += (("offsets", offsets, (groups + 1,), (torch.int64,)),)
+    elif groups != 1:
+        raise ValueError(f"{groups} groups need offsets")
+    for name, t, shape, dtypes in args:
+        if not (t.shape == shape and t.dtype in dtypes and t.is_contiguous() and t.get_device() == device >= 0):
+            _refuse(args, device)
+    return device
+
+
+def _refuse(args, device):
+    for name, t, shape, _ in args:
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
+    for name, t, _, dtypes in args:
         _arg(t, name, t.numel(), dtypes)
-    return CGrouped(groups, out_features, in_features, codes[dtype], rows)
+        if t.get_device() != device:
+            raise ValueError(f"{name} is on {t.device}, but device {device} is current")
+    raise ValueError("arguments do not fit together")
 
 
-def _on_current_device(t, name):
+def _raw_stream(stream, device):
     import torch
-    if t.is_cuda and t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, but device {torch.cuda.current_device()} is current")
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device)   # current_stream() without building an object
 
 
-def _weight_sizes(w):
-    if w.dim() not in (2, 3):
-        raise ValueError(f"w must be groups x O x I or O x I, got {tuple(w.shape)}")
-    return (1, *w.shape) if w.dim() == 2 else tuple(w.shape)
+def _rows_dtype(t):
+    import torch
+    if t.dtype is torch.bfloat16:
+        return DT_BF16
+    if t.dtype is torch.float16:
+        return DT_FP16
+    raise TypeError(f"rows must be bfloat16 or float16, got {t.dtype}")
+
+
+def _weight_sizes(w, name="w"):
+    shape = w.shape
+    if len(shape) == 3:
+        return shape
+    if len(shape) == 2:
+        return (1, *shape)
+    raise ValueError(f"{name} must be groups x O x I or O x I, got {tuple(shape)}")
 
 
 def _row_count(x, name):
-    if x.dim() != 2:
+    if len(x.shape) != 2:
         raise ValueError(f"{name} must be rows x features, got {tuple(x.shape)}")
     return x.shape[0]
 
 
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
 def grouped_forward(x, w, out, offsets=None, stream=None):
     """out = x W_e^T for the rows of each group (x, w, out: bfloat16 or float16)."""
-    (n, o, i), r = _weight_sizes(w), _row_count(x, "x")
-    g = _grouped({"x": (x, [(r, i)], (x.dtype,)), "w": (w, [tuple(w.shape)], (x.dtype,)),
-                  "out": (out, [(r, o)], (x.dtype,))}, n, r, o, i, x.dtype, offsets)
-    _check(load().gsq_grouped_forward(ctypes.byref(g), _ptr(x), _ptr(w), _ptr(offsets), _ptr(out),
-                                      _stream(stream)))
+    (n, o, i), r, dt, types = _weight_sizes(w), _row_count(x, "x"), _rows_dtype(x), (x.dtype,)
+    dev = _checked((("x", x, (r, i), types), ("w", w, w.shape, types), ("out", out, (r, o), types)), offsets, n)
+    _check(load().gsq_grouped_forward(ctypes.byref(CGrouped(n, o, i, dt, r)), x.data_ptr(), w.data_ptr(),
+                                      _address(offsets), out.data_ptr(), _raw_stream(stream, dev)))
 
 
 def grouped_input_grad(dy, w, out, offsets=None, stream=None):
     """out = dy W_e, the gradient of grouped_forward's x."""
-    (n, o, i), r = _weight_sizes(w), _row_count(dy, "dy")
-    g = _grouped({"dy": (dy, [(r, o)], (dy.dtype,)), "w": (w, [tuple(w.shape)], (dy.dtype,)),
-                  "out": (out, [(r, i)], (dy.dtype,))}, n, r, o, i, dy.dtype, offsets)
-    _check(load().gsq_grouped_input_grad(ctypes.byref(g), _ptr(dy), _ptr(w), _ptr(offsets), _ptr(out),
-                                         _stream(stream)))
+    (n, o, i), r, dt, types = _weight_sizes(w), _row_count(dy, "dy"), _rows_dtype(dy), (dy.dtype,)
+    dev = _checked((("dy", dy, (r, o), types), ("w", w, w.shape, types), ("out", out, (r, i), types)), offsets, n)
+    _check(load().gsq_grouped_input_grad(ctypes.byref(CGrouped(n, o, i, dt, r)), dy.data_ptr(), w.data_ptr(),
+                                         _address(offsets), out.data_ptr(), _raw_stream(stream, dev)))
 
 
 def grouped_weight_grad(dy, x, out, offsets=None, accumulate=False, stream=None):
     """out_e = sum of dy[r]^T x[r] over the rows of group e, the gradient of grouped_forward's w, in the
     type of x or in float32; ``accumulate`` adds to a float32 out."""
     import torch
-    (n, o, i), r = _weight_sizes(out), _row_count(dy, "dy")
-    g = _grouped({"dy": (dy, [(r, o)], (dy.dtype,)), "x": (x, [(r, i)], (dy.dtype,)),
-                  "out": (out, [tuple(out.shape)], (dy.dtype, torch.float32))}, n, r, o, i, dy.dtype, offsets)
-    dt = DT_FP32 if out.dtype == torch.float32 else g.dtype
-    _check(load().gsq_grouped_weight_grad(ctypes.byref(g), _ptr(dy), _ptr(x), _ptr(offsets), _ptr(out), dt,
-                                          1 if accumulate else 0, _stream(stream)))
+    (n, o, i), r, dt, types = _weight_sizes(out, "out"), _row_count(dy, "dy"), _rows_dtype(dy), (dy.dtype,)
+    dev = _checked((("dy", dy, (r, o), types), ("x", x, (r, i), types),
+                    ("out", out, out.shape, types + (torch.float32,))), offsets, n)
+    _check(load().gsq_grouped_weight_grad(ctypes.byref(CGrouped(n, o, i, dt, r)), dy.data_ptr(), x.data_ptr(),
+                                          _address(offsets), out.data_ptr(),
+                                          DT_FP32 if out.dtype is torch.float32 else dt,
+                                          1 if accumulate else 0, _raw_stream(stream, dev)))
 
 
 def gram(x, out, offsets=None, accumulate=False, stream=None):
     """out_e = X_e^T X_e in float32 (groups x I x I or I x I), the H of ``Layer``; ``accumulate`` adds to it."""
     import torch
-    (n, i, i2), r = _weight_sizes(out), _row_count(x, "x")
+    (n, i, i2), r, dt = _weight_sizes(out, "out"), _row_count(x, "x"), _rows_dtype(x)
     if i != i2:
         raise ValueError(f"out must be square, got {tuple(out.shape)}")
-    g = _grouped({"x": (x, [(r, i)], (x.dtype,)), "out": (out, [tuple(out.shape)], (torch.float32,))},
-                 n, r, 0, i, x.dtype, offsets)
-    _check(load().gsq_gram(ctypes.byref(g), _ptr(x), _ptr(offsets), _ptr(out), 1 if accumulate else 0,
-                           _stream(stream)))
+    dev = _checked((("x", x, (r, i), (x.dtype,)), ("out", out, out.shape, (torch.float32,))), offsets, n)
+    _check(load().gsq_gram(ctypes.byref(CGrouped(n, 0, i, dt, r)), x.data_ptr(), _address(offsets),
+                           out.data_ptr(), 1 if accumulate else 0, _raw_stream(stream, dev)))
 
 
 def quantize_rows(x, q, scales, stream=None):
     """Rows of x (rows x cols; float32, bfloat16 or float16) as int8 ``q`` and a float32 scale each: tokens
     of activations, or output channels of weights (a groups x O x I tensor has groups * O rows)."""
     import torch
-    codes = {torch.float32: DT_FP32, torch.bfloat16: DT_BF16, torch.float16: DT_FP16}
-    if x.dim() < 2:
+    if len(x.shape) < 2:
         raise ValueError(f"x must be rows x columns, got {tuple(x.shape)}")
-    if tuple(q.shape) != tuple(x.shape) or tuple(scales.shape) != tuple(x.shape[:-1]):
-        raise ValueError(f"q must have the shape of x and scales that of its rows, got {tuple(q.shape)} and "
-                         f"{tuple(scales.shape)} for {tuple(x.shape)}")
-    for name, t, dtypes in (("x", x, tuple(codes)), ("q", q, (torch.int8,)),
-                            ("scales", scales, (torch.float32,))):
-        _on_current_device(t, name)
-        _arg(t, name, t.numel(), dtypes)
-    _check(load().gsq_quantize_rows(_ptr(x), codes[x.dtype], scales.numel(), x.shape[-1], _ptr(q),
-                                    _ptr(scales), _stream(stream)))
+    dt = DT_FP32 if x.dtype is torch.float32 else _rows_dtype(x)
+    dev = _checked((("x", x, x.shape, (x.dtype,)), ("q", q, x.shape, (torch.int8,)),
+                    ("scales", scales, x.shape[:-1], (torch.float32,))), None, 1)
+    _check(load().gsq_quantize_rows(x.data_ptr(), dt, scales.numel(), x.shape[-1], q.data_ptr(),
+                                    scales.data_ptr(), _raw_stream(stream, dev)))
 
 
 def grouped_forward_i8(x, x_scales, w, w_scales, out, offsets=None, stream=None):
     """out[r, n] = x_scales[r] w_scales[e, n] sum_k x[r, k] w[e, n, k] for int8 x and w."""
     import torch
-    (n, o, i), r = _weight_sizes(w), _row_count(x, "x")
-    g = _grouped({"x": (x, [(r, i)], (torch.int8,)), "x_scales": (x_scales, [(r,)], (torch.float32,)),
-                  "w": (w, [tuple(w.shape)], (torch.int8,)),
-                  "w_scales": (w_scales, [tuple(w.shape[:-1])], (torch.float32,)),
-                  "out": (out, [(r, o)], (out.dtype,))}, n, r, o, i, out.dtype, offsets)
-    _check(load().gsq_grouped_forward_i8(ctypes.byref(g), _ptr(x), _ptr(x_scales), _ptr(w), _ptr(w_scales),
-                                         _ptr(offsets), _ptr(out), _stream(stream)))
+    (n, o, i), r, dt = _weight_sizes(w), _row_count(x, "x"), _rows_dtype(out)
+    ints, floats = (torch.int8,), (torch.float32,)
+    dev = _checked((("x", x, (r, i), ints), ("x_scales", x_scales, (r,), floats), ("w", w, w.shape, ints),
+                    ("w_scales", w_scales, w.shape[:-1], floats), ("out", out, (r, o), (out.dtype,))), offsets, n)
+    _check(load().gsq_grouped_forward_i8(ctypes.byref(CGrouped(n, o, i, dt, r)), x.data_ptr(),
+                                         x_scales.data_ptr(), w.data_ptr(), w_scales.data_ptr(),
+                                         _address(offsets), out.data_ptr(), _raw_stream(stream, dev)))
 
 
 class Linear:
@@ -468,12 +483,10 @@ class Linear:
     def __init__(self, cfg, packed, stream=None):
         self._h = None
         self.cfg = cfg
-        if not (packed.is_cuda and packed.is_contiguous()):
-            raise ValueError("packed must be a contiguous device tensor")
-        _on_current_device(packed, "packed")
+        dev = _checked((("packed", packed, packed.shape, (packed.dtype,)),), None, 1)
         h = ctypes.c_void_p()
-        _check(load().gsq_linear_init(ctypes.byref(cfg.to_c()), _ptr(packed),
-                                      packed.numel() * packed.element_size(), _stream(stream),
+        _check(load().gsq_linear_init(ctypes.byref(cfg.to_c()), packed.data_ptr(),
+                                      packed.numel() * packed.element_size(), _raw_stream(stream, dev),
                                       ctypes.byref(h)))
         self._h = h
 
@@ -481,12 +494,11 @@ class Linear:
         """out = x W_e^T with the packed weights (x, out: bfloat16 or float16)."""
         if self._h is None:
             raise RuntimeError("layer destroyed")
-        c, r = self.cfg, _row_count(x, "x")
-        g = _grouped({"x": (x, [(r, c.in_features)], (x.dtype,)),
-                      "out": (out, [(r, c.out_features)], (x.dtype,))}, c.batch, r, c.out_features,
-                     c.in_features, x.dtype, offsets)
-        _check(load().gsq_linear_forward(self._h, _ptr(x), g.dtype, r, _ptr(offsets), _ptr(out),
-                                         _stream(stream)))
+        c, r, dt, types = self.cfg, _row_count(x, "x"), _rows_dtype(x), (x.dtype,)
+        dev = _checked((("x", x, (r, c.in_features), types), ("out", out, (r, c.out_features), types)),
+                       offsets, c.batch)
+        _check(load().gsq_linear_forward(self._h, x.data_ptr(), dt, r, _address(offsets), out.data_ptr(),
+                                         _raw_stream(stream, dev)))
 
     def destroy(self):
         if self._h is not None:

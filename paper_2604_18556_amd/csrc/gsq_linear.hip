@@ -417,10 +417,16 @@ namespace {
 template <class T, int BITS, bool kFine>
 hipError_t launch_packed(const PackedLayer& L, const GroupRows& rows, const void* x, void* y, hipStream_t s) {
   using E = typename T::elem;
-  const int height = pick_height(rows, L.O);
-  if (rows.rows > 64 * (int64_t)rows.groups && aligned16(x))
-    return launch_ring<k_packed_tile<T, BITS, kFine>>(most_panels(rows, height) * tiles_of(L.O, Whole::TN), s, L,
-                       rows, static_cast<const E*>(x), static_cast<E*>(y), height, (int)four_at_once(y, T::kDtype, L.O));
+  // as for dense weights; the tiles' slabs take longer to write than to copy
+  const TileCost large[] = {{256, 256, 1.45, 1.9}, {128, 256, 1.0, 1.15}, {64, 256, 0.8, 0.95}};
+  const TileCost small[] = {{64, 16, 0.2, 0.25}, {16, 16, 0.014, 0.03}};
+  double best = 1e30;
+  RowsPlan plan = cheapest(rows, L.O, 2 * L.blocks, small, true, 5.0, best, RowsPlan{});
+  if (aligned16(x)) plan = cheapest(rows, L.O, 2 * L.blocks, large, false, 7.0, best, plan);
+  if (!plan.split)
+    return launch_ring<k_packed_tile<T, BITS, kFine>>(most_panels(rows, plan.height) * tiles_of(L.O, Whole::TN), s, L,
+                                                      rows, static_cast<const E*>(x), static_cast<E*>(y), plan.height,
+                                                      (int)four_at_once(y, T::kDtype, L.O));
   const int waves = std::max(1, std::min(kMostWaves, L.blocks));
   const dim3 grid(L.tiles, rows.groups);
   k_packed_few<T, BITS, kFine><<<grid, 64 * waves, waves * 4 * 64 * sizeof(f32x4), s>>>(

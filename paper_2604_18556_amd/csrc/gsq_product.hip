@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "gsq_split.hpp"
 
@@ -216,49 +217,92 @@ __global__ __launch_bounds__(64 * kSplitWaves) void k_sums_split(ProductArgs p) 
 
 // Rows in 8-bit integers: s = max |x| / 127 in fp32, q = x / s to the nearest integer, ties to even.  A
 // row of zeros has s = 0 and q = 0; a row with an infinity or NaN s = NaN and q = 0, so that its products
-// are NaN.
+// are NaN.  A row is read once: up to kHeld chunks of 16 values stay with each thread, what is longer is read
+// again.  Chunks begin at multiples of 16 values; from any address, by unaligned loads and stores.
+constexpr int kHeld = 2, kChunk = 16;
+
+template <class E>
+struct QuantChunk {
+  E v[kChunk];
+  __device__ __forceinline__ void load(const E* x, int64_t c, int64_t cols) {
+    if (c + kChunk <= cols) {
+      __builtin_memcpy(v, x + c, sizeof(v));
+    } else {
+#pragma unroll
+      for (int i = 0; i < kChunk; ++i) v[i] = c + i < cols ? x[c + i] : (E)0;
+    }
+  }
+  // The largest magnitude as its bits, which order like the values; infinities and NaN lie above all others.
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t t = 0;
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) t = max(t, __float_as_uint((float)v[i]) & 0x7fffffffu);
+    return t;
+  }
+  // x, s and 1 / s, with x and s scaled by `by`.
+  __device__ __forceinline__ void write(int8_t* q, int64_t c, int64_t cols, float s, float inv, float by) const {
+    int8_t out[kChunk];
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) {
+      const float x = inv == 0.f ? 0.f : (float)v[i] * by;
+      // x times a reciprocal may round onto a half, off it, or past it: the remainder, exact in an fma, decides
+      float r = rintf(x * inv);
+      const float rest = fmaf(-r, s, x), twice = 2.f * fabsf(rest);
+      if (twice > s || (twice == s && ((int)r & 1))) r += copysignf(1.f, rest);
+      out[i] = (int8_t)(int)fminf(fmaxf(r, -127.f), 127.f);
+    }
+    if (c + kChunk <= cols) {
+      __builtin_memcpy(q + c, out, sizeof(out));
+    } else {
+#pragma unroll
+      for (int i = 0; i < kChunk; ++i)
+        if (c + i < cols) q[c + i] = out[i];
+    }
+  }
+};
+
 template <class E>
 __global__ __launch_bounds__(256) void k_quantize_rows(const E* __restrict__ x, int64_t cols,
                                                        int8_t* __restrict__ q, float* __restrict__ scales) {
-  __shared__ float part[4];
-  __shared__ int bad_part[4];
+  __shared__ uint32_t part[4];
   const int64_t row = blockIdx.x;
   x += row * cols;
   q += row * cols;
-  float top = 0.f;
-  bool bad = false;
-  for (int64_t c = threadIdx.x; c < cols; c += 256) {
-    const float v = fabsf((float)x[c]);
-    bad |= !(v <= __FLT_MAX__);
-    top = fmaxf(top, v);
+  const int64_t c0 = (int64_t)threadIdx.x * kChunk, step = (int64_t)blockDim.x * kChunk;
+  QuantChunk<E> held[kHeld];
+  uint32_t top = 0;
+#pragma unroll
+  for (int h = 0; h < kHeld; ++h) {
+    held[h].load(x, min(c0 + h * step, cols), cols);
+    top = max(top, held[h].top());
+  }
+  for (int64_t c = c0 + kHeld * step; c < cols; c += step) {
+    QuantChunk<E> more;
+    more.load(x, c, cols);
+    top = max(top, more.top());
   }
 #pragma unroll
-  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-  const bool wave_bad = __any(bad);
-  if ((threadIdx.x & 63) == 0) {
-    part[threadIdx.x >> 6] = top;
-    bad_part[threadIdx.x >> 6] = wave_bad;
+  for (int d = 32; d; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+  if (blockDim.x > 64) {
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
+    __syncthreads();
+    for (unsigned w = 0; w < blockDim.x >> 6; ++w) top = max(top, part[w]);
   }
-  __syncthreads();
-  top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-  bad = bad_part[0] | bad_part[1] | bad_part[2] | bad_part[3];
-  const float s = bad ? __builtin_nanf("") : top / 127.f;
+  const float s = top >= 0x7f800000u ? __builtin_nanf("") : __uint_as_float(top) / 127.f;
   if (threadIdx.x == 0) scales[row] = s;
-  for (int64_t c = threadIdx.x; c < cols; c += 256) {
-    const float v = (float)x[c];
-    float r = 0.f;
-    if (s > 0.f) {
-      // the division may round onto a half, or off it: the remainder, exact in an fma, decides
-      r = rintf(v / s);
-      const float rest = fmaf(-r, s, v), twice = 2.f * fabsf(rest);
-      if (twice > s || (twice == s && ((int)r & 1))) r += copysignf(1.f, rest);
-      r = fminf(fmaxf(r, -127.f), 127.f);
-    }
-    q[c] = (int8_t)r;
+  const bool some = s > 0.f;   // else every q is zero: nothing is divided by zero or NaN
+  // the reciprocal of a very small scale would overflow: row and scale are taken 2^24 times as large
+  const float tiny = s < 1e-37f ? 0x1p24f : 1.f;
+  const float sc = some ? s * tiny : 1.f, inv = some ? 1.f / sc : 0.f;
+#pragma unroll
+  for (int h = 0; h < kHeld; ++h)
+    if (c0 + h * step < cols) held[h].write(q, c0 + h * step, cols, sc, inv, tiny);
+  for (int64_t c = c0 + kHeld * step; c < cols; c += step) {
+    QuantChunk<E> more;
+    more.load(x, c, cols);
+    more.write(q, c, cols, sc, inv, tiny);
   }
 }
-
-int path() { static const char* h = getenv("GSQ_PATH"); return h ? atoi(h) : 0; }
 
 template <class T, int kForm, int TM, int TN, bool kLoose>
 hipError_t launch_rows_split(const ProductArgs& p, hipStream_t s) {
@@ -270,26 +314,42 @@ hipError_t launch_rows_split(const ProductArgs& p, hipStream_t s) {
 }
 
 template <class T, int kForm, bool kLoose>
-hipError_t launch_rows_split(const ProductArgs& p, hipStream_t s) {
-  const int ns = kForm == kForward ? p.O : p.I;
-  const int64_t groups = std::min<int64_t>(p.rows.rows, p.rows.groups);
-  const bool few = p.rows.rows <= 16 * groups, wide = most_panels(p.rows, few ? 16 : 64) * tiles_of(ns, 64) >= 256;
-  if (few) return wide ? launch_rows_split<T, kForm, 16, 64, kLoose>(p, s) : launch_rows_split<T, kForm, 16, 16, kLoose>(p, s);
-  return wide ? launch_rows_split<T, kForm, 64, 64, kLoose>(p, s) : launch_rows_split<T, kForm, 64, 16, kLoose>(p, s);
+hipError_t launch_rows_split(const ProductArgs& p, const RowsPlan& plan, hipStream_t s) {
+  if (plan.height == 16)
+    return plan.width == 64 ? launch_rows_split<T, kForm, 16, 64, kLoose>(p, s)
+                            : launch_rows_split<T, kForm, 16, 16, kLoose>(p, s);
+  return plan.width == 64 ? launch_rows_split<T, kForm, 64, 64, kLoose>(p, s)
+                          : launch_rows_split<T, kForm, 64, 16, kLoose>(p, s);
 }
 
+// Which tiles: whole workgroups on panels of 256, 128 or 64 rows, or wavefronts that share a sum.  The costs
+// are fitted to bf16 products of one group (us for x W^T; 256 | 128 | 64 rows by workgroups, 64 x 64 | 64 x 16
+// split):
+//   8192 x 8192: 64 rows - | - | 101, 44 | 51; 256 rows 154 | 111 | 100, 71 | 141; 512 rows 158 | 112 | 101,
+//     125 | 246; 1024 rows 162 | 123 | 205, 225 | -; 2048 rows 208 | 242 | 371, 432 | -
+//   2048 x 2048: 64 rows - | - | 18.1, 9.6 | 6.7; 512 rows 47 | 30 | 19, 11 | 19; 2048 rows 49 | 31 | 24, 38 | -
+//   O 512, I 8192: 512 rows 147 | 90 | 57, 25 | 18; 4096 rows 150 | 92 | 60, 54 | -
+// and 8192 x 8192 at one row by 16 x 64 | 16 x 16 split 30 | 28, at 64 rows 50 | 68.  8-bit integers take
+// longer in large tiles, which the power of the matrix cores bounds.
 template <class T, int kForm>
 hipError_t launch_rows(ProductArgs p, hipStream_t s) {
   if (p.rows.rows == 0) return hipSuccess;
-  const int ns = kForm == kForward ? p.O : p.I;
+  const int ns = kForm == kForward ? p.O : p.I, ks = kForm == kForward ? p.I : p.O;
   const int64_t unit = 16 / (int64_t)sizeof(typename T::elem);
+  const int slabs = tiles_of(ks, ROW_BYTES / (int)sizeof(typename T::elem));
   p.vector_out = four_at_once(p.out, p.out_dtype, ns);
   const bool tight = p.O % (kForm == kForward ? 1 : unit) == 0 && p.I % unit == 0 && aligned16(p.a) && aligned16(p.b);
-  if (!tight) return launch_rows_split<T, kForm, true>(p, s);
-  p.height = pick_height(p.rows, ns);
-  const int64_t tiles = most_panels(p.rows, p.height) * tiles_of(ns, Whole::TN);
-  if (path() == 2 || (path() == 0 && tiles < 128)) return launch_rows_split<T, kForm, false>(p, s);
-  return launch_ring<k_rows_tile<T, kForm>>(tiles, s, p);
+  constexpr double kMore = T::kDtype < 0 ? 1.4 : 1;
+  const TileCost large[] = {{256, 256, 1.15 * kMore, 1.6 * kMore}, {128, 256, 0.7 * kMore, 0.95 * kMore},
+                            {64, 256, 0.43 * kMore, 0.72 * kMore}};
+  const TileCost small[] = {{64, 64, 0.165, 0.22}, {64, 16, 0.1, 0.115}, {16, 64, 0.06, 0.1}, {16, 16, 0.02, 0.055}};
+  double best = 1e30;
+  RowsPlan plan = cheapest(p.rows, ns, slabs, small, true, 5.0, best, RowsPlan{});
+  if (tight) plan = cheapest(p.rows, ns, slabs, large, false, 7.0, best, plan);
+  if (!tight) return launch_rows_split<T, kForm, true>(p, plan, s);
+  if (plan.split) return launch_rows_split<T, kForm, false>(p, plan, s);
+  p.height = plan.height;
+  return launch_ring<k_rows_tile<T, kForm>>(most_panels(p.rows, p.height) * tiles_of(ns, Whole::TN), s, p);
 }
 
 template <class T, bool kGram>
@@ -300,8 +360,15 @@ hipError_t launch_sums(ProductArgs p, hipStream_t s) {
     return p.rows.groups * (kGram ? (tn + 1) / 2 * (tn + 1) : tm * tn);
   };
   const bool tight = p.O % 8 == 0 && p.I % 8 == 0 && aligned16(p.a) && aligned16(p.b);
-  if (tight && (path() == 1 || (path() == 0 && count(Whole::TM) >= 128 && p.rows.rows >= 128 * (int64_t)p.rows.groups)))
-    return launch_ring<k_sums_tile<T, kGram>>(count(Whole::TM), s, p);
+  // Whole workgroups on 256 x 256 tiles or wavefronts that share the sum of 64 x 64 ones, by the same reckoning
+  // (us, 256 | 64): 512 x 512 from 1024 rows 34 | 7, 16384 rows 317 | 62; 2048 x 2048 from 1024 rows 41 | 24,
+  // 16384 rows 326 | 300; 4096 x 4096 from 256 rows 28 | 38, 4096 rows 122 | 250
+  const double slabs = (double)p.rows.rows / 64 / p.rows.groups;
+  const auto rounds = [&](int64_t tile) { return std::max(1.0, std::ceil(count(tile) / 256.0)); };
+  const double load = std::min(1.0, count(Whole::TM) / 256.0);
+  const double us_large = 15 + slabs * (1.2 + 0.5 * load) * rounds(Whole::TM);
+  const double us_small = 5 + (slabs + 1) * 0.3 * rounds(kSumTile);
+  if (tight && us_large < us_small) return launch_ring<k_sums_tile<T, kGram>>(count(Whole::TM), s, p);
   const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(kSplitWaves, (p.rows.rows + 63) / 64));
   const size_t lds = waves * 2 * kSumTile * ROW_BYTES;
   return tight ? launch_lds<k_sums_split<T, kGram, false>>(count(kSumTile), 64 * waves, lds, s, p)
@@ -326,12 +393,13 @@ hipError_t launch_gram(int dtype, const ProductArgs& p, hipStream_t s) {
 hipError_t launch_quantize_rows(const void* x, int dtype, int64_t rows, int64_t cols, int8_t* q,
                                 float* scales, hipStream_t s) {
   if (rows == 0) return hipSuccess;
+  const int threads = (int)std::min<int64_t>(256, (cols + 64 * kChunk - 1) / (64 * kChunk) * 64);
   if (dtype == GSQ_DT_BF16)
-    k_quantize_rows<<<rows, 256, 0, s>>>(static_cast<const __bf16*>(x), cols, q, scales);
+    k_quantize_rows<<<rows, threads, 0, s>>>(static_cast<const __bf16*>(x), cols, q, scales);
   else if (dtype == GSQ_DT_FP16)
-    k_quantize_rows<<<rows, 256, 0, s>>>(static_cast<const _Float16*>(x), cols, q, scales);
+    k_quantize_rows<<<rows, threads, 0, s>>>(static_cast<const _Float16*>(x), cols, q, scales);
   else
-    k_quantize_rows<<<rows, 256, 0, s>>>(static_cast<const float*>(x), cols, q, scales);
+    k_quantize_rows<<<rows, threads, 0, s>>>(static_cast<const float*>(x), cols, q, scales);
   return hipGetLastError();
 }
 

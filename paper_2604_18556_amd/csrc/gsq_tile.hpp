@@ -353,11 +353,6 @@ __device__ __forceinline__ bool find_rows_tile(const GroupRows& rows, int height
   return true;
 }
 
-inline int pick_height(const GroupRows& rows, int cols) {
-  static const char* h = getenv("GSQ_H");
-  return h ? atoi(h) : 256;
-}
-
 // A kernel that uses more LDS than the default limit needs leave for it, once on each device.
 template <auto kKernel, class... Args>
 hipError_t launch_lds(int64_t blocks, int threads, size_t lds, hipStream_t s, const Args&... args) {
@@ -384,6 +379,39 @@ hipError_t launch_ring(int64_t blocks, hipStream_t s, const Args&... args) {
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 int tiles_of(int n, int tile) { return (n + tile - 1) / tile; }
+
+// How a product of rows is cut: panels of `height` rows and `width` columns, by whole workgroups (ring) or by
+// wavefronts that share the sum (split).
+struct RowsPlan {
+  bool split;
+  int height, width;
+};
+
+// Microseconds of each slab (128 bytes of k) of a tile: on an empty GPU, and with a tile on each of 256 CUs.
+struct TileCost {
+  int height, width;
+  double alone, full;
+};
+
+// The cheapest of several tiles.  A product takes a start, and its slabs times the rounds of 256 tiles that it
+// fills; the groups' last panels are taken to be half full.
+template <int N>
+RowsPlan cheapest(const GroupRows& r, int cols, int slabs, const TileCost (&costs)[N], bool split, double start,
+                  double& best, RowsPlan plan) {
+  const double few = (double)(r.rows < r.groups ? r.rows : r.groups);
+  for (const TileCost& c : costs) {
+    const double panels = r.groups == 1 ? (double)((r.rows + c.height - 1) / c.height) : r.rows / (double)c.height + few / 2;
+    const double tiles = panels * tiles_of(cols, c.width), rounds = tiles / 256;
+    const double whole = rounds < 1 ? 1 : r.groups == 1 ? (double)(int64_t)(rounds + 0.999) : rounds;
+    const double each = c.alone + (c.full - c.alone) * (rounds < 1 ? rounds : 1);
+    const double us = start + slabs * each * whole;
+    if (us < best) {
+      best = us;
+      plan = {split, c.height, c.width};
+    }
+  }
+  return plan;
+}
 
 // Results can be stored four at a time: whole rows of them, at aligned addresses.
 bool four_at_once(const void* out, int32_t dtype, int32_t cols) {
