@@ -4,7 +4,7 @@
 
 #include <algorithm>
 
-#include "gsq_tile.hpp"
+#include "gsq_split.hpp"
 
 namespace gsq {
 namespace {
@@ -182,6 +182,13 @@ struct WeightTable {
     d0 = __builtin_amdgcn_perm(h, l, 0x05010400);
     d1 = __builtin_amdgcn_perm(h, l, 0x07030602);
   }
+  // Weights 8 s .. 8 s + 7.
+  __device__ __forceinline__ typename T::frag frag(const uint32_t* words, int s) const {
+    union { uint32_t d[4]; typename T::frag f; } w;
+    pick(words, 2 * s, w.d[0], w.d[1]);
+    pick(words, 2 * s + 1, w.d[2], w.d[3]);
+    return w.f;
+  }
 };
 
 // What one lane holds of a unit: its 32 codes, and the scales of their first and second half.
@@ -223,97 +230,156 @@ struct LaneCodes {
   }
 };
 
-// ---- few rows: each workgroup has 16 output channels, its wavefronts share the inputs between them, and the
-// partial sums are added in LDS in a fixed order.
-constexpr int kMostWaves = 16;
+// ---- up to 16 rows: a workgroup has 16 output channels, its wavefronts take their units in turn, and the
+// partial sums are added in LDS in a fixed order.  Bound by the codes' way from memory: all that a wavefront
+// needs for kFewUnits units, x included, is asked for before the units before them are multiplied.
+constexpr int kFewWaves = 16, kFewUnits = 2;
 
-// 16 MI rows: y[r, n] for the 16 channels of `tile`.
-template <class T, int BITS, bool kFine, int MI>
-__device__ __forceinline__ void few_rows(const PackedLayer& L, const typename T::elem* x, typename T::elem* y,
-                                         int64_t first, int ms, int64_t tile, int n0, f32x4* part) {
+template <class T, int BITS, bool kFine>
+struct FewOperands {
+  LaneCodes<BITS, kFine> codes[kFewUnits];
+  typename T::frag x[kFewUnits][4];
+
+  __device__ __forceinline__ void load(const PackedLayer& L, int64_t tile, const typename T::elem* row, bool some,
+                                       int kb0, int step) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int u = 0; u < kFewUnits; ++u)   // past the end: the last unit again, not used
+      codes[u].load(L, tile, min(kb0 + u * step, L.blocks - 1), lane);
+#pragma unroll
+    for (int u = 0; u < kFewUnits; ++u) {
+      const int k0 = (kb0 + u * step) * 128 + (lane >> 4) * 32;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        x[u][s] = typename T::frag{};
+        if (some && k0 + 8 * s < L.I) __builtin_memcpy(&x[u][s], row + k0 + 8 * s, 16);
+      }
+    }
+  }
+};
+
+template <class T, int BITS, bool kFine>
+__global__ __launch_bounds__(64 * kFewWaves) void k_packed_few(PackedLayer L, GroupRows rows,
+                                                              const typename T::elem* __restrict__ x,
+                                                              typename T::elem* __restrict__ y) {
   using E = typename T::elem;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int g = lane >> 4;
-  f32x4 acc[MI] = {};
-  constexpr int U = MI <= 2 ? 2 : 1;      // units in flight
-  LaneCodes<BITS, kFine> now[U], next[U];
+  __shared__ f32x4 part[kFewWaves * 64];
+  PanelPlace at;
+  if (!find_panel(rows, 16, blockIdx.x / (unsigned)L.tiles, at)) return;
+  // panels of a group share its codes: they are neighbours
+  const int j = (int)(blockIdx.x - at.before * L.tiles), n0 = j / at.panels * 16;
+  const int64_t first = at.first + (int64_t)(j % at.panels) * 16, tile = (int64_t)at.group * L.tiles + n0 / 16;
+  const int ms = (int)min(at.end - first, (int64_t)16);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, g = lane >> 4;
+  const bool some = (lane & 15) < ms;
+  const E* row = x + (first + (some ? lane & 15 : 0)) * L.I;
+  f32x4 acc = {};
+  FewOperands<T, BITS, kFine> now, next;
+  next.load(L, tile, row, some, wave, waves);
+  for (int kb0 = wave; kb0 < L.blocks; kb0 += kFewUnits * waves) {
+    now = next;
+    next.load(L, tile, row, some, kb0 + kFewUnits * waves, waves);
 #pragma unroll
-  for (int u = 0; u < U; ++u)
-    next[u].load(L, tile, min(wave + u * waves, L.blocks - 1), lane);
-  for (int kb0 = wave; kb0 < L.blocks; kb0 += U * waves) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) now[u] = next[u];
-#pragma unroll
-    for (int u = 0; u < U; ++u)   // past the end: the last unit again, not used
-      next[u].load(L, tile, min(kb0 + (U + u) * waves, L.blocks - 1), lane);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int kb = kb0 + u * waves;
-      if (kb >= L.blocks) break;
-      const int k0 = kb * 128 + g * 32;
-      typename T::frag a[MI][4] = {};
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-        if (i * 16 + (lane & 15) < ms) {
-          const E* row = x + (first + i * 16 + (lane & 15)) * L.I + k0;
-#pragma unroll
-          for (int s = 0; s < 4; ++s)
-            if (k0 + 8 * s < L.I) __builtin_memcpy(&a[i][s], row + 8 * s, 16);
-        }
+    for (int u = 0; u < kFewUnits; ++u) {
+      if (kb0 + u * waves >= L.blocks) break;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const WeightTable<T, BITS> table(now[u].scale(L, kFine ? h : 0), L.levels);
+        const WeightTable<T, BITS> table(now.codes[u].scale(L, kFine ? h : 0), L.levels);
 #pragma unroll
-        for (int s = 2 * h; s < 2 * h + 2; ++s) {
-          union { uint32_t d[4]; typename T::frag f; } w;
-          table.pick(now[u].words, 2 * s, w.d[0], w.d[1]);
-          table.pick(now[u].words, 2 * s + 1, w.d[2], w.d[3]);
-#pragma unroll
-          for (int i = 0; i < MI; ++i) acc[i] = T::mfma(w.f, a[i][s], acc[i]);
-        }
+        for (int s = 2 * h; s < 2 * h + 2; ++s) acc = T::mfma(table.frag(now.codes[u].words, s), now.x[u][s], acc);
       }
     }
   }
   // acc: row of x lane % 16, channels 4 (lane / 16) .. + 3
-  if (waves > 1) {
+  part[threadIdx.x] = acc;
+  __syncthreads();
+  if (wave) return;
+  for (int w = 1; w < waves; ++w) acc += part[w * 64 + lane];
+  if (some)
 #pragma unroll
-    for (int i = 0; i < MI; ++i) part[(wave * MI + i) * 64 + lane] = acc[i];
-    __syncthreads();
+    for (int c = 0; c < 4; ++c)
+      if (n0 + 4 * g + c < L.O) y[(first + (lane & 15)) * L.O + n0 + 4 * g + c] = (E)acc[c];
+}
+
+// ---- more rows, but too few tiles for whole workgroups: 64 channels and TM rows, the units shared by eight
+// wavefronts as tile_split() does it.  x goes through LDS, the weights from the codes to registers.
+constexpr int kSharedCols = 64;
+
+template <class T, int BITS, bool kFine, int TM>
+__device__ __forceinline__ void packed_shared(const PackedLayer& L, const typename T::elem* x, typename T::elem* y,
+                                              int group, int64_t first, int ms, int n0, int vector_out, uint8_t* smem) {
+  constexpr int MI = TM / 16, NJ = kSharedCols / 16, A_SLAB = TM * ROW_BYTES, OWN = 2 * A_SLAB;
+  constexpr int FOURS = kSharedCols / 4;
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint8_t* const own = smem + wave * OWN;
+  Copied<SlabAlong<TM, TM / 8>> a(x + first * L.I, (int64_t)L.I * 2, ms, 0, lane);
+  const int64_t tile0 = (int64_t)group * L.tiles;
+  int64_t tile[NJ];
+  LaneCodes<BITS, kFine> next[NJ];
+  f32x4 acc[MI][NJ] = {};
+  const auto fetch = [&](int kb) {
+    a.fetch(2 * kb, own);
+    a.fetch(2 * kb + 1, own + A_SLAB);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) next[j].load(L, tile[j], kb, lane);
+  };
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) tile[j] = tile0 + min(n0 / 16 + j, L.tiles - 1);   // beyond: not stored
+  if (wave < L.blocks) fetch(wave);
+  for (int kb = wave; kb < L.blocks; kb += waves) {
+    wait_all();
+    typename T::frag fa[MI][4];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int s = 0; s < 4; ++s)   // inputs 32 g + 8 s of the unit
+        fa[i][s] = read_frag<typename T::frag>(own + (g >> 1) * A_SLAB, i * 16 + (lane & 15), 4 * (g & 1) + s);
+    LaneCodes<BITS, kFine> now[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) now[j] = next[j];
+    wait_reads();
+    if (kb + waves < L.blocks) fetch(kb + waves);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const WeightTable<T, BITS> table(now[j].scale(L, kFine ? h : 0), L.levels);
+#pragma unroll
+        for (int s = 2 * h; s < 2 * h + 2; ++s) {
+          const typename T::frag w = table.frag(now[j].words, s);
+#pragma unroll
+          for (int i = 0; i < MI; ++i) acc[i][j] = T::mfma(w, fa[i][s], acc[i][j]);
+        }
+      }
   }
-  for (int i = wave; i < MI; i += waves) {
-    f32x4 v = waves > 1 ? part[i * 64 + lane] : acc[0];
-    for (int w = 1; w < waves; ++w) v += part[(w * MI + i) * 64 + lane];
-    if (waves == 1)
-#pragma unroll
-      for (int k = 1; k < MI; ++k)
-        if (k == i) v = acc[k];
-    const int m = i * 16 + (lane & 15);
-    if (m < ms)
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (n0 + 4 * g + c < L.O) y[(first + m) * L.O + n0 + 4 * g + c] = (E)v[c];
+  split_sums<TM, kSharedCols>(acc, own);
+  __syncthreads();
+  const int parts = min(waves, L.blocks);
+  for (int f = threadIdx.x; f < TM * FOURS; f += blockDim.x) {
+    const int m = f / FOURS, c = f % FOURS;
+    const f32x4 v = added_sums<kSharedCols, f32x4>(smem, OWN, parts, m, c);
+    if (m < ms && n0 + 4 * c < L.O)
+      store_four(y, T::kDtype, (first + m) * L.O + n0 + 4 * c, v, L.O - n0 - 4 * c, vector_out);
   }
-  __syncthreads();   // `part` is free again
 }
 
 template <class T, int BITS, bool kFine>
-__global__ __launch_bounds__(64 * kMostWaves) void k_packed_few(PackedLayer L, GroupRows rows,
-                                                               const typename T::elem* __restrict__ x,
-                                                               typename T::elem* __restrict__ y) {
-  extern __shared__ __attribute__((aligned(16))) f32x4 part[];
-  int64_t first, end;
-  group_rows(rows, blockIdx.y, first, end);
-  const int64_t tile = (int64_t)blockIdx.y * L.tiles + blockIdx.x;
-  const int n0 = blockIdx.x * 16;
-  for (; first < end; first += 64) {
-    const int ms = (int)min(end - first, (int64_t)64);
-    if (ms <= 16)
-      few_rows<T, BITS, kFine, 1>(L, x, y, first, ms, tile, n0, part);
-    else if (ms <= 32)
-      few_rows<T, BITS, kFine, 2>(L, x, y, first, ms, tile, n0, part);
-    else
-      few_rows<T, BITS, kFine, 4>(L, x, y, first, ms, tile, n0, part);
-  }
+__global__ __launch_bounds__(64 * kSplitWaves) void k_packed_shared(PackedLayer L, GroupRows rows,
+                                                                   const typename T::elem* __restrict__ x,
+                                                                   typename T::elem* __restrict__ y, int vector_out) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  const int tiles_n = (L.O + kSharedCols - 1) / kSharedCols;
+  PanelPlace at;
+  if (!find_panel(rows, 64, blockIdx.x / (unsigned)tiles_n, at)) return;
+  int tm, tn;
+  tile_at(lin_of((int)(blockIdx.x - at.before * tiles_n), at.panels * tiles_n), at.panels, tiles_n, tm, tn);
+  const int64_t first = at.first + (int64_t)tm * 64;
+  const int ms = (int)min(at.end - first, (int64_t)64);
+  if (ms <= 32)
+    packed_shared<T, BITS, kFine, 32>(L, x, y, at.group, first, ms, tn * kSharedCols, vector_out, smem);
+  else
+    packed_shared<T, BITS, kFine, 64>(L, x, y, at.group, first, ms, tn * kSharedCols, vector_out, smem);
 }
 
 // ---- many rows: tiles as for a dense layer, whose slabs of weights the wavefronts write to LDS from the
@@ -350,12 +416,7 @@ struct SlabPacked {
       for (int u = 0; u < UNITS; ++u) codes[u].arrived();
     if (s == 0 || (kFine && s == 2))   // slabs past the last unit are zeros
       table = WeightTable<T, BITS>(!kEnd || k >> 1 < L.blocks ? codes[i].scale(L, s / 2) : 0.f, L.levels);
-    i32x4 w;
-    uint32_t d[4];
-    table.pick(codes[i].words, 2 * s, d[0], d[1]);
-    table.pick(codes[i].words, 2 * s + 1, d[2], d[3]);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) w[c] = (int)d[c];
+    const i32x4 w = __builtin_bit_cast(i32x4, table.frag(codes[i].words, s));
     const int row = (2 * i + (lane >> 5)) * 16 + (lane & 15), chunk = 4 * ((lane >> 4) & 1) + s;
     *reinterpret_cast<i32x4*>(lds + row * ROW_BYTES + ((chunk ^ swz(row)) << 4)) = w;
     if (j == LOADS - 1) prefetch(k + 1);
@@ -373,10 +434,11 @@ __device__ __forceinline__ void packed_tile(const PackedLayer& L, const typename
   SlabPacked<T, BITS, kFine, S::TN> b(L, at.group, at.n0, wave, lane);
   typename T::acc acc[S::MI][S::NJ];
   tile_ring<T, S>(a, b, (L.I + 63) / 64, acc, smem);
-  tile_results<S>(acc, [&](int m, int n, f32x4 v) {
+  const auto store = [&](int m, int n, f32x4 v) {
     if (m < at.ms && at.n0 + n < L.O)
       store_four(y, T::kDtype, (at.first + m) * L.O + at.n0 + n, v, L.O - at.n0 - n, vector_out);
-  });
+  };
+  tile_results<S>(acc, smem, false, store, store);
 }
 
 template <class T, int BITS, bool kFine>
@@ -417,21 +479,37 @@ namespace {
 template <class T, int BITS, bool kFine>
 hipError_t launch_packed(const PackedLayer& L, const GroupRows& rows, const void* x, void* y, hipStream_t s) {
   using E = typename T::elem;
-  // as for dense weights; the tiles' slabs take longer to write than to copy
-  const TileCost large[] = {{256, 256, 1.45, 1.9}, {128, 256, 1.0, 1.15}, {64, 256, 0.8, 0.95}};
-  const TileCost small[] = {{64, 16, 0.2, 0.25}, {16, 16, 0.014, 0.03}};
+  // Which kernel, by the same reckoning as for dense weights (us at 2 bits; 16 rows and channels | 64 x 64 shared |
+  // panels of 64 | 128 | 256 rows by workgroups):
+  //   I 4096, O 4096: 1 row 6.9 | 10.3 | 52 | - | -; 17 rows 17 | 11; 256 rows - | 17 | 55 | 72 | 96; 2048 rows
+  //     - | 116 | 135 | 86 | 107; 4096 rows - | 219 | 247 | 152 | 113
+  //   I 4096, O 14336: 1 row 23 | 10; 64 rows 103 | 15 | 54; 512 rows - | 98 | 129 | 80 | 102; 1024 rows - | 188 |
+  //     246 | 150 | 107
+  //   I 14336, O 4096: 1 row 13 | 25; 16 rows 20 | 25; 64 rows 76 | 35
+  // 3 bits take 4 to 8 % longer, 4 bits 15 to 40 %.
+  const bool low = rows.rows <= 32 * std::min<int64_t>(rows.rows, rows.groups);
+  const TileCost large[] = {{256, 256, 3, 1.4, 1.65}, {128, 256, 2, 1.0, 1.15}, {64, 256, 1.5, 0.72, 0.95}};
+  const TileCost shared[] = {{64, 64, 1, low ? 0.095 : 0.15, low ? 0.12 : 0.2}};
+  const TileCost few[] = {{16, 16, 2.5, 0.03, 0.05}};
+  const int vector_out = four_at_once(y, T::kDtype, L.O), slabs = 2 * L.blocks;
+  const E* xe = static_cast<const E*>(x);
+  E* ye = static_cast<E*>(y);
   double best = 1e30;
-  RowsPlan plan = cheapest(rows, L.O, 2 * L.blocks, small, true, 5.0, best, RowsPlan{});
-  if (aligned16(x)) plan = cheapest(rows, L.O, 2 * L.blocks, large, false, 7.0, best, plan);
+  RowsPlan plan = cheapest(rows, L.O, slabs, few, true, best, RowsPlan{});
+  if (aligned16(x)) {
+    plan = cheapest(rows, L.O, slabs, shared, true, best, plan);
+    plan = cheapest(rows, L.O, slabs, large, false, best, plan);
+  }
   if (!plan.split)
     return launch_ring<k_packed_tile<T, BITS, kFine>>(most_panels(rows, plan.height) * tiles_of(L.O, Whole::TN), s, L,
-                                                      rows, static_cast<const E*>(x), static_cast<E*>(y), plan.height,
-                                                      (int)four_at_once(y, T::kDtype, L.O));
-  const int waves = std::max(1, std::min(kMostWaves, L.blocks));
-  const dim3 grid(L.tiles, rows.groups);
-  k_packed_few<T, BITS, kFine><<<grid, 64 * waves, waves * 4 * 64 * sizeof(f32x4), s>>>(
-      L, rows, static_cast<const E*>(x), static_cast<E*>(y));
-  return hipGetLastError();
+                                                      rows, xe, ye, plan.height, vector_out);
+  if (plan.height == 64) {
+    const int waves = std::min(kSplitWaves, L.blocks);
+    return launch_lds<k_packed_shared<T, BITS, kFine>>(most_panels(rows, 64) * tiles_of(L.O, kSharedCols), 64 * waves,
+                                                       (size_t)waves * 2 * 64 * ROW_BYTES, s, L, rows, xe, ye, vector_out);
+  }
+  return launch_lds<k_packed_few<T, BITS, kFine>>(most_panels(rows, 16) * L.tiles, 64 * std::min(kFewWaves, L.blocks),
+                                                  0, s, L, rows, xe, ye);
 }
 
 template <class T, int BITS>

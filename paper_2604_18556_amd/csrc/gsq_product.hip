@@ -46,7 +46,8 @@ __device__ __forceinline__ void rows_tile(const ProductArgs& p, const RowsTile& 
     SlabAcross<S::TN> b(w + n0, (int64_t)ns * sizeof(E), ns - n0, ks, wave, lane);
     tile_ring<T, S>(a, b, nk, acc, smem);
   }
-  tile_results<S>(acc, [&](int m, int n, auto v) { store_rows<T>(p, at.group, first, ms, ns, m, n0 + n, v); });
+  const auto store = [&](int m, int n, typename T::acc v) { store_rows<T>(p, at.group, first, ms, ns, m, n0 + n, v); };
+  tile_results<S>(acc, smem, false, store, store);
 }
 
 // y or dx.
@@ -111,8 +112,6 @@ __global__ __launch_bounds__(64 * kSplitWaves) void k_rows_split(ProductArgs p) 
     rows_split<T, kForm, TM, TN, kLoose>(p, at.group, first, ms, tn * TN, smem);
 }
 
-constexpr int kSumTile = 64;   // of the small tiles
-
 // Four consecutive columns of row m of a group's sum, those in bounds.
 __device__ __forceinline__ void store_sums(const ProductArgs& p, int e, int m, int n, f32x4 v) {
   if (m >= p.O || n >= p.I) return;
@@ -140,25 +139,14 @@ __device__ __forceinline__ void sum_tile(const ProductArgs& p, int e, int m0, in
   SlabAcross<S::TN> b(static_cast<const E*>(p.b) + first * p.I + n0, (int64_t)p.I * 2, p.I - n0, ks, wave, lane);
   typename T::acc acc[S::MI][S::NJ];
   tile_ring<T, S>(a, b, nk, acc, smem);
-  tile_results<S>(acc, [&](int m, int n, f32x4 v) { store_sums(p, e, m0 + m, n0 + n, v); });
-  if (!mirror) return;
-  const int64_t out0 = (int64_t)e * p.O * p.I;
-  tile_results<S>(acc, [&](int m, int n, f32x4 v) {   // 16 lanes hold 16 neighbours of a transposed row
-    m += m0;
-    n += n0;
-    if (m >= p.O) return;
-    float* sums = static_cast<float*>(p.out) + out0 + (int64_t)n * p.I + m;
-#pragma unroll
-    for (int c = 0; c < 4; ++c, sums += p.I)
-      if (n + c < p.I) *sums = p.accumulate ? *sums + v[c] : v[c];
-  });
+  tile_results<S>(acc, smem, mirror, [&](int m, int n, f32x4 v) { store_sums(p, e, m0 + m, n0 + n, v); },
+                  [&](int n, int m, f32x4 v) { store_sums(p, e, n0 + n, m0 + m, v); });
 }
 
 // The same as a small tile.
-template <class T, bool kLoose>
+template <class T, int S, bool kLoose>
 __device__ __forceinline__ void sum_split(const ProductArgs& p, int e, int m0, int n0, bool mirror, uint8_t* smem) {
   using E = typename T::elem;
-  constexpr int S = kSumTile;
   const int lane = threadIdx.x & 63;
   int64_t first, end;
   group_rows(p.rows, e, first, end);
@@ -208,11 +196,11 @@ __global__ __launch_bounds__(256, 1) void k_sums_tile(ProductArgs p) {
   if (find_sum_tile(p, Whole::TM, kGram, e, m0, n0)) sum_tile<T>(p, e, m0, n0, kGram && m0 != n0, smem);
 }
 
-template <class T, bool kGram, bool kLoose>
+template <class T, bool kGram, int S, bool kLoose>
 __global__ __launch_bounds__(64 * kSplitWaves) void k_sums_split(ProductArgs p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   int e, m0, n0;
-  if (find_sum_tile(p, kSumTile, kGram, e, m0, n0)) sum_split<T, kLoose>(p, e, m0, n0, kGram && m0 != n0, smem);
+  if (find_sum_tile(p, S, kGram, e, m0, n0)) sum_split<T, S, kLoose>(p, e, m0, n0, kGram && m0 != n0, smem);
 }
 
 // Rows in 8-bit integers: s = max |x| / 127 in fp32, q = x / s to the nearest integer, ties to even.  A
@@ -340,12 +328,12 @@ hipError_t launch_rows(ProductArgs p, hipStream_t s) {
   p.vector_out = four_at_once(p.out, p.out_dtype, ns);
   const bool tight = p.O % (kForm == kForward ? 1 : unit) == 0 && p.I % unit == 0 && aligned16(p.a) && aligned16(p.b);
   constexpr double kMore = T::kDtype < 0 ? 1.4 : 1;
-  const TileCost large[] = {{256, 256, 1.15 * kMore, 1.6 * kMore}, {128, 256, 0.7 * kMore, 0.95 * kMore},
-                            {64, 256, 0.43 * kMore, 0.72 * kMore}};
-  const TileCost small[] = {{64, 64, 0.165, 0.22}, {64, 16, 0.1, 0.115}, {16, 64, 0.06, 0.1}, {16, 16, 0.02, 0.055}};
+  const TileCost large[] = {{256, 256, 3, 1.15 * kMore, 1.6 * kMore}, {128, 256, 2, 0.7 * kMore, 0.95 * kMore},
+                            {64, 256, 1.5, 0.43 * kMore, 0.72 * kMore}};
+  const TileCost small[] = {{64, 64, 1, 0.165, 0.22}, {64, 16, 1, 0.1, 0.115}, {16, 64, 1, 0.06, 0.1}, {16, 16, 0.5, 0.02, 0.055}};
   double best = 1e30;
-  RowsPlan plan = cheapest(p.rows, ns, slabs, small, true, 5.0, best, RowsPlan{});
-  if (tight) plan = cheapest(p.rows, ns, slabs, large, false, 7.0, best, plan);
+  RowsPlan plan = cheapest(p.rows, ns, slabs, small, true, best, RowsPlan{});
+  if (tight) plan = cheapest(p.rows, ns, slabs, large, false, best, plan);
   if (!tight) return launch_rows_split<T, kForm, true>(p, plan, s);
   if (plan.split) return launch_rows_split<T, kForm, false>(p, plan, s);
   p.height = plan.height;
@@ -360,19 +348,30 @@ hipError_t launch_sums(ProductArgs p, hipStream_t s) {
     return p.rows.groups * (kGram ? (tn + 1) / 2 * (tn + 1) : tm * tn);
   };
   const bool tight = p.O % 8 == 0 && p.I % 8 == 0 && aligned16(p.a) && aligned16(p.b);
-  // Whole workgroups on 256 x 256 tiles or wavefronts that share the sum of 64 x 64 ones, by the same reckoning
-  // (us, 256 | 64): 512 x 512 from 1024 rows 34 | 7, 16384 rows 317 | 62; 2048 x 2048 from 1024 rows 41 | 24,
-  // 16384 rows 326 | 300; 4096 x 4096 from 256 rows 28 | 38, 4096 rows 122 | 250
+  // Whole workgroups on 256 x 256 tiles, or wavefronts that share the sum of 64 x 64 or 32 x 32 ones: the cheapest
+  // by a tile's start and slabs, fitted to dW of one group (us, 256 | 64 | 32): 256 x 256 from 4096 rows 96 | 14 |
+  // 8, 16384 rows 318 | 49 | 42; 1024 x 1024 from 4096 rows 95 | 19 | 38; 2048 x 2048 from 256 rows 21 | 12 | 14,
+  // 16384 rows 318 | 304 | 850; 4096 x 4096 from 256 rows 27 | 38 | 46, 4096 rows 113 | 235 | 514; 8192 x 8192 from
+  // 16 rows 82 | 54 | 54, 256 rows 104 | 138 | 170.  H stores most tiles twice.
   const double slabs = (double)p.rows.rows / 64 / p.rows.groups;
-  const auto rounds = [&](int64_t tile) { return std::max(1.0, std::ceil(count(tile) / 256.0)); };
-  const double load = std::min(1.0, count(Whole::TM) / 256.0);
-  const double us_large = 15 + slabs * (1.2 + 0.5 * load) * rounds(Whole::TM);
-  const double us_small = 5 + (slabs + 1) * 0.3 * rounds(kSumTile);
-  if (tight && us_large < us_small) return launch_ring<k_sums_tile<T, kGram>>(count(Whole::TM), s, p);
+  const auto cost = [&](int64_t tile, double start, double more_start, double alone, double full) {
+    const double rounds = count(tile) / 256.0, load = std::min(1.0, rounds);
+    return std::max(1.0, p.rows.groups == 1 ? std::ceil(rounds) : rounds) *
+           (start + more_start * load + (slabs + 0.5) * (alone + (full - alone) * load));
+  };
+  const double us_large = cost(Whole::TM, kGram ? 20 : 12, kGram ? 12 : 7, 1.2, 1.4);
+  const double us_small = cost(64, kGram ? 1.4 : 0.7, 0, 0.17, 0.23), us_tiny = cost(32, kGram ? 0.3 : 0.15, 0, 0.08, 0.14);
+  if (tight && us_large < std::min(us_small, us_tiny)) return launch_ring<k_sums_tile<T, kGram>>(count(Whole::TM), s, p);
   const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(kSplitWaves, (p.rows.rows + 63) / 64));
-  const size_t lds = waves * 2 * kSumTile * ROW_BYTES;
-  return tight ? launch_lds<k_sums_split<T, kGram, false>>(count(kSumTile), 64 * waves, lds, s, p)
-               : launch_lds<k_sums_split<T, kGram, true>>(count(kSumTile), 64 * waves, lds, s, p);
+  const auto launch = [&](auto size, auto loose) {
+    constexpr int S = decltype(size)::value;
+    return launch_lds<k_sums_split<T, kGram, S, decltype(loose)::value>>(count(S), 64 * waves, (size_t)waves * 2 * S * ROW_BYTES,
+                                                                         s, p);
+  };
+  using Is64 = std::integral_constant<int, 64>;
+  using Is32 = std::integral_constant<int, 32>;
+  if (us_tiny < us_small) return tight ? launch(Is32{}, std::false_type{}) : launch(Is32{}, std::true_type{});
+  return tight ? launch(Is64{}, std::false_type{}) : launch(Is64{}, std::true_type{});
 }
 
 }  // namespace

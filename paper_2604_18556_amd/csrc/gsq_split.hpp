@@ -23,10 +23,22 @@ __device__ __forceinline__ i32x4 load_chunk(const E* p, int n) {
   if (n >= PER) {
     __builtin_memcpy(&v, p, 16);
   } else if (n > 0) {
-    E e[PER];
-#pragma unroll
-    for (int c = 0; c < PER; ++c) e[c] = c < n ? p[c] : (E)0;
-    __builtin_memcpy(&v, e, 16);
+    // eight, four, two bytes and one, of which n's bits say which there are
+    uint64_t part[2] = {0, 0};
+    const uint8_t* b = reinterpret_cast<const uint8_t*>(p);
+    const int bytes = n * (int)sizeof(E);
+    int at = 0;
+    const auto add = [&](uint64_t piece, int size) {
+      piece <<= 8 * (at & 7);
+      part[0] |= at < 8 ? piece : 0;
+      part[1] |= at < 8 ? 0 : piece;
+      at += size;
+    };
+    if (bytes & 8) { uint64_t x; __builtin_memcpy(&x, b, 8); add(x, 8); }
+    if (bytes & 4) { uint32_t x; __builtin_memcpy(&x, b + at, 4); add(x, 4); }
+    if (bytes & 2) { uint16_t x; __builtin_memcpy(&x, b + at, 2); add(x, 2); }
+    if (sizeof(E) == 1 && (bytes & 1)) add(b[at], 1);
+    __builtin_memcpy(&v, part, 16);
   }
   return v;
 }
@@ -103,6 +115,31 @@ struct Copied : Slab {
   __device__ __forceinline__ void commit(uint8_t*) const {}
 };
 
+// A wavefront's sums of a tile to LDS, rows of TN: a lane has row lane % 16 and four columns of a block.  The
+// fours of a row are turned by the row, so that rows fall on different banks.
+template <int TM, int TN, class Acc>
+__device__ __forceinline__ void split_sums(const Acc (&acc)[TM / 16][TN / 16], uint8_t* own) {
+  constexpr int FOURS = TN / 4;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < TM / 16; ++i)
+#pragma unroll
+    for (int j = 0; j < TN / 16; ++j) {
+      const int row = i * 16 + (lane & 15), c = j * 4 + (lane >> 4);
+      reinterpret_cast<Acc*>(own)[row * FOURS + (c ^ (row % FOURS))] = acc[i][j];
+    }
+}
+
+// The c-th four of a row, added over the first `parts` wavefronts.
+template <int TN, class Acc>
+__device__ __forceinline__ Acc added_sums(const uint8_t* smem, int pitch, int parts, int row, int c) {
+  constexpr int FOURS = TN / 4;
+  Acc v = {};
+  for (int w = 0; w < parts; ++w)
+    v += reinterpret_cast<const Acc*>(smem + w * pitch)[row * FOURS + (c ^ (row % FOURS))];
+  return v;
+}
+
 // A TM x TN tile: sums of slabs k = wave, wave + waves, ... < nk of each wavefront, added up, to
 // store(row, column, four consecutive columns' sums), called for whole fours of the tile; with `mirror`, also
 // turned over, to store_mirror(column, row, four consecutive rows' sums).
@@ -146,25 +183,15 @@ __device__ __forceinline__ void tile_split(A& a, B& b, int nk, uint8_t* smem, bo
           for (int j = 0; j < NJ; ++j) acc[i][j] = T::mfma(fb[h][j], fa[h][i], acc[i][j]);
     }
   }
-  // a lane has row lane % 16 and four columns of a block; rows of TN sums in LDS, the last 16 bytes' place
-  // turned by the row
-  typename T::acc* const sums = reinterpret_cast<typename T::acc*>(own);
   constexpr int FOURS = TN / 4;
-#pragma unroll
-  for (int i = 0; i < MI; ++i)
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int row = i * 16 + (lane & 15), c = j * 4 + (lane >> 4);
-      sums[row * FOURS + (c ^ (row % FOURS))] = acc[i][j];
-    }
+  split_sums<TM, TN>(acc, own);
   __syncthreads();
   const int parts = min(waves, nk);
   for (int f = threadIdx.x; f < TM * FOURS; f += blockDim.x) {
-    const int row = f / FOURS, c = f % FOURS, at = row * FOURS + (c ^ (row % FOURS));
-    typename T::acc v = {};
-    for (int w = 0; w < parts; ++w) v += reinterpret_cast<typename T::acc*>(smem + w * SLAB)[at];
+    const int row = f / FOURS, c = f % FOURS;
+    const typename T::acc v = added_sums<TN, typename T::acc>(smem, SLAB, parts, row, c);
     store(row, 4 * c, v);
-    if (mirror) reinterpret_cast<typename T::acc*>(smem)[at] = v;
+    if (mirror) reinterpret_cast<typename T::acc*>(smem)[row * FOURS + (c ^ (row % FOURS))] = v;
   }
   if (!mirror) return;
   __syncthreads();
@@ -173,7 +200,7 @@ __device__ __forceinline__ void tile_split(A& a, B& b, int nk, uint8_t* smem, bo
     typename T::acc v;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      v[r] = reinterpret_cast<typename T::acc*>(smem)[(row + r) * FOURS + ((col / 4) ^ ((row + r) % FOURS))][col % 4];
+      v[r] = reinterpret_cast<const typename T::acc*>(smem)[(row + r) * FOURS + ((col / 4) ^ ((row + r) % FOURS))][col % 4];
     store_mirror(col, row, v);
   }
 }

@@ -4,7 +4,6 @@
 #include <stdint.h>
 
 #include <atomic>
-#include <cstdlib>
 #include <type_traits>
 #include <utility>
 
@@ -294,16 +293,51 @@ __device__ __forceinline__ void tile_ring(const A& a, B& b, int nk,
   acc_settled(acc);
 }
 
-// The tile's results: store(row, column, four consecutive columns' values) for every block.  Lane l of a
-// block has row l % 16 and columns 4 (l / 16) .. + 3.
-template <class S, class Acc, class Store>
-__device__ __forceinline__ void tile_results(const Acc (&acc)[S::MI][S::NJ], Store store) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int m = (wave >> 1) * (S::TM / 2) + (lane & 15), n = (wave & 1) * (S::TN / 2) + 4 * (lane >> 4);
+// Place of the c-th four of row m of half a tile's results in LDS (fours): the fours of a row are turned, so that
+// 16 rows, and every fourth of 64, fall on different banks.
+template <class S>
+__device__ __forceinline__ int result_place(int m, int c) {
+  return m * (S::TN / 8) + (c ^ ((m ^ (m >> 2)) & 15));
+}
+
+// The tile's results, half of its columns after the other through LDS (free of slabs by then):
+// store(row, column, four consecutive columns' values), whose lanes follow each other along a row; with
+// `mirror`, also store_mirror(column, row, four consecutive rows' values).  Stores straight from the
+// accumulators write pieces of 64 bytes, and their code, as long as there are accumulators and run through
+// once, is fetched more slowly than it runs.
+template <class S, class Acc, class Store, class StoreMirror>
+__device__ __forceinline__ void tile_results(const Acc (&acc)[S::MI][S::NJ], uint8_t* smem, bool mirror, Store store,
+                                             StoreMirror store_mirror) {
+  constexpr int FOURS = S::TN / 8, kTimes = S::TM * FOURS / 256;
+  static_assert(S::TM * FOURS * 16 <= (int)LDS_BYTES && FOURS % 16 == 0, "half a tile in LDS");
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  Acc* const part = reinterpret_cast<Acc*>(smem);
+#pragma unroll 1
+  for (int h = 0; h < 2; ++h) {
+    __syncthreads();
+    if ((wave & 1) == h)
 #pragma unroll
-  for (int i = 0; i < S::MI; ++i)
+      for (int i = 0; i < S::MI; ++i)
 #pragma unroll
-    for (int j = 0; j < S::NJ; ++j) store(m + i * 16, n + j * 16, acc[i][j]);
+        for (int j = 0; j < S::NJ; ++j)
+          part[result_place<S>((wave >> 1) * (S::TM / 2) + i * 16 + (lane & 15), j * 4 + (lane >> 4))] = acc[i][j];
+    __syncthreads();
+#pragma unroll 4
+    for (int k = 0; k < kTimes; ++k) {
+      const int f = k * 256 + tid, m = f / FOURS, c = f % FOURS;
+      store(m, h * (S::TN / 2) + 4 * c, part[result_place<S>(m, c)]);
+    }
+    if (mirror)
+#pragma unroll 1
+      for (int k = 0; k < kTimes / 4; ++k) {   // blocks of 4 x 4, neighbours along a transposed row
+        const int f = k * 256 + tid, m = f % (S::TM / 4) * 4, c = f / (S::TM / 4);
+        Acc v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = part[result_place<S>(m + r, c)];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) store_mirror(h * (S::TN / 2) + 4 * c + n, m, Acc{v[0][n], v[1][n], v[2][n], v[3][n]});
+      }
+  }
 }
 
 // Four consecutive output elements, together where `four` says that they are whole and aligned.
@@ -357,16 +391,18 @@ __device__ __forceinline__ bool find_rows_tile(const GroupRows& rows, int height
 template <auto kKernel, class... Args>
 hipError_t launch_lds(int64_t blocks, int threads, size_t lds, hipStream_t s, const Args&... args) {
   if (blocks * threads >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;   // the limit of grid.x
-  static std::atomic<uint64_t> leave{0};   // a bit per device
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return e;
-  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
-  if (!(leave.load(std::memory_order_relaxed) & bit)) {
-    e = hipFuncSetAttribute(reinterpret_cast<const void*>(kKernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                            (int)LDS_BYTES);
+  if (lds > 64 * 1024) {
+    static std::atomic<uint64_t> leave{0};   // a bit per device
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
-    leave.fetch_or(bit, std::memory_order_relaxed);
+    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+    if (!(leave.load(std::memory_order_relaxed) & bit)) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(kKernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)LDS_BYTES);
+      if (e != hipSuccess) return e;
+      leave.fetch_or(bit, std::memory_order_relaxed);
+    }
   }
   kKernel<<<(unsigned)blocks, threads, lds, s>>>(args...);
   return hipGetLastError();
@@ -387,24 +423,25 @@ struct RowsPlan {
   int height, width;
 };
 
-// Microseconds of each slab (128 bytes of k) of a tile: on an empty GPU, and with a tile on each of 256 CUs.
+// Microseconds of a tile: its start, and each slab (128 bytes of k) on an empty GPU and with a tile on each of
+// 256 CUs.
 struct TileCost {
   int height, width;
-  double alone, full;
+  double start, alone, full;
 };
 
-// The cheapest of several tiles.  A product takes a start, and its slabs times the rounds of 256 tiles that it
-// fills; the groups' last panels are taken to be half full.
+// The cheapest of several tiles: a launch, and a tile's time for each round of 256 tiles.  The groups' last
+// panels are taken to be half full.
 template <int N>
-RowsPlan cheapest(const GroupRows& r, int cols, int slabs, const TileCost (&costs)[N], bool split, double start,
-                  double& best, RowsPlan plan) {
+RowsPlan cheapest(const GroupRows& r, int cols, int slabs, const TileCost (&costs)[N], bool split, double& best,
+                  RowsPlan plan) {
   const double few = (double)(r.rows < r.groups ? r.rows : r.groups);
   for (const TileCost& c : costs) {
     const double panels = r.groups == 1 ? (double)((r.rows + c.height - 1) / c.height) : r.rows / (double)c.height + few / 2;
     const double tiles = panels * tiles_of(cols, c.width), rounds = tiles / 256;
     const double whole = rounds < 1 ? 1 : r.groups == 1 ? (double)(int64_t)(rounds + 0.999) : rounds;
     const double each = c.alone + (c.full - c.alone) * (rounds < 1 ? rounds : 1);
-    const double us = start + slabs * each * whole;
+    const double us = 4 + whole * (c.start + slabs * each);
     if (us < best) {
       best = us;
       plan = {split, c.height, c.width};
