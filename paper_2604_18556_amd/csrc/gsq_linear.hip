@@ -309,7 +309,6 @@ template <class T, int BITS, bool kFine, int TM>
 __device__ __forceinline__ void packed_shared(const PackedLayer& L, const typename T::elem* x, typename T::elem* y,
                                               int group, int64_t first, int ms, int n0, int vector_out, uint8_t* smem) {
   constexpr int MI = TM / 16, NJ = kSharedCols / 16, A_SLAB = TM * ROW_BYTES, OWN = 2 * A_SLAB;
-  constexpr int FOURS = kSharedCols / 4;
   const int lane = threadIdx.x & 63, waves = blockDim.x >> 6, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint8_t* const own = smem + wave * OWN;
@@ -354,14 +353,8 @@ __device__ __forceinline__ void packed_shared(const PackedLayer& L, const typena
       }
   }
   split_sums<TM, kSharedCols>(acc, own);
-  __syncthreads();
-  const int parts = min(waves, L.blocks);
-  for (int f = threadIdx.x; f < TM * FOURS; f += blockDim.x) {
-    const int m = f / FOURS, c = f % FOURS;
-    const f32x4 v = added_sums<kSharedCols, f32x4>(smem, OWN, parts, m, c);
-    if (m < ms && n0 + 4 * c < L.O)
-      store_four(y, T::kDtype, (first + m) * L.O + n0 + 4 * c, v, L.O - n0 - 4 * c, vector_out);
-  }
+  const ResultColumns<typename T::elem> out{y + first * L.O + n0, L.O, ms, L.O - n0, vector_out != 0};
+  store_added<TM, kSharedCols, f32x4>(smem, OWN, min(waves, L.blocks), out, false, out);
 }
 
 template <class T, int BITS, bool kFine>
@@ -434,11 +427,8 @@ __device__ __forceinline__ void packed_tile(const PackedLayer& L, const typename
   SlabPacked<T, BITS, kFine, S::TN> b(L, at.group, at.n0, wave, lane);
   typename T::acc acc[S::MI][S::NJ];
   tile_ring<T, S>(a, b, (L.I + 63) / 64, acc, smem);
-  const auto store = [&](int m, int n, f32x4 v) {
-    if (m < at.ms && at.n0 + n < L.O)
-      store_four(y, T::kDtype, (at.first + m) * L.O + at.n0 + n, v, L.O - at.n0 - n, vector_out);
-  };
-  tile_results<S>(acc, smem, false, store, store);
+  const ResultColumns<typename T::elem> out{y + at.first * L.O + at.n0, L.O, at.ms, L.O - at.n0, vector_out != 0};
+  tile_results<S>(acc, smem, out, false, out);
 }
 
 template <class T, int BITS, bool kFine>

@@ -10,21 +10,17 @@
 namespace gsq {
 namespace {
 
-// Four consecutive results of row `first` + m of y or dx from column n, those in bounds.
+// Columns n0 .. of y or dx for the ms rows from `first`.
 template <class T>
-__device__ __forceinline__ void store_rows(const ProductArgs& p, int group, int64_t first, int ms, int ns, int m,
-                                           int n, typename T::acc v) {
-  if (m >= ms || n >= ns) return;
-  f32x4 y;
-#pragma unroll
-  for (int c = 0; c < 4; ++c) y[c] = (float)v[c];
-  if constexpr (T::kDtype < 0) {   // 8-bit integers: the sum is exact in 32 bits
-    const float* bs = p.b_scales + (int64_t)group * p.O + n;
-    const float as = p.a_scales[first + m];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) y[c] = y[c] * as * bs[min(c, ns - n - 1)];
+__device__ __forceinline__ ResultColumns<typename T::out> row_columns(const ProductArgs& p, int group, int64_t first,
+                                                                      int ms, int ns, int n0) {
+  ResultColumns<typename T::out> r{static_cast<typename T::out*>(p.out) + first * ns + n0, ns, ms, ns - n0,
+                                   p.vector_out != 0};
+  if constexpr (T::kDtype < 0) {
+    r.row_scales = p.a_scales + first;
+    r.col_scales = p.b_scales + (int64_t)group * p.O + n0;
   }
-  store_four(p.out, p.out_dtype, (first + m) * ns + n, y, ns - n, p.vector_out);
+  return r;
 }
 
 // One tile of y or dx.
@@ -46,8 +42,8 @@ __device__ __forceinline__ void rows_tile(const ProductArgs& p, const RowsTile& 
     SlabAcross<S::TN> b(w + n0, (int64_t)ns * sizeof(E), ns - n0, ks, wave, lane);
     tile_ring<T, S>(a, b, nk, acc, smem);
   }
-  const auto store = [&](int m, int n, typename T::acc v) { store_rows<T>(p, at.group, first, ms, ns, m, n0 + n, v); };
-  tile_results<S>(acc, smem, false, store, store);
+  const auto out = row_columns<T>(p, at.group, first, ms, ns, n0);
+  tile_results<S>(acc, smem, out, false, out);
 }
 
 // y or dx.
@@ -74,24 +70,24 @@ __device__ __forceinline__ void rows_split(const ProductArgs& p, int group, int6
   const int nk = (int)(((int64_t)ks * sizeof(E) + ROW_BYTES - 1) / ROW_BYTES);
   const E* w = static_cast<const E*>(p.b) + (int64_t)group * p.O * p.I;
   const E* x = static_cast<const E*>(p.a) + first * ks;
-  const auto store = [&](int m, int n, typename T::acc v) { store_rows<T>(p, group, first, ms, ns, m, n0 + n, v); };
+  const auto out = row_columns<T>(p, group, first, ms, ns, n0);
   if constexpr (kLoose) {
     LooseAlong<E, TM> a(x, ks, ms, ks);
     if constexpr (kForm == kForward) {
       LooseAlong<E, TN> b(w + (int64_t)n0 * ks, ks, ns - n0, ks);
-      tile_split<T, TM, TN>(a, b, nk, smem, false, store, store);
+      tile_split<T, TM, TN>(a, b, nk, smem, out, false, out);
     } else {
       LooseAcross<E, TN> b(w + n0, ns, ns - n0, ks);
-      tile_split<T, TM, TN>(a, b, nk, smem, false, store, store);
+      tile_split<T, TM, TN>(a, b, nk, smem, out, false, out);
     }
   } else {
     Copied<SlabAlong<TM, TM / 8>> a(x, (int64_t)ks * sizeof(E), ms, 0, lane);
     if constexpr (kForm == kForward) {
       Copied<SlabAlong<TN, TN / 8>> b(w + (int64_t)n0 * ks, (int64_t)ks * sizeof(E), ns - n0, 0, lane);
-      tile_split<T, TM, TN>(a, b, nk, smem, false, store, store);
+      tile_split<T, TM, TN>(a, b, nk, smem, out, false, out);
     } else {
       Copied<SlabAcross<TN, TN / 8>> b(w + n0, (int64_t)ns * sizeof(E), ns - n0, ks, 0, lane);
-      tile_split<T, TM, TN>(a, b, nk, smem, false, store, store);
+      tile_split<T, TM, TN>(a, b, nk, smem, out, false, out);
     }
   }
 }
@@ -112,21 +108,16 @@ __global__ __launch_bounds__(64 * kSplitWaves) void k_rows_split(ProductArgs p) 
     rows_split<T, kForm, TM, TN, kLoose>(p, at.group, first, ms, tn * TN, smem);
 }
 
-// Four consecutive columns of row m of a group's sum, those in bounds.
-__device__ __forceinline__ void store_sums(const ProductArgs& p, int e, int m, int n, f32x4 v) {
-  if (m >= p.O || n >= p.I) return;
-  const int64_t at = ((int64_t)e * p.O + m) * p.I + n;
-  if (p.accumulate) {
-    const float* sums = static_cast<const float*>(p.out) + at;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) v[c] += n + c < p.I ? sums[c] : 0.f;
-  }
-  store_four(p.out, p.out_dtype, at, v, p.I - n, p.vector_out);
+// Columns n0 .. of a group's sum for the rows from m0.
+template <class Out>
+__device__ __forceinline__ ResultColumns<Out> sum_columns(const ProductArgs& p, int e, int m0, int n0) {
+  return {static_cast<Out*>(p.out) + ((int64_t)e * p.O + m0) * p.I + n0, p.I, p.O - m0, p.I - n0, p.vector_out != 0,
+          p.accumulate != 0};
 }
 
 // One tile of a sum over a group's rows: out[m0 .., n0 ..] (+)= sum_r a[r, m] b[r, n], and with `mirror` its
 // transpose too.
-template <class T>
+template <class T, class Out>
 __device__ __forceinline__ void sum_tile(const ProductArgs& p, int e, int m0, int n0, bool mirror, uint8_t* smem) {
   using E = typename T::elem;
   using S = Whole;
@@ -139,12 +130,11 @@ __device__ __forceinline__ void sum_tile(const ProductArgs& p, int e, int m0, in
   SlabAcross<S::TN> b(static_cast<const E*>(p.b) + first * p.I + n0, (int64_t)p.I * 2, p.I - n0, ks, wave, lane);
   typename T::acc acc[S::MI][S::NJ];
   tile_ring<T, S>(a, b, nk, acc, smem);
-  tile_results<S>(acc, smem, mirror, [&](int m, int n, f32x4 v) { store_sums(p, e, m0 + m, n0 + n, v); },
-                  [&](int n, int m, f32x4 v) { store_sums(p, e, n0 + n, m0 + m, v); });
+  tile_results<S>(acc, smem, sum_columns<Out>(p, e, m0, n0), mirror, sum_columns<Out>(p, e, n0, m0));
 }
 
 // The same as a small tile.
-template <class T, int S, bool kLoose>
+template <class T, class Out, int S, bool kLoose>
 __device__ __forceinline__ void sum_split(const ProductArgs& p, int e, int m0, int n0, bool mirror, uint8_t* smem) {
   using E = typename T::elem;
   const int lane = threadIdx.x & 63;
@@ -153,14 +143,13 @@ __device__ __forceinline__ void sum_split(const ProductArgs& p, int e, int m0, i
   const int ks = (int)(end - first), nk = (ks + kSlabRows - 1) / kSlabRows;
   const E* dy = static_cast<const E*>(p.a) + first * p.O + m0;
   const E* x = static_cast<const E*>(p.b) + first * p.I + n0;
-  const auto store = [&](int m, int n, f32x4 v) { store_sums(p, e, m0 + m, n0 + n, v); };
-  const auto store_mirror = [&](int n, int m, f32x4 v) { store_sums(p, e, n0 + n, m0 + m, v); };
+  const auto out = sum_columns<Out>(p, e, m0, n0), turned = sum_columns<Out>(p, e, n0, m0);
   if constexpr (kLoose) {
     LooseAcross<E, S> a(dy, p.O, p.O - m0, ks), b(x, p.I, p.I - n0, ks);
-    tile_split<T, S, S>(a, b, nk, smem, mirror, store, store_mirror);
+    tile_split<T, S, S>(a, b, nk, smem, out, mirror, turned);
   } else {
     Copied<SlabAcross<S, S / 8>> a(dy, (int64_t)p.O * 2, p.O - m0, ks, 0, lane), b(x, (int64_t)p.I * 2, p.I - n0, ks, 0, lane);
-    tile_split<T, S, S>(a, b, nk, smem, mirror, store, store_mirror);
+    tile_split<T, S, S>(a, b, nk, smem, out, mirror, turned);
   }
 }
 
@@ -189,18 +178,18 @@ __device__ __forceinline__ bool find_sum_tile(const ProductArgs& p, int size, bo
   return true;
 }
 
-template <class T, bool kGram>
+template <class T, class Out, bool kGram>
 __global__ __launch_bounds__(256, 1) void k_sums_tile(ProductArgs p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   int e, m0, n0;
-  if (find_sum_tile(p, Whole::TM, kGram, e, m0, n0)) sum_tile<T>(p, e, m0, n0, kGram && m0 != n0, smem);
+  if (find_sum_tile(p, Whole::TM, kGram, e, m0, n0)) sum_tile<T, Out>(p, e, m0, n0, kGram && m0 != n0, smem);
 }
 
-template <class T, bool kGram, int S, bool kLoose>
+template <class T, class Out, bool kGram, int S, bool kLoose>
 __global__ __launch_bounds__(64 * kSplitWaves) void k_sums_split(ProductArgs p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   int e, m0, n0;
-  if (find_sum_tile(p, S, kGram, e, m0, n0)) sum_split<T, S, kLoose>(p, e, m0, n0, kGram && m0 != n0, smem);
+  if (find_sum_tile(p, S, kGram, e, m0, n0)) sum_split<T, Out, S, kLoose>(p, e, m0, n0, kGram && m0 != n0, smem);
 }
 
 // Rows in 8-bit integers: s = max |x| / 127 in fp32, q = x / s to the nearest integer, ties to even.  A
@@ -340,7 +329,7 @@ hipError_t launch_rows(ProductArgs p, hipStream_t s) {
   return launch_ring<k_rows_tile<T, kForm>>(most_panels(p.rows, p.height) * tiles_of(ns, Whole::TN), s, p);
 }
 
-template <class T, bool kGram>
+template <class T, class Out, bool kGram>
 hipError_t launch_sums(ProductArgs p, hipStream_t s) {
   p.vector_out = four_at_once(p.out, p.out_dtype, p.I);
   const auto count = [&](int64_t tile) {
@@ -361,11 +350,11 @@ hipError_t launch_sums(ProductArgs p, hipStream_t s) {
   };
   const double us_large = cost(Whole::TM, kGram ? 20 : 12, kGram ? 12 : 7, 1.2, 1.4);
   const double us_small = cost(64, kGram ? 1.4 : 0.7, 0, 0.17, 0.23), us_tiny = cost(32, kGram ? 0.3 : 0.15, 0, 0.08, 0.14);
-  if (tight && us_large < std::min(us_small, us_tiny)) return launch_ring<k_sums_tile<T, kGram>>(count(Whole::TM), s, p);
+  if (tight && us_large < std::min(us_small, us_tiny)) return launch_ring<k_sums_tile<T, Out, kGram>>(count(Whole::TM), s, p);
   const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(kSplitWaves, (p.rows.rows + 63) / 64));
   const auto launch = [&](auto size, auto loose) {
     constexpr int S = decltype(size)::value;
-    return launch_lds<k_sums_split<T, kGram, S, decltype(loose)::value>>(count(S), 64 * waves, (size_t)waves * 2 * S * ROW_BYTES,
+    return launch_lds<k_sums_split<T, Out, kGram, S, decltype(loose)::value>>(count(S), 64 * waves, (size_t)waves * 2 * S * ROW_BYTES,
                                                                          s, p);
   };
   using Is64 = std::integral_constant<int, 64>;
@@ -380,13 +369,17 @@ hipError_t launch_product(int form, int dtype, const ProductArgs& p, hipStream_t
   const bool bf16 = dtype == GSQ_DT_BF16;
   if (form == kForward) return bf16 ? launch_rows<Bf16, kForward>(p, s) : launch_rows<F16, kForward>(p, s);
   if (form == kInputGrad) return bf16 ? launch_rows<Bf16, kInputGrad>(p, s) : launch_rows<F16, kInputGrad>(p, s);
-  return bf16 ? launch_sums<Bf16, false>(p, s) : launch_sums<F16, false>(p, s);
+  if (p.out_dtype == GSQ_DT_FP32)
+    return bf16 ? launch_sums<Bf16, float, false>(p, s) : launch_sums<F16, float, false>(p, s);
+  return bf16 ? launch_sums<Bf16, __bf16, false>(p, s) : launch_sums<F16, _Float16, false>(p, s);
 }
 
-hipError_t launch_product_i8(const ProductArgs& p, hipStream_t s) { return launch_rows<I8, kForward>(p, s); }
+hipError_t launch_product_i8(const ProductArgs& p, hipStream_t s) {
+  return p.out_dtype == GSQ_DT_BF16 ? launch_rows<I8<__bf16>, kForward>(p, s) : launch_rows<I8<_Float16>, kForward>(p, s);
+}
 
 hipError_t launch_gram(int dtype, const ProductArgs& p, hipStream_t s) {
-  return dtype == GSQ_DT_BF16 ? launch_sums<Bf16, true>(p, s) : launch_sums<F16, true>(p, s);
+  return dtype == GSQ_DT_BF16 ? launch_sums<Bf16, float, true>(p, s) : launch_sums<F16, float, true>(p, s);
 }
 
 hipError_t launch_quantize_rows(const void* x, int dtype, int64_t rows, int64_t cols, int8_t* q,

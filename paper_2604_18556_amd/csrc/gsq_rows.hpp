@@ -16,6 +16,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // Element types: what a matrix instruction of 16 x 16 x kStep takes and sums into.
 struct Bf16 {
   using elem = __bf16;
+  using out = __bf16;
   using frag = bf16x8;
   using acc = f32x4;
   static constexpr int kStep = 32, kDtype = GSQ_DT_BF16;
@@ -25,6 +26,7 @@ struct Bf16 {
 };
 struct F16 {
   using elem = _Float16;
+  using out = _Float16;
   using frag = f16x8;
   using acc = f32x4;
   static constexpr int kStep = 32, kDtype = GSQ_DT_FP16;
@@ -32,8 +34,10 @@ struct F16 {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
   }
 };
+template <class Out>      // of the scaled sums
 struct I8 {
   using elem = int8_t;
+  using out = Out;
   using frag = i32x4;
   using acc = i32x4;
   static constexpr int kStep = 64, kDtype = -1;
@@ -102,16 +106,6 @@ __device__ __forceinline__ bool find_panel(const GroupRows& g, int height, int64
 // Most panels there can be, for the grid.
 inline int64_t most_panels(const GroupRows& g, int64_t height) {
   return g.rows / height + (g.rows < g.groups ? g.rows : g.groups);
-}
-
-// Output element: rounded once, to the nearest (ties to even).
-__device__ __forceinline__ void store_out(void* out, int dtype, int64_t at, float v) {
-  if (dtype == GSQ_DT_BF16)
-    static_cast<__bf16*>(out)[at] = (__bf16)v;
-  else if (dtype == GSQ_DT_FP16)
-    static_cast<_Float16*>(out)[at] = (_Float16)v;
-  else
-    static_cast<float*>(out)[at] = v;
 }
 
 }  // namespace

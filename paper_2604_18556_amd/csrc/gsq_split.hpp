@@ -140,14 +140,40 @@ __device__ __forceinline__ Acc added_sums(const uint8_t* smem, int pitch, int pa
   return v;
 }
 
-// A TM x TN tile: sums of slabs k = wave, wave + waves, ... < nk of each wavefront, added up, to
-// store(row, column, four consecutive columns' sums), called for whole fours of the tile; with `mirror`, also
-// turned over, to store_mirror(column, row, four consecutive rows' sums).
+// Where the sums of a tile are added and stored: rows of TN in LDS, the first `parts` wavefronts' at `pitch`
+// bytes from each other; with `mirror` also turned over.  Every thread of the workgroup calls it.
+template <int TM, int TN, class Acc, class Columns>
+__device__ __forceinline__ void store_added(uint8_t* smem, int pitch, int parts, Columns out, bool mirror, Columns turned) {
+  constexpr int FOURS = TN / 4;
+  __syncthreads();
+  for (int f = threadIdx.x; f < TM * FOURS; f += blockDim.x) {
+    const int row = f / FOURS, c = f % FOURS;
+    out.begin(4 * c);
+    const auto held = out.hold(row);
+    const Acc v = added_sums<TN, Acc>(smem, pitch, parts, row, c);
+    out.put(row, v, held);
+    if (mirror) reinterpret_cast<Acc*>(smem)[row * FOURS + (c ^ (row % FOURS))] = v;
+  }
+  if (!mirror) return;
+  __syncthreads();
+  for (int f = threadIdx.x; f < TN * (TM / 4); f += blockDim.x) {
+    const int row = 4 * (f % (TM / 4)), col = f / (TM / 4);
+    Acc v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      v[r] = reinterpret_cast<const Acc*>(smem)[(row + r) * FOURS + ((col / 4) ^ ((row + r) % FOURS))][col % 4];
+    turned.begin(row);
+    turned.put(col, v, turned.hold(col));
+  }
+}
+
+// A TM x TN tile: sums of slabs k = wave, wave + waves, ... < nk of each wavefront, added up, to `out`, and with
+// `mirror` also turned over to `turned`.
 // A wavefront reads a slab's fragments into registers, lets the next slab follow into the same LDS, and
 // multiplies meanwhile.
-template <class T, int TM, int TN, class A, class B, class Store, class StoreMirror>
-__device__ __forceinline__ void tile_split(A& a, B& b, int nk, uint8_t* smem, bool mirror, Store store,
-                                           StoreMirror store_mirror) {
+template <class T, int TM, int TN, class A, class B, class Columns>
+__device__ __forceinline__ void tile_split(A& a, B& b, int nk, uint8_t* smem, Columns out, bool mirror,
+                                           Columns turned) {
   constexpr int MI = TM / 16, NJ = TN / 16;
   constexpr int A_SLAB = TM * ROW_BYTES, SLAB = A_SLAB + TN * ROW_BYTES;
   static_assert(TM * TN * 4 <= SLAB, "the sums take the slabs' place");
@@ -183,26 +209,8 @@ __device__ __forceinline__ void tile_split(A& a, B& b, int nk, uint8_t* smem, bo
           for (int j = 0; j < NJ; ++j) acc[i][j] = T::mfma(fb[h][j], fa[h][i], acc[i][j]);
     }
   }
-  constexpr int FOURS = TN / 4;
   split_sums<TM, TN>(acc, own);
-  __syncthreads();
-  const int parts = min(waves, nk);
-  for (int f = threadIdx.x; f < TM * FOURS; f += blockDim.x) {
-    const int row = f / FOURS, c = f % FOURS;
-    const typename T::acc v = added_sums<TN, typename T::acc>(smem, SLAB, parts, row, c);
-    store(row, 4 * c, v);
-    if (mirror) reinterpret_cast<typename T::acc*>(smem)[row * FOURS + (c ^ (row % FOURS))] = v;
-  }
-  if (!mirror) return;
-  __syncthreads();
-  for (int f = threadIdx.x; f < TN * (TM / 4); f += blockDim.x) {
-    const int row = 4 * (f % (TM / 4)), col = f / (TM / 4);
-    typename T::acc v;
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      v[r] = reinterpret_cast<const typename T::acc*>(smem)[(row + r) * FOURS + ((col / 4) ^ ((row + r) % FOURS))][col % 4];
-    store_mirror(col, row, v);
-  }
+  store_added<TM, TN, typename T::acc>(smem, SLAB, min(waves, nk), out, mirror, turned);
 }
 
 }  // namespace

@@ -300,16 +300,73 @@ __device__ __forceinline__ int result_place(int m, int c) {
   return m * (S::TN / 8) + (c ^ ((m ^ (m >> 2)) & 15));
 }
 
-// The tile's results, half of its columns after the other through LDS (free of slabs by then):
-// store(row, column, four consecutive columns' values), whose lanes follow each other along a row; with
-// `mirror`, also store_mirror(column, row, four consecutive rows' values).  Stores straight from the
-// accumulators write pieces of 64 bytes, and their code, as long as there are accumulators and run through
-// once, is fetched more slowly than it runs.
-template <class S, class Acc, class Store, class StoreMirror>
-__device__ __forceinline__ void tile_results(const Acc (&acc)[S::MI][S::NJ], uint8_t* smem, bool mirror, Store store,
-                                             StoreMirror store_mirror) {
-  constexpr int FOURS = S::TN / 8, kTimes = S::TM * FOURS / 256;
-  static_assert(S::TM * FOURS * 16 <= (int)LDS_BYTES && FOURS % 16 == 0, "half a tile in LDS");
+// Where a thread stores results: four consecutive columns of one row after another, those in bounds (`rows`,
+// `left` columns), rounded once to the nearest, ties to even; `four`: together, as they are whole and aligned.
+// 8-bit integers' sums, exact in 32 bits, are scaled here.  begin(n) comes before any put().
+template <class Out>
+struct ResultColumns {
+  Out* out;                // the tile's first element
+  int64_t ld;
+  int rows, cols;          // of the tile that exist
+  bool four;
+  bool add = false;        // to what is there (fp32)
+  const float* row_scales = nullptr;
+  const float* col_scales = nullptr;
+
+  struct Held { f32x4 old; float scale; };   // what a put() needs from memory, asked for before
+  Out* at = nullptr;
+  int left = 0;
+  f32x4 by = {1.f, 1.f, 1.f, 1.f};
+
+  __device__ __forceinline__ void begin(int n) {
+    at = out + n;
+    left = cols - n;
+    if (col_scales && left > 0)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) by[c] = col_scales[n + min(c, left - 1)];
+  }
+  __device__ __forceinline__ Held hold(int m) const {
+    Held h = {{0.f, 0.f, 0.f, 0.f}, 1.f};
+    if (m < rows && left > 0) {
+      if (row_scales) h.scale = row_scales[m];
+      if (std::is_same<Out, float>::value && add)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) h.old[c] = c < left ? (float)at[m * ld + c] : 0.f;
+    }
+    return h;
+  }
+  template <class Acc>
+  __device__ __forceinline__ void put(int m, Acc sums, const Held& h) const {
+    if (m >= rows || left <= 0) return;
+    f32x4 v;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = (float)sums[c];
+    if (row_scales)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[c] = v[c] * h.scale * by[c];
+    if (std::is_same<Out, float>::value && add) v += h.old;
+    Out* const to = at + m * ld;
+    if (four) {
+      typedef Out o4 __attribute__((ext_vector_type(4)));
+      *reinterpret_cast<o4*>(to) = __builtin_convertvector(v, o4);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (c < left) to[c] = (Out)v[c];
+    }
+  }
+};
+
+// The tile's results, half of its columns after the other through LDS (free of slabs by then), to `out`, whose
+// lanes then follow each other along a row; with `mirror`, also turned over to `turned`.  Stores straight from
+// the accumulators write pieces of 64 bytes, and their code, as long as there are accumulators and run through
+// once, is fetched more slowly than it runs.  Eight rows are read from LDS before they are stored: one at a time
+// took 350 clocks each.
+template <class S, class Acc, class Columns>
+__device__ __forceinline__ void tile_results(const Acc (&acc)[S::MI][S::NJ], uint8_t* smem, Columns out, bool mirror,
+                                             Columns turned) {
+  constexpr int FOURS = S::TN / 8, STEP = 256 / FOURS, kTimes = S::TM / STEP, kAtOnce = 8;
+  static_assert(S::TM * FOURS * 16 <= (int)LDS_BYTES && FOURS % 16 == 0 && kTimes % kAtOnce == 0, "half a tile in LDS");
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   Acc* const part = reinterpret_cast<Acc*>(smem);
 #pragma unroll 1
@@ -321,41 +378,43 @@ __device__ __forceinline__ void tile_results(const Acc (&acc)[S::MI][S::NJ], uin
 #pragma unroll
         for (int j = 0; j < S::NJ; ++j)
           part[result_place<S>((wave >> 1) * (S::TM / 2) + i * 16 + (lane & 15), j * 4 + (lane >> 4))] = acc[i][j];
+    const int c = tid % FOURS;
+    out.begin(h * (S::TN / 2) + 4 * c);
     __syncthreads();
-#pragma unroll 4
-    for (int k = 0; k < kTimes; ++k) {
-      const int f = k * 256 + tid, m = f / FOURS, c = f % FOURS;
-      store(m, h * (S::TN / 2) + 4 * c, part[result_place<S>(m, c)]);
-    }
-    if (mirror)
 #pragma unroll 1
-      for (int k = 0; k < kTimes / 4; ++k) {   // blocks of 4 x 4, neighbours along a transposed row
-        const int f = k * 256 + tid, m = f % (S::TM / 4) * 4, c = f / (S::TM / 4);
-        Acc v[4];
+    for (int m = tid / FOURS; m < S::TM; m += kAtOnce * STEP) {
+      Acc v[kAtOnce];
+      typename Columns::Held held[kAtOnce];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = part[result_place<S>(m + r, c)];
+      for (int u = 0; u < kAtOnce; ++u) v[u] = part[result_place<S>(m + u * STEP, c)];
 #pragma unroll
-        for (int n = 0; n < 4; ++n) store_mirror(h * (S::TN / 2) + 4 * c + n, m, Acc{v[0][n], v[1][n], v[2][n], v[3][n]});
+      for (int u = 0; u < kAtOnce; ++u) held[u] = out.hold(m + u * STEP);
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) out.put(m + u * STEP, v[u], held[u]);
+    }
+    if (mirror) {   // blocks of 4 x 4, neighbours along a transposed row
+      const int m = tid % (S::TM / 4) * 4;
+      turned.begin(m);
+#pragma unroll 1
+      for (int b = tid / (S::TM / 4); b < FOURS; b += 2 * (1024 / S::TM)) {
+        Acc v[2][4];
+        typename Columns::Held held[2][4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[u][r] = part[result_place<S>(m + r, b + u * (1024 / S::TM))];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int n = 0; n < 4; ++n) held[u][n] = turned.hold(h * (S::TN / 2) + 4 * (b + u * (1024 / S::TM)) + n);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int n = 0; n < 4; ++n)
+            turned.put(h * (S::TN / 2) + 4 * (b + u * (1024 / S::TM)) + n, Acc{v[u][0][n], v[u][1][n], v[u][2][n], v[u][3][n]},
+                       held[u][n]);
       }
-  }
-}
-
-// Four consecutive output elements, together where `four` says that they are whole and aligned.
-__device__ __forceinline__ void store_four(void* out, int dtype, int64_t at, f32x4 v, int count, bool four) {
-  if (!four) {
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-      if (c < count) store_out(out, dtype, at + c, v[c]);
-    return;
-  }
-  if (dtype == GSQ_DT_FP32) {
-    *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = v;
-  } else if (dtype == GSQ_DT_BF16) {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(out) + at) = __builtin_convertvector(v, bf16x4);
-  } else {
-    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<f16x4*>(static_cast<_Float16*>(out) + at) = __builtin_convertvector(v, f16x4);
+    }
   }
 }
 
