@@ -117,10 +117,9 @@ __device__ __forceinline__ ResultColumns<Out> sum_columns(const ProductArgs& p, 
 
 // One tile of a sum over a group's rows: out[m0 .., n0 ..] (+)= sum_r a[r, m] b[r, n], and with `mirror` its
 // transpose too.
-template <class T, class Out>
+template <class T, class Out, class S>
 __device__ __forceinline__ void sum_tile(const ProductArgs& p, int e, int m0, int n0, bool mirror, uint8_t* smem) {
   using E = typename T::elem;
-  using S = Whole;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int64_t first, end;
   group_rows(p.rows, e, first, end);
@@ -178,11 +177,11 @@ __device__ __forceinline__ bool find_sum_tile(const ProductArgs& p, int size, bo
   return true;
 }
 
-template <class T, class Out, bool kGram>
-__global__ __launch_bounds__(256, 1) void k_sums_tile(ProductArgs p) {
+template <class T, class Out, bool kGram, class S>
+__global__ __launch_bounds__(256, S::LDS > LDS_BYTES / 2 ? 1 : 2) void k_sums_tile(ProductArgs p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   int e, m0, n0;
-  if (find_sum_tile(p, Whole::TM, kGram, e, m0, n0)) sum_tile<T, Out>(p, e, m0, n0, kGram && m0 != n0, smem);
+  if (find_sum_tile(p, S::TM, kGram, e, m0, n0)) sum_tile<T, Out, S>(p, e, m0, n0, kGram && m0 != n0, smem);
 }
 
 template <class T, class Out, bool kGram, int S, bool kLoose>
@@ -337,20 +336,30 @@ hipError_t launch_sums(ProductArgs p, hipStream_t s) {
     return p.rows.groups * (kGram ? (tn + 1) / 2 * (tn + 1) : tm * tn);
   };
   const bool tight = p.O % 8 == 0 && p.I % 8 == 0 && aligned16(p.a) && aligned16(p.b);
-  // Whole workgroups on 256 x 256 tiles, or wavefronts that share the sum of 64 x 64 or 32 x 32 ones: the cheapest
-  // by a tile's start and slabs, fitted to dW of one group (us, 256 | 64 | 32): 256 x 256 from 4096 rows 96 | 14 |
-  // 8, 16384 rows 318 | 49 | 42; 1024 x 1024 from 4096 rows 95 | 19 | 38; 2048 x 2048 from 256 rows 21 | 12 | 14,
-  // 16384 rows 318 | 304 | 850; 4096 x 4096 from 256 rows 27 | 38 | 46, 4096 rows 113 | 235 | 514; 8192 x 8192 from
-  // 16 rows 82 | 54 | 54, 256 rows 104 | 138 | 170.  H stores most tiles twice.
+  // Whole workgroups on 256 x 256 or 128 x 128 tiles, or wavefronts that share the sum of 64 x 64 or 32 x 32 ones:
+  // the cheapest by a tile's start and slabs, fitted to dW of one group (us, 256 | 128 | 64 | 32):
+  //   256 x 256: 4096 rows 96 | - | 14 | 8; 16384 rows 318 | - | 49 | 42
+  //   1024 x 1024: 4096 rows 95 | 34 | 19 | 38; 16384 rows 319 | 121 | 62 | 177
+  //   2048 x 2048: 256 rows 21 | 8 | 12 | 14; 4096 rows 96 | 42 | 61 | 137; 16384 rows 318 | 133 | 304 | 850
+  //   4096 x 4096: 64 rows - | 17 | 18 | -; 256 rows 21 | 19 | 38 | 46; 4096 rows 105 | 120 | 235 | 514; 16384 rows
+  //     401 | 527 | 1451 | -
+  //   8192 x 8192: 256 rows 72 | 66 | 138 | 170; 4096 rows 432 | 475 | 883 | 2120; 16384 rows 1607 | 2516 | - | -
+  // and H, which stores most tiles twice: 4096 x 4096 from 1024 rows 57 | 39 | 57 | 83, 8192 x 8192 from 64 rows
+  // - | 59 | 51 | -, 1024 rows 156 | 106 | 202 | 306, 16384 rows 1093 | 1857 | - | -.
   const double slabs = (double)p.rows.rows / 64 / p.rows.groups;
   const auto cost = [&](int64_t tile, double start, double more_start, double alone, double full) {
     const double rounds = count(tile) / 256.0, load = std::min(1.0, rounds);
-    return std::max(1.0, p.rows.groups == 1 ? std::ceil(rounds) : rounds) *
-           (start + more_start * load + (slabs + 0.5) * (alone + (full - alone) * load));
+    const double whole = p.rows.groups == 1 && tile != Quarter::TM ? std::ceil(rounds) : rounds;
+    return std::max(1.0, whole) * (start + more_start * load + (slabs + 0.5) * (alone + (full - alone) * load));
   };
-  const double us_large = cost(Whole::TM, kGram ? 20 : 12, kGram ? 12 : 7, 1.2, 1.4);
-  const double us_small = cost(64, kGram ? 1.4 : 0.7, 0, 0.17, 0.23), us_tiny = cost(32, kGram ? 0.3 : 0.15, 0, 0.08, 0.14);
-  if (tight && us_large < std::min(us_small, us_tiny)) return launch_ring<k_sums_tile<T, Out, kGram>>(count(Whole::TM), s, p);
+  const double far = slabs > 100 ? 1.25 : 1;   // what the L2 holds of a long sum's operands no longer serves small tiles
+  const double us_whole = cost(Whole::TM, kGram ? 20 : 9, kGram ? 12 : 3.5, 1.2, kGram ? 1.35 : 1.5);
+  const double us_quarter = cost(Quarter::TM, kGram ? 6.5 : 2, 0, 0.45 * far, 0.5 * far);
+  const double us_64 = cost(64, kGram ? 1.4 : 0.7, 0, 0.17, 0.23), us_32 = cost(32, kGram ? 0.3 : 0.15, 0, 0.08, 0.14);
+  if (tight && std::min(us_whole, us_quarter) < std::min(us_64, us_32))
+    return us_whole < us_quarter
+               ? launch_lds<k_sums_tile<T, Out, kGram, Whole>>(count(Whole::TM), 256, Whole::LDS, s, p)
+               : launch_lds<k_sums_tile<T, Out, kGram, Quarter>>(count(Quarter::TM), 256, Quarter::LDS, s, p);
   const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(kSplitWaves, (p.rows.rows + 63) / 64));
   const auto launch = [&](auto size, auto loose) {
     constexpr int S = decltype(size)::value;
@@ -359,7 +368,7 @@ hipError_t launch_sums(ProductArgs p, hipStream_t s) {
   };
   using Is64 = std::integral_constant<int, 64>;
   using Is32 = std::integral_constant<int, 32>;
-  if (us_tiny < us_small) return tight ? launch(Is32{}, std::false_type{}) : launch(Is32{}, std::true_type{});
+  if (us_32 < us_64) return tight ? launch(Is32{}, std::false_type{}) : launch(Is32{}, std::true_type{});
   return tight ? launch(Is64{}, std::false_type{}) : launch(Is64{}, std::true_type{});
 }
 

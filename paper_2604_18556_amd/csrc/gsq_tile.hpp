@@ -29,7 +29,8 @@ struct TileShape {
   static constexpr int B_BASE = A_STAGES * A_SLAB;
   static constexpr int A_LOADS = TM / 32, B_LOADS = TN / 32;   // 1 KB loads per wavefront and slab
   static constexpr int MI = TM / 32, NJ = TN / 32;             // 16 x 16 blocks per wavefront
-  static_assert(B_BASE + B_STAGES * B_SLAB <= (int)LDS_BYTES, "the ring fits the LDS");
+  static constexpr size_t LDS = B_BASE + B_STAGES * B_SLAB;
+  static_assert(LDS <= LDS_BYTES, "the ring fits the LDS");
 };
 
 // One block's product: B's columns are the instruction's rows, so that a lane's four results are four
@@ -423,6 +424,8 @@ __device__ __forceinline__ void tile_results(const Acc (&acc)[S::MI][S::NJ], uin
 using Whole = TileShape<256, 256, 2>;
 using Half = TileShape<128, 256, 3>;
 using Low = TileShape<64, 256, 3>;
+// Two of these share a CU: one's loads and stores pass while the other multiplies.
+using Quarter = TileShape<128, 128, 2>;
 
 // The tile of y or dx that this workgroup has: up to `height` rows of one group, 256 columns.
 struct RowsTile {
