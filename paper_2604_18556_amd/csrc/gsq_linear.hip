@@ -423,7 +423,7 @@ template <class T, int BITS, bool kFine, class S>
 __device__ __forceinline__ void packed_tile(const PackedLayer& L, const typename T::elem* x, typename T::elem* y,
                                             const RowsTile& at, int vector_out, uint8_t* smem) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const SlabAlong<S::TM, S::TM / 32, true> a(x + at.first * L.I, (int64_t)L.I * 2, at.ms, wave, lane);
+  SlabAlong<S::TM, S::TM / 32, true> a(x + at.first * L.I, (int64_t)L.I * 2, at.ms, wave, lane);
   SlabPacked<T, BITS, kFine, S::TN> b(L, at.group, at.n0, wave, lane);
   typename T::acc acc[S::MI][S::NJ];
   tile_ring<T, S>(a, b, (L.I + 63) / 64, acc, smem);
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(256, 1) void k_packed_tile(PackedLayer L, GroupRows
                                                         typename T::elem* __restrict__ y, int height, int vector_out) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   RowsTile at;
-  if (!find_rows_tile(rows, height, L.O, at)) return;
+  if (!find_rows_tile(rows, height, Whole::TN, L.O, at)) return;
   if (at.ms > Half::TM)
     packed_tile<T, BITS, kFine, Whole>(L, x, y, at, vector_out, smem);
   else if (at.ms > Low::TM)

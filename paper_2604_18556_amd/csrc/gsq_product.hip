@@ -24,7 +24,7 @@ __device__ __forceinline__ ResultColumns<typename T::out> row_columns(const Prod
 }
 
 // One tile of y or dx.
-template <class T, int kForm, class S>
+template <class T, int kForm, class S, bool kLoose = false>
 __device__ __forceinline__ void rows_tile(const ProductArgs& p, const RowsTile& at, uint8_t* smem) {
   const int64_t first = at.first;
   const int ms = at.ms, n0 = at.n0;
@@ -33,14 +33,26 @@ __device__ __forceinline__ void rows_tile(const ProductArgs& p, const RowsTile& 
   const int ks = kForm == kForward ? p.I : p.O, ns = kForm == kForward ? p.O : p.I;
   const int nk = (int)(((int64_t)ks * sizeof(E) + ROW_BYTES - 1) / ROW_BYTES);
   const E* w = static_cast<const E*>(p.b) + (int64_t)at.group * p.O * p.I;
-  const SlabAlong<S::TM> a(static_cast<const E*>(p.a) + first * ks, (int64_t)ks * sizeof(E), ms, wave, lane);
+  const E* x = static_cast<const E*>(p.a) + first * ks;
   typename T::acc acc[S::MI][S::NJ];
-  if constexpr (kForm == kForward) {
-    SlabAlong<S::TN> b(w + (int64_t)n0 * ks, (int64_t)ks * sizeof(E), ns - n0, wave, lane);
-    tile_ring<T, S>(a, b, nk, acc, smem);
+  if constexpr (kLoose) {
+    RingLoose<LooseAlong<E, S::TM, S::TM / 32>> a(x, ks, ms, ks, wave);
+    if constexpr (kForm == kForward) {
+      RingLoose<LooseAlong<E, S::TN, S::TN / 32>> b(w + (int64_t)n0 * ks, ks, ns - n0, ks, wave);
+      tile_ring<T, S>(a, b, nk, acc, smem);
+    } else {
+      RingLoose<LooseAcross<E, S::TN, S::TN / 32>> b(w + n0, ns, ns - n0, ks, wave);
+      tile_ring<T, S>(a, b, nk, acc, smem);
+    }
   } else {
-    SlabAcross<S::TN> b(w + n0, (int64_t)ns * sizeof(E), ns - n0, ks, wave, lane);
-    tile_ring<T, S>(a, b, nk, acc, smem);
+    SlabAlong<S::TM> a(x, (int64_t)ks * sizeof(E), ms, wave, lane);
+    if constexpr (kForm == kForward) {
+      SlabAlong<S::TN> b(w + (int64_t)n0 * ks, (int64_t)ks * sizeof(E), ns - n0, wave, lane);
+      tile_ring<T, S>(a, b, nk, acc, smem);
+    } else {
+      SlabAcross<S::TN> b(w + n0, (int64_t)ns * sizeof(E), ns - n0, ks, wave, lane);
+      tile_ring<T, S>(a, b, nk, acc, smem);
+    }
   }
   const auto out = row_columns<T>(p, at.group, first, ms, ns, n0);
   tile_results<S>(acc, smem, out, false, out);
@@ -51,13 +63,22 @@ template <class T, int kForm>
 __global__ __launch_bounds__(256, 1) void k_rows_tile(ProductArgs p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   RowsTile at;
-  if (!find_rows_tile(p.rows, p.height, kForm == kForward ? p.O : p.I, at)) return;
+  if (!find_rows_tile(p.rows, p.height, Whole::TN, kForm == kForward ? p.O : p.I, at)) return;
   if (at.ms > Half::TM)
     rows_tile<T, kForm, Whole>(p, at, smem);
   else if (at.ms > Low::TM)
     rows_tile<T, kForm, Half>(p, at, smem);
   else
     rows_tile<T, kForm, Low>(p, at, smem);
+}
+
+// From any addresses, by way of registers: a quarter tile, two to a CU, so that one's waits are the other's work.
+template <class T, int kForm>
+__global__ __launch_bounds__(256, 2) void k_rows_loose(ProductArgs p) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  RowsTile at;
+  if (find_rows_tile(p.rows, Quarter::TM, Quarter::TN, kForm == kForward ? p.O : p.I, at))
+    rows_tile<T, kForm, Quarter, true>(p, at, smem);
 }
 
 // The same from small tiles: panels of TM rows (of which one of 16 or fewer is taken as 16), TN columns.
@@ -72,12 +93,12 @@ __device__ __forceinline__ void rows_split(const ProductArgs& p, int group, int6
   const E* x = static_cast<const E*>(p.a) + first * ks;
   const auto out = row_columns<T>(p, group, first, ms, ns, n0);
   if constexpr (kLoose) {
-    LooseAlong<E, TM> a(x, ks, ms, ks);
+    LooseAlong<E, TM> a(x, ks, ms, ks, 0);
     if constexpr (kForm == kForward) {
-      LooseAlong<E, TN> b(w + (int64_t)n0 * ks, ks, ns - n0, ks);
+      LooseAlong<E, TN> b(w + (int64_t)n0 * ks, ks, ns - n0, ks, 0);
       tile_split<T, TM, TN>(a, b, nk, smem, out, false, out);
     } else {
-      LooseAcross<E, TN> b(w + n0, ns, ns - n0, ks);
+      LooseAcross<E, TN> b(w + n0, ns, ns - n0, ks, 0);
       tile_split<T, TM, TN>(a, b, nk, smem, out, false, out);
     }
   } else {
@@ -117,18 +138,23 @@ __device__ __forceinline__ ResultColumns<Out> sum_columns(const ProductArgs& p, 
 
 // One tile of a sum over a group's rows: out[m0 .., n0 ..] (+)= sum_r a[r, m] b[r, n], and with `mirror` its
 // transpose too.
-template <class T, class Out, class S>
+template <class T, class Out, class S, bool kLoose>
 __device__ __forceinline__ void sum_tile(const ProductArgs& p, int e, int m0, int n0, bool mirror, uint8_t* smem) {
   using E = typename T::elem;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int64_t first, end;
   group_rows(p.rows, e, first, end);
   const int ks = (int)(end - first), nk = (ks + kSlabRows - 1) / kSlabRows;
-  // a group without rows reads zeros only: its addresses are not used
-  const SlabAcross<S::TM> a(static_cast<const E*>(p.a) + first * p.O + m0, (int64_t)p.O * 2, p.O - m0, ks, wave, lane);
-  SlabAcross<S::TN> b(static_cast<const E*>(p.b) + first * p.I + n0, (int64_t)p.I * 2, p.I - n0, ks, wave, lane);
+  const E* dy = static_cast<const E*>(p.a) + first * p.O + m0;   // without rows, only zeros are read
+  const E* x = static_cast<const E*>(p.b) + first * p.I + n0;
   typename T::acc acc[S::MI][S::NJ];
-  tile_ring<T, S>(a, b, nk, acc, smem);
+  if constexpr (kLoose) {
+    RingLoose<LooseAcross<E, S::TM, S::TM / 32>> a(dy, p.O, p.O - m0, ks, wave), b(x, p.I, p.I - n0, ks, wave);
+    tile_ring<T, S>(a, b, nk, acc, smem);
+  } else {
+    SlabAcross<S::TM> a(dy, (int64_t)p.O * 2, p.O - m0, ks, wave, lane), b(x, (int64_t)p.I * 2, p.I - n0, ks, wave, lane);
+    tile_ring<T, S>(a, b, nk, acc, smem);
+  }
   tile_results<S>(acc, smem, sum_columns<Out>(p, e, m0, n0), mirror, sum_columns<Out>(p, e, n0, m0));
 }
 
@@ -144,7 +170,7 @@ __device__ __forceinline__ void sum_split(const ProductArgs& p, int e, int m0, i
   const E* x = static_cast<const E*>(p.b) + first * p.I + n0;
   const auto out = sum_columns<Out>(p, e, m0, n0), turned = sum_columns<Out>(p, e, n0, m0);
   if constexpr (kLoose) {
-    LooseAcross<E, S> a(dy, p.O, p.O - m0, ks), b(x, p.I, p.I - n0, ks);
+    LooseAcross<E, S> a(dy, p.O, p.O - m0, ks, 0), b(x, p.I, p.I - n0, ks, 0);
     tile_split<T, S, S>(a, b, nk, smem, out, mirror, turned);
   } else {
     Copied<SlabAcross<S, S / 8>> a(dy, (int64_t)p.O * 2, p.O - m0, ks, 0, lane), b(x, (int64_t)p.I * 2, p.I - n0, ks, 0, lane);
@@ -177,11 +203,11 @@ __device__ __forceinline__ bool find_sum_tile(const ProductArgs& p, int size, bo
   return true;
 }
 
-template <class T, class Out, bool kGram, class S>
+template <class T, class Out, bool kGram, class S, bool kLoose>
 __global__ __launch_bounds__(256, S::LDS > LDS_BYTES / 2 ? 1 : 2) void k_sums_tile(ProductArgs p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   int e, m0, n0;
-  if (find_sum_tile(p, S::TM, kGram, e, m0, n0)) sum_tile<T, Out, S>(p, e, m0, n0, kGram && m0 != n0, smem);
+  if (find_sum_tile(p, S::TM, kGram, e, m0, n0)) sum_tile<T, Out, S, kLoose>(p, e, m0, n0, kGram && m0 != n0, smem);
 }
 
 template <class T, class Out, bool kGram, int S, bool kLoose>
@@ -319,10 +345,17 @@ hipError_t launch_rows(ProductArgs p, hipStream_t s) {
   const TileCost large[] = {{256, 256, 3, 1.15 * kMore, 1.6 * kMore}, {128, 256, 2, 0.7 * kMore, 0.95 * kMore},
                             {64, 256, 1.5, 0.43 * kMore, 0.72 * kMore}};
   const TileCost small[] = {{64, 64, 1, 0.165, 0.22}, {64, 16, 1, 0.1, 0.115}, {16, 64, 1, 0.06, 0.1}, {16, 16, 0.5, 0.02, 0.055}};
+  const TileCost loose[] = {{128, 128, 2, 0.6, 0.7}};
   double best = 1e30;
   RowsPlan plan = cheapest(p.rows, ns, slabs, small, true, best, RowsPlan{});
   if (tight) plan = cheapest(p.rows, ns, slabs, large, false, best, plan);
-  if (!tight) return launch_rows_split<T, kForm, true>(p, plan, s);
+  if (!tight) {
+    const char* ev = getenv("GSQ_Q");
+    if (!ev) plan = cheapest(p.rows, ns, slabs, loose, false, best, plan); else plan.split = ev[0] == '0';
+    if (plan.split) return launch_rows_split<T, kForm, true>(p, plan, s);
+    return launch_lds<k_rows_loose<T, kForm>>(most_panels(p.rows, Quarter::TM) * tiles_of(ns, Quarter::TN), 256,
+                                              Quarter::LDS, s, p);
+  }
   if (plan.split) return launch_rows_split<T, kForm, false>(p, plan, s);
   p.height = plan.height;
   return launch_ring<k_rows_tile<T, kForm>>(most_panels(p.rows, p.height) * tiles_of(ns, Whole::TN), s, p);
@@ -353,13 +386,14 @@ hipError_t launch_sums(ProductArgs p, hipStream_t s) {
     return std::max(1.0, whole) * (start + more_start * load + (slabs + 0.5) * (alone + (full - alone) * load));
   };
   const double far = slabs > 100 ? 1.25 : 1;   // what the L2 holds of a long sum's operands no longer serves small tiles
-  const double us_whole = cost(Whole::TM, kGram ? 20 : 9, kGram ? 12 : 3.5, 1.2, kGram ? 1.35 : 1.5);
+  const double us_whole = !tight ? 1e30 : cost(Whole::TM, kGram ? 20 : 9, kGram ? 12 : 3.5, 1.2, kGram ? 1.35 : 1.5);
   const double us_quarter = cost(Quarter::TM, kGram ? 6.5 : 2, 0, 0.45 * far, 0.5 * far);
   const double us_64 = cost(64, kGram ? 1.4 : 0.7, 0, 0.17, 0.23), us_32 = cost(32, kGram ? 0.3 : 0.15, 0, 0.08, 0.14);
-  if (tight && std::min(us_whole, us_quarter) < std::min(us_64, us_32))
-    return us_whole < us_quarter
-               ? launch_lds<k_sums_tile<T, Out, kGram, Whole>>(count(Whole::TM), 256, Whole::LDS, s, p)
-               : launch_lds<k_sums_tile<T, Out, kGram, Quarter>>(count(Quarter::TM), 256, Quarter::LDS, s, p);
+  if (us_whole < std::min(us_quarter, std::min(us_64, us_32)))
+    return launch_lds<k_sums_tile<T, Out, kGram, Whole, false>>(count(Whole::TM), 256, Whole::LDS, s, p);
+  if (us_quarter < std::min(us_64, us_32))
+    return tight ? launch_lds<k_sums_tile<T, Out, kGram, Quarter, false>>(count(Quarter::TM), 256, Quarter::LDS, s, p)
+                 : launch_lds<k_sums_tile<T, Out, kGram, Quarter, true>>(count(Quarter::TM), 256, Quarter::LDS, s, p);
   const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(kSplitWaves, (p.rows.rows + 63) / 64));
   const auto launch = [&](auto size, auto loose) {
     constexpr int S = decltype(size)::value;

@@ -43,64 +43,81 @@ __device__ __forceinline__ i32x4 load_chunk(const E* p, int n) {
   return v;
 }
 
-// Operands as in gsq_tile.hpp, for one wavefront, by way of registers and from any address: fetch() reads slab
-// k, commit() writes it to LDS.
-template <class E, int ROWS>
+// Operands as in gsq_tile.hpp by way of registers, from any address: fetch() reads a wavefront's part of slab k,
+// commit() writes it, or piece j of it, to LDS.
+template <class E, int ROWS, int LOADS_ = ROWS / 8>
 struct LooseAlong {
-  static constexpr int LOADS = ROWS / 8, PER = 16 / (int)sizeof(E);
+  static constexpr int LOADS = LOADS_, PER = 16 / (int)sizeof(E);
   const E* base;
   int64_t ld;
-  int rows, ks;
+  int rows, ks, row0;
   i32x4 held[LOADS];
 
-  __device__ __forceinline__ LooseAlong(const E* first, int64_t ld_, int rows_, int ks_)
-      : base(first), ld(ld_), rows(rows_), ks(ks_) {}
+  __device__ __forceinline__ LooseAlong(const E* first, int64_t ld_, int rows_, int ks_, int wave)
+      : base(first), ld(ld_), rows(rows_), ks(ks_), row0(wave * LOADS * 8) {}
   __device__ __forceinline__ void fetch(int k, uint8_t*) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-      const int row = j * 8 + (lane >> 3), at = (k * 8 + ((lane & 7) ^ swz(row))) * PER;
+      const int row = row0 + j * 8 + (lane >> 3), at = (k * 8 + ((lane & 7) ^ swz(row))) * PER;
       held[j] = load_chunk(base + min(row, rows - 1) * ld + at, ks - at);
     }
   }
+  __device__ __forceinline__ void commit(uint8_t* lds, int j) const {
+    *reinterpret_cast<i32x4*>(lds + j * 1024 + (threadIdx.x & 63) * 16) = held[j];
+  }
   __device__ __forceinline__ void commit(uint8_t* lds) const {
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j)
-      *reinterpret_cast<i32x4*>(lds + j * 1024 + (threadIdx.x & 63) * 16) = held[j];
+    for (int j = 0; j < LOADS; ++j) commit(lds, j);
   }
   static __device__ __forceinline__ i32x4 frag(const uint8_t* slab, int row0, int half, int lane) {
     return read_frag<i32x4>(slab, row0 + (lane & 15), half * 4 + (lane >> 4));
   }
 };
 
-template <class E, int COLS>
+template <class E, int COLS, int LOADS_ = COLS / 8>
 struct LooseAcross {
-  using Tight = SlabAcross<COLS, COLS / 8>;
-  static constexpr int LOADS = COLS / 8;
+  using Tight = SlabAcross<COLS, LOADS_>;
+  static constexpr int LOADS = LOADS_;
   const E* base;
   int64_t ld;
-  int cols, ks;
+  int cols, ks, at0;
   i32x4 held[LOADS];
 
-  __device__ __forceinline__ LooseAcross(const E* first, int64_t ld_, int cols_, int ks_)
-      : base(first), ld(ld_), cols(cols_), ks(ks_) {}
+  __device__ __forceinline__ LooseAcross(const E* first, int64_t ld_, int cols_, int ks_, int wave)
+      : base(first), ld(ld_), cols(cols_), ks(ks_), at0(wave * LOADS * 64) {}
   __device__ __forceinline__ void fetch(int k, uint8_t*) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
       int row, chunk;
-      Tight::place(j * 64 + lane, row, chunk);
+      Tight::place(at0 + j * 64 + lane, row, chunk);
       const int64_t r = (int64_t)k * kSlabRows + row;
       held[j] = load_chunk(base + r * ld + chunk * 8, r < ks ? cols - chunk * 8 : 0);
     }
   }
+  __device__ __forceinline__ void commit(uint8_t* lds, int j) const {
+    *reinterpret_cast<i32x4*>(lds + j * 1024 + (threadIdx.x & 63) * 16) = held[j];
+  }
   __device__ __forceinline__ void commit(uint8_t* lds) const {
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j)
-      *reinterpret_cast<i32x4*>(lds + j * 1024 + (threadIdx.x & 63) * 16) = held[j];
+    for (int j = 0; j < LOADS; ++j) commit(lds, j);
   }
   static __device__ __forceinline__ i32x4 frag(const uint8_t* slab, int col0, int half, int lane) {
     return Tight::frag(slab, col0, half, lane);
+  }
+};
+
+// One of them in the ring of whole workgroups.
+template <class Loose>
+struct RingLoose : Loose {
+  using Loose::Loose;
+  static constexpr bool kCopied = false;
+  __device__ __forceinline__ void prefetch(int k) { Loose::fetch(k, nullptr); }
+  template <bool kEnd>
+  __device__ __forceinline__ void load(int k, int j, uint8_t* lds) {
+    Loose::commit(lds, j);
+    if (j == Loose::LOADS - 1) prefetch(k + 1);
   }
 };
 

@@ -195,10 +195,11 @@ __device__ __forceinline__ void static_for(F f) {
 // reads of the next half and slab loads are issued between the products, a load after every two reads.
 // Blocks are walked back and forth: one operand of each product is the last one's.
 //
-// B need not be copied (!B::kCopied): its load(k, j) then writes its part of slab k itself, from what its
-// prefetch() and the calls for slab k - 1 have fetched into registers.
+// An operand need not be copied (!kCopied): its load(k, j, place) then writes 1 KB of slab k at that place (in
+// SlabPacked's case relative to the wavefront's part), from what its prefetch() and the calls for slab k - 1 have
+// fetched into registers.
 template <class T, class S, class A, class B>
-__device__ __forceinline__ void tile_ring(const A& a, B& b, int nk,
+__device__ __forceinline__ void tile_ring(A& a, B& b, int nk,
                                           typename T::acc (&acc)[S::MI][S::NJ], uint8_t* smem) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -246,6 +247,7 @@ __device__ __forceinline__ void tile_ring(const A& a, B& b, int nk,
 
   // p: first half of the current slab; q: second half
   i32x4 pa[S::MI], pb[S::NJ], qa[S::MI], qb[S::NJ];
+  if constexpr (!A::kCopied) a.prefetch(0);
   if constexpr (!B::kCopied) b.prefetch(0);
 #pragma unroll
   for (int k = 0; k < S::AHEAD; ++k) {
@@ -254,9 +256,9 @@ __device__ __forceinline__ void tile_ring(const A& a, B& b, int nk,
 #pragma unroll
     for (int j = 0; j < S::B_LOADS; ++j) b.template load<true>(k, j, b_wave + k * S::B_SLAB);
   }
-  // copies of a slab; what B fetches besides makes the waits longer than need be, never shorter
-  constexpr int kSlabLoads = S::A_LOADS + (B::kCopied ? S::B_LOADS : 0);
-  wait_vm<(S::AHEAD - 1) * kSlabLoads>();
+  // copies of a slab; what is fetched besides makes the waits longer than need be, never shorter
+  constexpr int kACopies = A::kCopied ? S::A_LOADS : 0, kSlabLoads = kACopies + (B::kCopied ? S::B_LOADS : 0);
+  if constexpr (kSlabLoads > 0) wait_vm<(S::AHEAD - 1) * kSlabLoads>();
   slab_barrier();
 #pragma unroll
   for (int n = 0; n < kReads; ++n) read(pa, pb, 0, 0, n);
@@ -271,7 +273,7 @@ __device__ __forceinline__ void tile_ring(const A& a, B& b, int nk,
     __builtin_amdgcn_sched_barrier(0);   // every product of this half is issued before the wait
     // slab kt + 1 has landed (later ones, of kt + AHEAD only A's, may be in flight), and every
     // wavefront has read slab kt
-    wait_vm<(S::AHEAD - 2) * kSlabLoads + S::A_LOADS>();
+    if constexpr (kSlabLoads > 0) wait_vm<(S::AHEAD - 2) * kSlabLoads + kACopies>();
     slab_barrier();
     half_slab(qa, qb, kReads, S::B_LOADS, [&](int n) { read(pa, pb, kt + 1, 0, n); },
               [&](int j) {
@@ -285,7 +287,7 @@ __device__ __forceinline__ void tile_ring(const A& a, B& b, int nk,
   // the last slabs: nothing more to load
   for (; kt < nk - 1; ++kt) {
     half_slab(pa, pb, kReads, 0, [&](int n) { read(qa, qb, kt, 1, n); }, none);
-    wait_vm<0>();
+    if constexpr (kSlabLoads > 0) wait_vm<0>();
     slab_barrier();
     half_slab(qa, qb, kReads, 0, [&](int n) { read(pa, pb, kt + 1, 0, n); }, none);
   }
@@ -427,7 +429,7 @@ using Low = TileShape<64, 256, 3>;
 // Two of these share a CU: one's loads and stores pass while the other multiplies.
 using Quarter = TileShape<128, 128, 2>;
 
-// The tile of y or dx that this workgroup has: up to `height` rows of one group, 256 columns.
+// The tile of y or dx that this workgroup has: up to `height` rows of one group, `width` columns.
 struct RowsTile {
   int group;
   int64_t first;     // its first row
@@ -436,8 +438,8 @@ struct RowsTile {
 
 // Which one: the tiles of a group follow each other, and are spread over the XCDs so that each has a
 // contiguous part of the group's tile order.  False: there are fewer.
-__device__ __forceinline__ bool find_rows_tile(const GroupRows& rows, int height, int cols, RowsTile& t) {
-  const int tiles_n = (cols + Whole::TN - 1) / Whole::TN;
+__device__ __forceinline__ bool find_rows_tile(const GroupRows& rows, int height, int width, int cols, RowsTile& t) {
+  const int tiles_n = (cols + width - 1) / width;
   PanelPlace at;
   if (!find_panel(rows, height, blockIdx.x / (unsigned)tiles_n, at)) return false;
   int tm, tn;
@@ -445,7 +447,7 @@ __device__ __forceinline__ bool find_rows_tile(const GroupRows& rows, int height
   t.group = at.group;
   t.first = at.first + (int64_t)tm * height;
   t.ms = (int)min(at.end - t.first, (int64_t)height);
-  t.n0 = tn * Whole::TN;
+  t.n0 = tn * width;
   return true;
 }
 
