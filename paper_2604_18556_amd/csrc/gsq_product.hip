@@ -344,14 +344,16 @@ hipError_t launch_rows(ProductArgs p, hipStream_t s) {
   constexpr double kMore = T::kDtype < 0 ? 1.4 : 1;
   const TileCost large[] = {{256, 256, 3, 1.15 * kMore, 1.6 * kMore}, {128, 256, 2, 0.7 * kMore, 0.95 * kMore},
                             {64, 256, 1.5, 0.43 * kMore, 0.72 * kMore}};
+  // from any addresses (I 4001, O 8190; 64 x 64 split | 128 x 128): 64 rows 32 | 72, 512 rows 118 | 78, 4096 rows
+  // 866 | 378
+  const TileCost loose[] = {{128, 128, 2, kForm == kForward ? 0.85 : 2.0, kForm == kForward ? 0.75 : 1.05}};
+  const TileCost small_loose[] = {{64, 64, 1, 0.17, 0.42}, {64, 16, 1, 0.1, 0.21}, {16, 64, 1, 0.07, 0.15}, {16, 16, 0.5, 0.025, 0.08}};
   const TileCost small[] = {{64, 64, 1, 0.165, 0.22}, {64, 16, 1, 0.1, 0.115}, {16, 64, 1, 0.06, 0.1}, {16, 16, 0.5, 0.02, 0.055}};
-  const TileCost loose[] = {{128, 128, 2, 0.6, 0.7}};
   double best = 1e30;
-  RowsPlan plan = cheapest(p.rows, ns, slabs, small, true, best, RowsPlan{});
+  RowsPlan plan = cheapest(p.rows, ns, slabs, tight ? small : small_loose, true, best, RowsPlan{});
   if (tight) plan = cheapest(p.rows, ns, slabs, large, false, best, plan);
   if (!tight) {
-    const char* ev = getenv("GSQ_Q");
-    if (!ev) plan = cheapest(p.rows, ns, slabs, loose, false, best, plan); else plan.split = ev[0] == '0';
+    plan = cheapest(p.rows, ns, slabs, loose, false, best, plan);
     if (plan.split) return launch_rows_split<T, kForm, true>(p, plan, s);
     return launch_lds<k_rows_loose<T, kForm>>(most_panels(p.rows, Quarter::TM) * tiles_of(ns, Quarter::TN), 256,
                                               Quarter::LDS, s, p);
