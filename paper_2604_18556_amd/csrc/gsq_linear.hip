@@ -230,96 +230,36 @@ struct LaneCodes {
   }
 };
 
-// ---- up to 16 rows: a workgroup has 16 output channels, its wavefronts take their units in turn, and the
-// partial sums are added in LDS in a fixed order.  Bound by the codes' way from memory: all that a wavefront
-// needs for kFewUnits units, x included, is asked for before the units before them are multiplied.
-constexpr int kFewWaves = 16, kFewUnits = 2;
-
-template <class T, int BITS, bool kFine>
-struct FewOperands {
-  LaneCodes<BITS, kFine> codes[kFewUnits];
-  typename T::frag x[kFewUnits][4];
-
-  __device__ __forceinline__ void load(const PackedLayer& L, int64_t tile, const typename T::elem* row, bool some,
-                                       int kb0, int step) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int u = 0; u < kFewUnits; ++u)   // past the end: the last unit again, not used
-      codes[u].load(L, tile, min(kb0 + u * step, L.blocks - 1), lane);
-#pragma unroll
-    for (int u = 0; u < kFewUnits; ++u) {
-      const int k0 = (kb0 + u * step) * 128 + (lane >> 4) * 32;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        x[u][s] = typename T::frag{};
-        if (some && k0 + 8 * s < L.I) __builtin_memcpy(&x[u][s], row + k0 + 8 * s, 16);
-      }
-    }
-  }
-};
-
-template <class T, int BITS, bool kFine>
-__global__ __launch_bounds__(64 * kFewWaves) void k_packed_few(PackedLayer L, GroupRows rows,
-                                                              const typename T::elem* __restrict__ x,
-                                                              typename T::elem* __restrict__ y) {
-  using E = typename T::elem;
-  __shared__ f32x4 part[kFewWaves * 64];
-  PanelPlace at;
-  if (!find_panel(rows, 16, blockIdx.x / (unsigned)L.tiles, at)) return;
-  // panels of a group share its codes: they are neighbours
-  const int j = (int)(blockIdx.x - at.before * L.tiles), n0 = j / at.panels * 16;
-  const int64_t first = at.first + (int64_t)(j % at.panels) * 16, tile = (int64_t)at.group * L.tiles + n0 / 16;
-  const int ms = (int)min(at.end - first, (int64_t)16);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, g = lane >> 4;
-  const bool some = (lane & 15) < ms;
-  const E* row = x + (first + (some ? lane & 15 : 0)) * L.I;
-  f32x4 acc = {};
-  FewOperands<T, BITS, kFine> now, next;
-  next.load(L, tile, row, some, wave, waves);
-  for (int kb0 = wave; kb0 < L.blocks; kb0 += kFewUnits * waves) {
-    now = next;
-    next.load(L, tile, row, some, kb0 + kFewUnits * waves, waves);
-#pragma unroll
-    for (int u = 0; u < kFewUnits; ++u) {
-      if (kb0 + u * waves >= L.blocks) break;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const WeightTable<T, BITS> table(now.codes[u].scale(L, kFine ? h : 0), L.levels);
-#pragma unroll
-        for (int s = 2 * h; s < 2 * h + 2; ++s) acc = T::mfma(table.frag(now.codes[u].words, s), now.x[u][s], acc);
-      }
-    }
-  }
-  // acc: row of x lane % 16, channels 4 (lane / 16) .. + 3
-  part[threadIdx.x] = acc;
-  __syncthreads();
-  if (wave) return;
-  for (int w = 1; w < waves; ++w) acc += part[w * 64 + lane];
-  if (some)
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-      if (n0 + 4 * g + c < L.O) y[(first + (lane & 15)) * L.O + n0 + 4 * g + c] = (E)acc[c];
-}
-
-// ---- more rows, but too few tiles for whole workgroups: 64 channels and TM rows, the units shared by eight
+// ---- few rows, or too few tiles for whole workgroups: COLS channels and up to 64 rows, the units shared by the
 // wavefronts as tile_split() does it.  x goes through LDS, the weights from the codes to registers.
-constexpr int kSharedCols = 64;
-
-template <class T, int BITS, bool kFine, int TM>
+//
+// At one row bound by the vector units, which take some three instructions for a weight of 3 bits, and by latency:
+// 4096 x 14336 (23 MB) in 11.4 us, 4096 x 4096 in 6.1.  x straight from memory to the fragments, without LDS: 12.8
+// us at one row, and 23 at 16 instead of 13.
+template <class T, int BITS, bool kFine, int COLS, int TM, bool kLoose>
 __device__ __forceinline__ void packed_shared(const PackedLayer& L, const typename T::elem* x, typename T::elem* y,
                                               int group, int64_t first, int ms, int n0, int vector_out, uint8_t* smem) {
-  constexpr int MI = TM / 16, NJ = kSharedCols / 16, A_SLAB = TM * ROW_BYTES, OWN = 2 * A_SLAB;
+  using E = typename T::elem;
+  constexpr int MI = TM / 16, NJ = COLS / 16, A_SLAB = TM * ROW_BYTES, OWN = 2 * A_SLAB;
+  static_assert(TM * COLS * 4 <= OWN, "the sums take the slabs' place");
+  using Slab = std::conditional_t<kLoose, LooseAlong<E, TM>, Copied<SlabAlong<TM, TM / 8>>>;
   const int lane = threadIdx.x & 63, waves = blockDim.x >> 6, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint8_t* const own = smem + wave * OWN;
-  Copied<SlabAlong<TM, TM / 8>> a(x + first * L.I, (int64_t)L.I * 2, ms, 0, lane);
+  const auto slab_of_x = [&] {
+    if constexpr (kLoose)
+      return Slab(x + first * L.I, L.I, ms, L.I, 0);
+    else
+      return Slab(x + first * L.I, (int64_t)L.I * 2, ms, 0, lane);
+  };
+  Slab a[2] = {slab_of_x(), slab_of_x()};   // the two of a unit
   const int64_t tile0 = (int64_t)group * L.tiles;
   int64_t tile[NJ];
   LaneCodes<BITS, kFine> next[NJ];
   f32x4 acc[MI][NJ] = {};
   const auto fetch = [&](int kb) {
-    a.fetch(2 * kb, own);
-    a.fetch(2 * kb + 1, own + A_SLAB);
+    a[0].fetch(2 * kb, own);
+    a[1].fetch(2 * kb + 1, own + A_SLAB);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) next[j].load(L, tile[j], kb, lane);
   };
@@ -327,6 +267,8 @@ __device__ __forceinline__ void packed_shared(const PackedLayer& L, const typena
   for (int j = 0; j < NJ; ++j) tile[j] = tile0 + min(n0 / 16 + j, L.tiles - 1);   // beyond: not stored
   if (wave < L.blocks) fetch(wave);
   for (int kb = wave; kb < L.blocks; kb += waves) {
+    a[0].commit(own);
+    a[1].commit(own + A_SLAB);
     wait_all();
     typename T::frag fa[MI][4];
 #pragma unroll
@@ -352,27 +294,38 @@ __device__ __forceinline__ void packed_shared(const PackedLayer& L, const typena
         }
       }
   }
-  split_sums<TM, kSharedCols>(acc, own);
-  const ResultColumns<typename T::elem> out{y + first * L.O + n0, L.O, ms, L.O - n0, vector_out != 0};
-  store_added<TM, kSharedCols, f32x4>(smem, OWN, min(waves, L.blocks), out, false, out);
+  split_sums<TM, COLS>(acc, own);
+  const ResultColumns<E> out{y + first * L.O + n0, L.O, ms, L.O - n0, vector_out != 0};
+  store_added<TM, COLS, f32x4>(smem, OWN, min(waves, L.blocks), out, false, out);
 }
 
-template <class T, int BITS, bool kFine>
-__global__ __launch_bounds__(64 * kSplitWaves) void k_packed_shared(PackedLayer L, GroupRows rows,
-                                                                   const typename T::elem* __restrict__ x,
-                                                                   typename T::elem* __restrict__ y, int vector_out) {
+// Panels of 64 rows, of which the shorter ones are taken as 32 or 16; with 16 channels, panels of 16.
+constexpr int kFewWaves = 16;
+template <int COLS>
+constexpr int shared_panel() { return COLS == 16 ? 16 : 64; }
+template <int COLS>
+constexpr int shared_waves() { return COLS == 16 ? kFewWaves : kSplitWaves; }
+
+template <class T, int BITS, bool kFine, int COLS, bool kLoose>
+__global__ __launch_bounds__(64 * shared_waves<COLS>()) void k_packed_shared(PackedLayer L, GroupRows rows,
+                                                                            const typename T::elem* __restrict__ x,
+                                                                            typename T::elem* __restrict__ y, int vector_out) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-  const int tiles_n = (L.O + kSharedCols - 1) / kSharedCols;
+  constexpr int TM = shared_panel<COLS>();
+  const int tiles_n = (L.O + COLS - 1) / COLS;
   PanelPlace at;
-  if (!find_panel(rows, 64, blockIdx.x / (unsigned)tiles_n, at)) return;
+  if (!find_panel(rows, TM, blockIdx.x / (unsigned)tiles_n, at)) return;
   int tm, tn;
   tile_at(lin_of((int)(blockIdx.x - at.before * tiles_n), at.panels * tiles_n), at.panels, tiles_n, tm, tn);
-  const int64_t first = at.first + (int64_t)tm * 64;
-  const int ms = (int)min(at.end - first, (int64_t)64);
-  if (ms <= 32)
-    packed_shared<T, BITS, kFine, 32>(L, x, y, at.group, first, ms, tn * kSharedCols, vector_out, smem);
-  else
-    packed_shared<T, BITS, kFine, 64>(L, x, y, at.group, first, ms, tn * kSharedCols, vector_out, smem);
+  const int64_t first = at.first + (int64_t)tm * TM;
+  const int ms = (int)min(at.end - first, (int64_t)TM);
+  if constexpr (COLS == 64) {
+    if (ms > 32)
+      return packed_shared<T, BITS, kFine, COLS, 64, kLoose>(L, x, y, at.group, first, ms, tn * COLS, vector_out, smem);
+    if (ms > 16)
+      return packed_shared<T, BITS, kFine, COLS, 32, kLoose>(L, x, y, at.group, first, ms, tn * COLS, vector_out, smem);
+  }
+  packed_shared<T, BITS, kFine, COLS, 16, kLoose>(L, x, y, at.group, first, ms, tn * COLS, vector_out, smem);
 }
 
 // ---- many rows: tiles as for a dense layer, whose slabs of weights the wavefronts write to LDS from the
@@ -466,21 +419,32 @@ hipError_t launch_unpack_layer(const gsq_config& cfg, const uint8_t* packed, con
 
 namespace {
 
+template <class T, int BITS, bool kFine, int COLS, bool kLoose>
+hipError_t launch_shared(const PackedLayer& L, const GroupRows& rows, const typename T::elem* x, typename T::elem* y,
+                         int vector_out, hipStream_t s) {
+  constexpr int TM = shared_panel<COLS>();
+  const int waves = std::min(shared_waves<COLS>(), L.blocks);
+  return launch_lds<k_packed_shared<T, BITS, kFine, COLS, kLoose>>(most_panels(rows, TM) * tiles_of(L.O, COLS), 64 * waves,
+                                                                   (size_t)waves * 2 * TM * ROW_BYTES, s, L, rows, x, y,
+                                                                   vector_out);
+}
+
 template <class T, int BITS, bool kFine>
 hipError_t launch_packed(const PackedLayer& L, const GroupRows& rows, const void* x, void* y, hipStream_t s) {
   using E = typename T::elem;
-  // Which kernel, by the same reckoning as for dense weights (us at 2 bits; 16 rows and channels | 64 x 64 shared |
-  // panels of 64 | 128 | 256 rows by workgroups):
-  //   I 4096, O 4096: 1 row 6.9 | 10.3 | 52 | - | -; 17 rows 17 | 11; 256 rows - | 17 | 55 | 72 | 96; 2048 rows
-  //     - | 116 | 135 | 86 | 107; 4096 rows - | 219 | 247 | 152 | 113
-  //   I 4096, O 14336: 1 row 23 | 10; 64 rows 103 | 15 | 54; 512 rows - | 98 | 129 | 80 | 102; 1024 rows - | 188 |
+  // Which kernel, by the same reckoning as for dense weights (us at 2 bits; 16 | 64 channels shared | panels of 64 |
+  // 128 | 256 rows by workgroups):
+  //   I 4096, O 4096: 1 row 6 | 10 | 52 | - | -; 17 rows - | 10; 256 rows - | 17 | 55 | 72 | 96; 2048 rows - | 116 |
+  //     135 | 86 | 107; 4096 rows - | 219 | 247 | 152 | 113
+  //   I 4096, O 14336: 1 row - | 9 | 52; 64 rows - | 15 | 54; 512 rows - | 98 | 129 | 80 | 102; 1024 rows - | 188 |
   //     246 | 150 | 107
-  //   I 14336, O 4096: 1 row 13 | 25; 16 rows 20 | 25; 64 rows 76 | 35
-  // 3 bits take 4 to 8 % longer, 4 bits 15 to 40 %.
-  const bool low = rows.rows <= 32 * std::min<int64_t>(rows.rows, rows.groups);
+  //   I 14336, O 4096: 1 row 11 | 25 | 173; 16 rows 11 | 25; 64 rows - | 35 | 193
+  // 3 bits take 4 to 10 % longer, 4 bits 15 to 40 %.
+  const double each = (double)rows.rows / std::min<int64_t>(rows.rows, rows.groups);   // rows of a group
   const TileCost large[] = {{256, 256, 3, 1.4, 1.65}, {128, 256, 2, 1.0, 1.15}, {64, 256, 1.5, 0.72, 0.95}};
-  const TileCost shared[] = {{64, 64, 1, low ? 0.095 : 0.15, low ? 0.12 : 0.2}};
-  const TileCost few[] = {{16, 16, 2.5, 0.03, 0.05}};
+  const TileCost shared[] = {{64, 64, 1, each <= 16 ? 0.07 : each <= 32 ? 0.095 : 0.15,
+                              each <= 16 ? 0.09 : each <= 32 ? 0.12 : 0.2}};
+  const TileCost few[] = {{16, 16, 0.7, 0.02, 0.03}};
   const int vector_out = four_at_once(y, T::kDtype, L.O), slabs = 2 * L.blocks;
   const E* xe = static_cast<const E*>(x);
   E* ye = static_cast<E*>(y);
@@ -493,13 +457,9 @@ hipError_t launch_packed(const PackedLayer& L, const GroupRows& rows, const void
   if (!plan.split)
     return launch_ring<k_packed_tile<T, BITS, kFine>>(most_panels(rows, plan.height) * tiles_of(L.O, Whole::TN), s, L,
                                                       rows, xe, ye, plan.height, vector_out);
-  if (plan.height == 64) {
-    const int waves = std::min(kSplitWaves, L.blocks);
-    return launch_lds<k_packed_shared<T, BITS, kFine>>(most_panels(rows, 64) * tiles_of(L.O, kSharedCols), 64 * waves,
-                                                       (size_t)waves * 2 * 64 * ROW_BYTES, s, L, rows, xe, ye, vector_out);
-  }
-  return launch_lds<k_packed_few<T, BITS, kFine>>(most_panels(rows, 16) * L.tiles, 64 * std::min(kFewWaves, L.blocks),
-                                                  0, s, L, rows, xe, ye);
+  if (plan.height == 64) return launch_shared<T, BITS, kFine, 64, false>(L, rows, xe, ye, vector_out, s);
+  return aligned16(x) ? launch_shared<T, BITS, kFine, 16, false>(L, rows, xe, ye, vector_out, s)
+                      : launch_shared<T, BITS, kFine, 16, true>(L, rows, xe, ye, vector_out, s);
 }
 
 template <class T, int BITS>
