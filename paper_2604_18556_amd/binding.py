@@ -1,4 +1,4 @@
-"""ctypes binding of include/gsq.h: argument marshalling only.
+"""ctypes binding of include/gsq.h and include/gsq_products.h: argument marshalling only.
 
 Every computation runs in ``libgsq.so``; this module passes device pointers
 (``tensor.data_ptr()``) and the current HIP stream to it and turns status codes
@@ -24,10 +24,10 @@ STATUS_NAMES = {0: "GSQ_OK", -1: "GSQ_EINVAL", -2: "GSQ_ENOMEM", -3: "GSQ_EHIP",
 
 EXPORTS = ("gsq_layer_init", "gsq_step", "gsq_step_static", "gsq_harden", "gsq_packed_size",
            "gsq_pack", "gsq_get_state", "gsq_set_state", "gsq_get_intermediates", "gsq_gumbel", "gsq_check",
-           "gsq_layer_destroy", "gsq_release_cached", "gsq_last_error", "gsq_timing", "gsq_timing_read",
-           "gsq_grouped_forward", "gsq_grouped_input_grad", "gsq_grouped_weight_grad", "gsq_gram",
-           "gsq_quantize_rows", "gsq_grouped_forward_i8", "gsq_linear_init", "gsq_linear_forward",
-           "gsq_linear_destroy")
+           "gsq_layer_destroy", "gsq_release_cached", "gsq_last_error", "gsq_timing", "gsq_timing_read")
+PRODUCT_EXPORTS = ("gsq_grouped_forward", "gsq_grouped_input_grad", "gsq_grouped_weight_grad", "gsq_gram",
+                   "gsq_quantize_rows", "gsq_grouped_forward_i8", "gsq_linear_init", "gsq_linear_forward",
+                   "gsq_linear_destroy")
 KERNEL_NAMES = ("init", "forward", "contract", "reduce", "backward", "harden", "pack")
 
 
@@ -160,9 +160,7 @@ def load(path=None):
     lib.gsq_linear_init.argtypes = [ctypes.POINTER(CConfig), vp, sz, vp, ctypes.POINTER(vp)]
     lib.gsq_linear_forward.argtypes = [vp, vp, i32, i64, vp, vp, vp]
     lib.gsq_linear_destroy.argtypes = [vp]
-    for name in ("gsq_grouped_forward", "gsq_grouped_input_grad", "gsq_grouped_weight_grad",
-                 "gsq_gram", "gsq_quantize_rows", "gsq_grouped_forward_i8", "gsq_linear_init",
-                 "gsq_linear_forward", "gsq_linear_destroy"):
+    for name in PRODUCT_EXPORTS:
         getattr(lib, name).restype = ctypes.c_int
     for name in ("gsq_layer_init", "gsq_step", "gsq_step_static", "gsq_harden", "gsq_pack",
                  "gsq_get_state", "gsq_set_state", "gsq_get_intermediates", "gsq_gumbel", "gsq_check",

@@ -3,7 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "gsq.h"
+#include "gsq_products.h"
 
 namespace gsq {
 

@@ -56,6 +56,13 @@ gsq_status check_array(const char* name, const void* p, size_t elem, bool any) {
   return GSQ_OK;
 }
 
+// A launch's outcome.  Its grid is checked before anything is enqueued.
+gsq_status launched(hipError_t e, const char* what) {
+  if (e == hipSuccess) return GSQ_OK;
+  if (e == hipErrorInvalidConfiguration) return fail(GSQ_EINVAL, "%s: more tiles than one launch holds", what);
+  return gsq::hip_fail(e, what);
+}
+
 #define GSQ_TRY(call)                    \
   do {                                   \
     const gsq_status st_ = (call);       \
@@ -97,8 +104,8 @@ gsq_status gsq_grouped_forward(const gsq_grouped* g, const void* x, const void* 
   GSQ_TRY(check_array("x", x, 2, g->rows > 0));
   GSQ_TRY(check_array("w", w, 2, true));
   GSQ_TRY(check_array("y", y, 2, g->rows > 0));
-  GSQ_HIP(gsq::launch_product(gsq::kForward, g->dtype, product_args(g, offsets, x, w, y, g->dtype), stream));
-  return GSQ_OK;
+  return launched(gsq::launch_product(gsq::kForward, g->dtype, product_args(g, offsets, x, w, y, g->dtype), stream),
+                  "gsq_grouped_forward");
 }
 
 gsq_status gsq_grouped_input_grad(const gsq_grouped* g, const void* dy, const void* w,
@@ -108,8 +115,8 @@ gsq_status gsq_grouped_input_grad(const gsq_grouped* g, const void* dy, const vo
   GSQ_TRY(check_array("dy", dy, 2, g->rows > 0));
   GSQ_TRY(check_array("w", w, 2, true));
   GSQ_TRY(check_array("dx", dx, 2, g->rows > 0));
-  GSQ_HIP(gsq::launch_product(gsq::kInputGrad, g->dtype, product_args(g, offsets, dy, w, dx, g->dtype), stream));
-  return GSQ_OK;
+  return launched(gsq::launch_product(gsq::kInputGrad, g->dtype, product_args(g, offsets, dy, w, dx, g->dtype), stream),
+                  "gsq_grouped_input_grad");
 }
 
 gsq_status gsq_grouped_weight_grad(const gsq_grouped* g, const void* dy, const void* x,
@@ -126,8 +133,8 @@ gsq_status gsq_grouped_weight_grad(const gsq_grouped* g, const void* dy, const v
   GSQ_TRY(check_array("dw", dw, dw_dtype == GSQ_DT_FP32 ? 4 : 2, true));
   gsq::ProductArgs p = product_args(g, offsets, dy, x, dw, dw_dtype);
   p.accumulate = accumulate ? 1 : 0;
-  GSQ_HIP(gsq::launch_product(gsq::kWeightGrad, g->dtype, p, stream));
-  return GSQ_OK;
+  return launched(gsq::launch_product(gsq::kWeightGrad, g->dtype, p, stream),
+                  "gsq_grouped_weight_grad");
 }
 
 gsq_status gsq_gram(const gsq_grouped* g, const void* x, const int64_t* offsets, float* h,
@@ -139,8 +146,8 @@ gsq_status gsq_gram(const gsq_grouped* g, const void* x, const int64_t* offsets,
   gsq::ProductArgs p = product_args(g, offsets, x, x, h, GSQ_DT_FP32);
   p.O = g->in_features;
   p.accumulate = accumulate ? 1 : 0;
-  GSQ_HIP(gsq::launch_gram(g->dtype, p, stream));
-  return GSQ_OK;
+  return launched(gsq::launch_gram(g->dtype, p, stream),
+                  "gsq_gram");
 }
 
 gsq_status gsq_quantize_rows(const void* x, int32_t dtype, int64_t rows, int32_t cols, int8_t* q,
@@ -173,8 +180,8 @@ gsq_status gsq_grouped_forward_i8(const gsq_grouped* g, const int8_t* x, const f
   gsq::ProductArgs p = product_args(g, offsets, x, w, y, g->dtype);
   p.a_scales = x_scales;
   p.b_scales = w_scales;
-  GSQ_HIP(gsq::launch_product_i8(p, stream));
-  return GSQ_OK;
+  return launched(gsq::launch_product_i8(p, stream),
+                  "gsq_grouped_forward_i8");
 }
 
 gsq_status gsq_linear_init(const gsq_config* cfg, const void* packed, size_t packed_bytes,
@@ -255,8 +262,8 @@ gsq_status gsq_linear_forward(const gsq_linear* h, const void* x, int32_t dtype,
   GSQ_HIP(hipGetDevice(&dev));
   if (dev != h->device)
     return fail(GSQ_EINVAL, "the handle was created on device %d, device %d is current", h->device, dev);
-  GSQ_HIP(gsq::launch_packed_product(h->L, dtype, gsq::GroupRows{offsets, rows, h->groups}, x, y, stream));
-  return GSQ_OK;
+  return launched(gsq::launch_packed_product(h->L, dtype, gsq::GroupRows{offsets, rows, h->groups}, x, y, stream),
+                  "gsq_linear_forward");
 }
 
 gsq_status gsq_linear_destroy(gsq_linear* h) {

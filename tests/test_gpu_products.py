@@ -134,6 +134,65 @@ def test_products_of_random_values(dev, counts, o, i, dtype):
     assert torch.equal(h, h.mT.contiguous())
 
 
+# sizes that fill the GPU: whole workgroups on 256, 128 and 64 rows, on 128 x 128 tiles, from unaligned arrays
+LARGE = [([2048], 8192, 520), ([1000], 8192, 1032), ([520], 8192, 2056), ([700, 0, 300, 90, 20], 4096, 1032),
+         ([4000], 4096, 4104), ([300] * 5, 2048, 2048), ([4100], 2050, 514), ([600, 40], 1030, 3001)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("counts,o,i", LARGE)
+def test_large_products_of_whole_numbers_are_exact(dev, counts, o, i, dtype):
+    """As above, against 64-bit products on the GPU.  Values up to 1, so that 8192 of them stay exact in fp16."""
+    print(f"large {counts} {o}x{i} {dtype}", flush=True)
+    gen = torch.Generator(device=dev).manual_seed(o + i)
+    e, first = len(counts), 5
+    rows, off = first + sum(counts) + 9, offsets_of(counts, dev, first)
+
+    def numbers(*shape):
+        return torch.randint(-1, 2, shape, generator=gen, device=dev, dtype=torch.int8)
+
+    x, w, dy = numbers(rows, i), numbers(e, o, i), numbers(rows, o)
+    y, dx = torch.full((rows, o), 7.0, dtype=dtype, device=dev), torch.full((rows, i), 7.0, dtype=dtype, device=dev)
+    dw, h = torch.empty(e, o, i, dtype=dtype, device=dev), torch.empty(e, i, i, device=dev)
+    y8, ones = torch.full((rows, o), 7.0, dtype=dtype, device=dev), torch.ones(max(rows, e * o), device=dev)
+    B.grouped_forward(x.to(dtype), w.to(dtype), y, offsets=off)
+    B.grouped_input_grad(dy.to(dtype), w.to(dtype), dx, offsets=off)
+    B.grouped_weight_grad(dy.to(dtype), x.to(dtype), dw, offsets=off)
+    B.gram(x.to(dtype), h, offsets=off)
+    B.grouped_forward_i8(x, ones[:rows], w, ones[:e * o].view(e, o), y8, offsets=off)
+    for k, (a, b) in enumerate(split(off)):
+        xe, we, de = x[a:b].double(), w[k].double(), dy[a:b].double()
+        ref = (xe @ we.t()).to(dtype)
+        assert torch.equal(y[a:b], ref) and torch.equal(y8[a:b], ref)
+        assert torch.equal(dx[a:b], (de @ we).to(dtype))
+        assert torch.equal(dw[k], (de.t() @ xe).to(dtype))
+        assert torch.equal(h[k], (xe.t() @ xe).float())
+    for t in (y, y8, dx):
+        assert (t[:first] == 7).all() and (t[rows - 9:] == 7).all()
+
+
+def test_many_groups(dev):
+    """More groups than a wavefront has lanes, most of them empty, several times over."""
+    gen, e, o, i = rng_of(21), 1000, 72, 136
+    counts = torch.randint(0, 4, (e,), generator=gen) * (torch.rand(e, generator=gen) < 0.3)
+    counts[777] = 150
+    rows, off = int(counts.sum()), offsets_of(counts.tolist(), dev)
+    x, w, dy = whole((rows, i), gen, 2), whole((e, o, i), gen, 2), whole((rows, o), gen, 2)
+    y, dx = torch.empty(rows, o, dtype=BF16, device=dev), torch.empty(rows, i, dtype=BF16, device=dev)
+    dw = torch.empty(e, o, i, device=dev)
+    xd, wd, dyd = (t.to(BF16).to(dev) for t in (x, w, dy))
+    B.grouped_forward(xd, wd, y, offsets=off)
+    B.grouped_input_grad(dyd, wd, dx, offsets=off)
+    B.grouped_weight_grad(dyd, xd, dw, offsets=off)
+    group = torch.arange(e).repeat_interleave(counts)
+    assert torch.equal(y.cpu(), torch.stack([x[r] @ w[group[r]].t() for r in range(rows)]).to(BF16))
+    assert torch.equal(dx.cpu(), torch.stack([dy[r] @ w[group[r]] for r in range(rows)]).to(BF16))
+    ref = torch.zeros(e, o, i).double()
+    for r in range(rows):
+        ref[group[r]] += torch.outer(dy[r], x[r])
+    assert torch.equal(dw.cpu(), ref.float())
+
+
 def test_gradients_are_the_forwards_differences(dev):
     """f = <dy, y(x, w)> is linear in x and in w: with whole numbers its differences are exact."""
     gen, counts, o, i = rng_of(1), [6, 0, 11], 40, 56
@@ -506,6 +565,46 @@ def test_packed_codes_beyond_the_levels_are_the_last_one(dev):
     y = torch.empty(1, 16, dtype=BF16, device=dev)
     lin.forward(x, y)
     assert (y == 64).all()
+
+
+@pytest.mark.parametrize("counts", [[2048], [700, 0, 130, 20], [300, 300, 300, 300]])
+@pytest.mark.parametrize("layout,levels,group", [("group", inputs.L8, 128), ("superblock", inputs.L8, 16),
+                                                 ("base3", inputs.L3, 32), ("group", inputs.L4, 256)])
+def test_packed_products_with_many_rows(dev, layout, levels, group, counts):
+    """Whole tiles, against the dense product with the same weights, which has the same sums in another order."""
+    gen, o, i, e = rng_of(group, len(counts)), 2048, 1280, len(counts)
+    cfg, packed, w = packed_layer(layout, levels, group, e, o, i, gen)
+    lin = B.Linear(cfg, packed.to(dev))
+    rows, off = sum(counts), offsets_of(counts, dev)
+    x = torch.randn(rows, i, generator=gen).to(BF16).to(dev)
+    y = torch.empty(rows, o, dtype=BF16, device=dev)
+    lin.forward(x, y, offsets=off)
+    w = w.to(BF16).to(dev)
+    for k, (a, b) in enumerate(split(off)):
+        xe, we = x[a:b].double(), w[k].double()
+        assert_close(y[a:b], (xe @ we.t()).cpu(), (xe.abs() @ we.abs().t()).cpu(), i, BF16, f"{layout} {k}")
+
+
+@pytest.mark.parametrize("rows", [1, 40, 700])
+def test_packed_products_from_any_address(dev, rows):
+    """x and y that begin at an odd element, and calls on two streams at once."""
+    gen, o, i = rng_of(rows, 6), 136, 640
+    cfg, packed, w = packed_layer("group", inputs.L4, 64, 1, o, i, gen)
+    lin = B.Linear(cfg, packed.to(dev))
+    torch.cuda.synchronize()
+    x = torch.randn(rows, i, generator=gen).to(BF16)
+    xd = torch.zeros(rows * i + 3, dtype=BF16, device=dev)[3:].view(rows, i)
+    xd.copy_(x)
+    ys = [torch.zeros(rows * o + 1, dtype=BF16, device=dev)[1:].view(rows, o) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in ys]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, y in zip(streams, ys):
+            lin.forward(xd, y, stream=s)
+    torch.cuda.synchronize()
+    w = w[0].to(BF16).double()
+    assert_close(ys[0], x.double() @ w.t(), x.double().abs() @ w.abs().t(), i, BF16)
+    assert torch.equal(ys[0], ys[1])
 
 
 def test_packed_values_that_are_not_finite(dev):

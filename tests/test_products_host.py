@@ -1,6 +1,8 @@
 """What the products refuse, and in what words, before anything reaches the device."""
 import ctypes
 import os
+import re
+import subprocess
 
 import pytest
 
@@ -95,6 +97,40 @@ def test_no_rows_need_no_arrays(lib):
     assert lib.gsq_grouped_input_grad(g, None, a, None, None, None) == B.GSQ_OK
     assert lib.gsq_grouped_forward_i8(g, None, None, a, a, None, None, None) == B.GSQ_OK
     assert lib.gsq_quantize_rows(None, B.DT_BF16, 0, 8, None, None, None) == B.GSQ_OK
+
+
+def test_products_of_more_tiles_than_a_launch_holds(lib):
+    """The grid is checked before anything is enqueued."""
+    g, a = ctypes.byref(sizes(groups=1, out=1 << 21, inn=64, rows=1 << 29)), P(64)
+    for st in (lib.gsq_grouped_forward(g, a, a, None, a, None),
+               lib.gsq_grouped_forward_i8(g, a, a, a, a, None, a, None),
+               lib.gsq_grouped_weight_grad(ctypes.byref(sizes(groups=65535, out=1 << 21, inn=1 << 21)), a, a, a, a,
+                                           B.DT_FP32, 0, None)):
+        assert st == B.GSQ_EINVAL
+        assert b"tiles" in lib.gsq_last_error()
+
+
+def test_header_and_library_have_the_same_calls(lib):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    text = open(os.path.join(root, "include", "gsq_products.h")).read()
+    assert set(re.findall(r"^gsq_status\s+(gsq_\w+)\s*\(", text, re.M)) == set(B.PRODUCT_EXPORTS)
+    for name in B.PRODUCT_EXPORTS:
+        assert getattr(lib, name) is not None
+
+
+def test_header_is_plain_c(tmp_path):
+    """The header compiles as C, and its struct is the binding's."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "layout.c"
+    src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "gsq_products.h"\n'
+                   'int main(void) { printf("%zu %zu %d", sizeof(gsq_grouped), offsetof(gsq_grouped, rows), '
+                   'GSQ_DT_FP16); return 0; }\n')
+    r = subprocess.run(["gcc", "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(root, "include"), "-I",
+                        "/opt/rocm/include", str(src), "-o", str(tmp_path / "layout")], capture_output=True, text=True)
+    if r.returncode:
+        pytest.skip("cannot compile against hip_runtime_api.h: " + r.stderr[-300:])
+    out = subprocess.run([str(tmp_path / "layout")], capture_output=True, text=True).stdout.split()
+    assert [int(v) for v in out] == [ctypes.sizeof(B.CGrouped), B.CGrouped.rows.offset, B.DT_FP16]
 
 
 def test_linear_refusals(lib):
