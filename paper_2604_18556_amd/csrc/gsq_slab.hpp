@@ -1,5 +1,5 @@
-// Device parts of the kernels whose operands move as slabs through a ring in LDS: the order of the tiles,
-// the slab's layout, and the waits.
+// Device parts of the products whose operands move as slabs through LDS: the order of the tiles, a slab's layout,
+// and the waits.  (gsq_contract.hip, whose measured traffic is recorded for its exact source, has its own.)
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -14,8 +14,8 @@ constexpr int GROUP_M = 8;           // tile rows swept together for L2 reuse
 constexpr size_t LDS_BYTES = 160 * 1024;
 
 // Position of block `bid` of nblk in the tile order.  Workgroups are handed to the 8 XCDs
-// round-robin; renumbering so each XCD owns a contiguous range of the blocks keeps the R and H
-// panels a group of tiles shares in the same XCD's L2.
+// round-robin; renumbering so each XCD owns a contiguous range of the blocks keeps the panels of both
+// operands that a group of tiles shares in the same XCD's L2.
 __device__ __forceinline__ int lin_of(int bid, int nblk) {
   const int x = bid & 7, base = nblk >> 3, rem = nblk & 7;
   return x * base + min(x, rem) + (bid >> 3);
@@ -40,8 +40,7 @@ __device__ __forceinline__ void tile_at(int lin, int tiles_m, int tiles_n, int& 
 __device__ __forceinline__ int swz(int r) { return (r >> 1) & 7; }
 
 // Global->LDS copy of a wavefront's share of one operand slab: n instructions of eight rows, 16
-// bytes per lane.  `src` is wave-uniform (the slab's first column); off[j] is the lane's element
-// offset of instruction j, fixed for the whole K loop.
+// bytes per lane, by the compiler's own instruction, whose waits it keeps account of.
 __device__ __forceinline__ void load_rows(const uint16_t* src, uint8_t* lds) {
   __builtin_amdgcn_global_load_lds(src, lds, 16, 0, 0);
 }
