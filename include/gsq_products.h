@@ -18,7 +18,7 @@
  * arithmetic has them, within the rows and channels they belong to.  Pointers need the alignment of their
  * elements only; arrays with 16-byte aligned bases and rows are read faster.  Limits (GSQ_EINVAL):
  * groups <= 65535, rows <= 2^29, out_features and in_features <= 2^21, and the tiles of one launch (an
- * output of more than some 2^35 elements may pass them).  The device that the pointers belong to has to be
+ * output of more than 2^32 elements may pass them).  The device that the pointers belong to has to be
  * current.
  */
 #ifndef GSQ_PRODUCTS_H

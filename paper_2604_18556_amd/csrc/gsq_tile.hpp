@@ -52,7 +52,9 @@ __device__ __forceinline__ void mfma_block(typename T::acc& acc, const i32x4& b,
 // make every transposing LDS read wait for all of them: the loop's own wait_vm() and barrier order them, and
 // they return nothing to a register.  Addresses: a uniform base with 32-bit lane offsets, or one per lane.
 // M0 holds the LDS address; nothing else in these kernels uses it (it is no register that the compiler keeps
-// values in).
+// values in).  A uniform base has to come from scalar instructions, as a slab's does that is reckoned from the
+// operand's: one that a vector instruction wrote needs five instructions between, which the compiler does not
+// see to here.
 __device__ __forceinline__ uint32_t lds_address(const uint8_t* lds) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)lds;
 }
