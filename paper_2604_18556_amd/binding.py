@@ -37,6 +37,13 @@ class GsqError(RuntimeError):
         self.status = status
 
 
+def _int32(name, value):
+    """`value`, which has to fit the library's 32-bit argument: ctypes would keep its low bits in silence."""
+    if not -(1 << 31) <= value < 1 << 31:
+        raise ValueError(f"{name} does not fit 32 bits: {value}")
+    return value
+
+
 class CConfig(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("out_features", ctypes.c_int32),
                 ("in_features", ctypes.c_int32), ("n_levels", ctypes.c_int32),
@@ -77,11 +84,13 @@ class LayerConfig:
 
     def to_c(self):
         c = CConfig()
-        c.batch, c.out_features, c.in_features = self.batch, self.out_features, self.in_features
+        c.batch = _int32("batch", self.batch)
+        c.out_features = _int32("out_features", self.out_features)
+        c.in_features = _int32("in_features", self.in_features)
         c.n_levels = len(self.levels)
         for k, x in enumerate(self.levels):
             c.levels[k] = float(x)
-        c.group_size, c.layout, c.precision = self.group_size, self.layout, self.precision
+        c.group_size, c.layout, c.precision = _int32("group_size", self.group_size), self.layout, self.precision
         c.seed, c.alpha, c.sigma_init = self.seed, self.alpha, self.sigma_init
         c.init_noise = 1 if self.init_noise else 0
         c.relaxation = self.relaxation
@@ -393,11 +402,12 @@ def _rows_dtype(t):
 
 def _weight_sizes(w, name="w"):
     shape = w.shape
-    if len(shape) == 3:
-        return shape
     if len(shape) == 2:
-        return (1, *shape)
-    raise ValueError(f"{name} must be groups x O x I or O x I, got {tuple(shape)}")
+        shape = (1, *shape)
+    elif len(shape) != 3:
+        raise ValueError(f"{name} must be groups x O x I or O x I, got {tuple(shape)}")
+    _int32(f"the largest size of {name}", max(shape))
+    return shape
 
 
 def _row_count(x, name):
@@ -456,10 +466,10 @@ def quantize_rows(x, q, scales, stream=None):
     import torch
     if len(x.shape) < 2:
         raise ValueError(f"x must be rows x columns, got {tuple(x.shape)}")
-    dt = DT_FP32 if x.dtype is torch.float32 else _rows_dtype(x)
+    dt, cols = DT_FP32 if x.dtype is torch.float32 else _rows_dtype(x), _int32("the columns of x", x.shape[-1])
     dev = _checked((("x", x, x.shape, (x.dtype,)), ("q", q, x.shape, (torch.int8,)),
                     ("scales", scales, x.shape[:-1], (torch.float32,))), None, 1)
-    _check(load().gsq_quantize_rows(x.data_ptr(), dt, scales.numel(), x.shape[-1], q.data_ptr(),
+    _check(load().gsq_quantize_rows(x.data_ptr(), dt, scales.numel(), cols, q.data_ptr(),
                                     scales.data_ptr(), _raw_stream(stream, dev)))
 
 

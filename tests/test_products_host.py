@@ -184,3 +184,29 @@ def test_binding_checks_tensors_before_the_library():
         B.quantize_rows(x, torch.zeros(3, 7, dtype=torch.int8), torch.zeros(3))
     with pytest.raises(ValueError, match="device tensor"):
         B.Linear(B.LayerConfig(4, 16, (-1.0, 1.0), 16), torch.zeros(64, dtype=torch.uint8))
+
+
+BIG = (1 << 32) + 8          # 8 in its low 32 bits
+
+
+@pytest.mark.parametrize("call", [
+    lambda t: B.grouped_forward(t(1, BIG), t(8, BIG), t(1, 8)),
+    lambda t: B.grouped_forward(t(1, 8), t(BIG, 8), t(1, BIG)),
+    lambda t: B.grouped_forward(t(1, 8), t(BIG, 8, 8), t(1, 8), offsets=t(BIG + 1, dtype=torch.int64)),
+    lambda t: B.grouped_input_grad(t(1, BIG), t(BIG, 8), t(1, 8)),
+    lambda t: B.grouped_weight_grad(t(1, 8), t(1, BIG), t(8, BIG)),
+    lambda t: B.quantize_rows(t(1, BIG), t(1, BIG, dtype=torch.int8), t(1, dtype=torch.float32)),
+    lambda t: B.grouped_forward_i8(t(1, BIG, dtype=torch.int8), t(1, dtype=torch.float32), t(8, BIG, dtype=torch.int8),
+                                   t(8, dtype=torch.float32), t(1, 8))])
+def test_sizes_beyond_32_bits_are_refused_not_cut(call):
+    """A size whose low 32 bits are a fine size would be taken for that one."""
+    with pytest.raises(ValueError, match="32 bits"):
+        call(lambda *shape, dtype=torch.bfloat16: torch.empty(*shape, dtype=dtype, device="meta"))
+
+
+@pytest.mark.parametrize("name", ["out_features", "in_features", "batch", "group_size"])
+def test_layers_beyond_32_bits_are_refused_not_cut(name):
+    cfg = B.LayerConfig(8, 256, (-1.0, 1.0))
+    setattr(cfg, name, (1 << 32) + getattr(cfg, name))
+    with pytest.raises(ValueError, match=name):
+        B.packed_size(cfg)
