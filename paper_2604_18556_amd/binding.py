@@ -387,6 +387,8 @@ def _refuse(args, device):
 def _raw_stream(stream, device):
     import torch
     if stream is not None:
+        if getattr(stream, "device_index", device) != device:
+            raise ValueError(f"the stream is on device {stream.device_index}, but device {device} is current")
         return stream.cuda_stream
     return torch._C._cuda_getCurrentRawStream(device)   # current_stream() without building an object
 

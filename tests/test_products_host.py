@@ -3,6 +3,7 @@ import ctypes
 import os
 import re
 import subprocess
+from types import SimpleNamespace
 
 import pytest
 
@@ -210,3 +211,10 @@ def test_layers_beyond_32_bits_are_refused_not_cut(name):
     setattr(cfg, name, (1 << 32) + getattr(cfg, name))
     with pytest.raises(ValueError, match=name):
         B.packed_size(cfg)
+
+
+def test_streams_of_another_device_are_refused():
+    """The tensors are checked to be on the current device: their kernel may not go to another one's stream."""
+    assert B._raw_stream(SimpleNamespace(cuda_stream=64, device_index=1), 1) == 64
+    with pytest.raises(ValueError, match="stream is on device 1"):
+        B._raw_stream(SimpleNamespace(cuda_stream=64, device_index=1), 0)
