@@ -432,28 +432,10 @@ hipError_t launch_shared(const PackedLayer& L, const GroupRows& rows, const type
 template <class T, int BITS, bool kFine>
 hipError_t launch_packed(const PackedLayer& L, const GroupRows& rows, const void* x, void* y, hipStream_t s) {
   using E = typename T::elem;
-  // Which kernel, by the same reckoning as for dense weights (us at 2 bits; 16 | 64 channels shared | panels of 64 |
-  // 128 | 256 rows by workgroups):
-  //   I 4096, O 4096: 1 row 6 | 10 | 52 | - | -; 17 rows - | 10; 256 rows - | 17 | 55 | 72 | 96; 2048 rows - | 116 |
-  //     135 | 86 | 107; 4096 rows - | 219 | 247 | 152 | 113
-  //   I 4096, O 14336: 1 row - | 9 | 52; 64 rows - | 15 | 54; 512 rows - | 98 | 129 | 80 | 102; 1024 rows - | 188 |
-  //     246 | 150 | 107
-  //   I 14336, O 4096: 1 row 11 | 25 | 173; 16 rows 11 | 25; 64 rows - | 35 | 193
-  // 3 bits take 4 to 10 % longer, 4 bits 15 to 40 %.
-  const double each = (double)rows.rows / std::min<int64_t>(rows.rows, rows.groups);   // rows of a group
-  const TileCost large[] = {{256, 256, 3, 1.4, 1.65}, {128, 256, 2, 1.0, 1.15}, {64, 256, 1.5, 0.72, 0.95}};
-  const TileCost shared[] = {{64, 64, 1, each <= 16 ? 0.07 : each <= 32 ? 0.095 : 0.15,
-                              each <= 16 ? 0.09 : each <= 32 ? 0.12 : 0.2}};
-  const TileCost few[] = {{16, 16, 0.7, 0.02, 0.03}};
-  const int vector_out = four_at_once(y, T::kDtype, L.O), slabs = 2 * L.blocks;
+  const int vector_out = four_at_once(y, T::kDtype, L.O);
   const E* xe = static_cast<const E*>(x);
   E* ye = static_cast<E*>(y);
-  double best = 1e30;
-  RowsPlan plan = cheapest(rows, L.O, slabs, few, true, best, RowsPlan{});
-  if (aligned16(x)) {
-    plan = cheapest(rows, L.O, slabs, shared, true, best, plan);
-    plan = cheapest(rows, L.O, slabs, large, false, best, plan);
-  }
+  const RowsPlan plan = plan_packed(rows.rows, rows.groups, L.O, L.blocks, aligned16(x));
   if (!plan.split)
     return launch_ring<k_packed_tile<T, BITS, kFine>>(most_panels(rows, plan.height) * tiles_of(L.O, Whole::TN), s, L,
                                                       rows, xe, ye, plan.height, vector_out);

@@ -3,7 +3,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cmath>
 
 #include "gsq_split.hpp"
 
@@ -309,7 +308,7 @@ __global__ __launch_bounds__(256) void k_quantize_rows(const E* __restrict__ x, 
 template <class T, int kForm, int TM, int TN, bool kLoose>
 hipError_t launch_rows_split(const ProductArgs& p, hipStream_t s) {
   const int ks = kForm == kForward ? p.I : p.O, ns = kForm == kForward ? p.O : p.I;
-  const int nk = tiles_of(ks, ROW_BYTES / (int)sizeof(typename T::elem));
+  const int nk = (int)tiles_of(ks, ROW_BYTES / (int)sizeof(typename T::elem));
   const int waves = std::min(nk, kSplitWaves);
   return launch_lds<k_rows_split<T, kForm, TM, TN, kLoose>>(most_panels(p.rows, TM) * tiles_of(ns, TN), 64 * waves,
                     waves * (TM + TN) * ROW_BYTES, s, p);
@@ -324,41 +323,19 @@ hipError_t launch_rows_split(const ProductArgs& p, const RowsPlan& plan, hipStre
                           : launch_rows_split<T, kForm, 64, 16, kLoose>(p, s);
 }
 
-// Which tiles: whole workgroups on panels of 256, 128 or 64 rows, or wavefronts that share a sum.  The costs
-// are fitted to bf16 products of one group (us for x W^T; 256 | 128 | 64 rows by workgroups, 64 x 64 | 64 x 16
-// split):
-//   8192 x 8192: 64 rows - | - | 101, 44 | 51; 256 rows 154 | 111 | 100, 71 | 141; 512 rows 158 | 112 | 101,
-//     125 | 246; 1024 rows 162 | 123 | 205, 225 | -; 2048 rows 208 | 242 | 371, 432 | -
-//   2048 x 2048: 64 rows - | - | 18.1, 9.6 | 6.7; 512 rows 47 | 30 | 19, 11 | 19; 2048 rows 49 | 31 | 24, 38 | -
-//   O 512, I 8192: 512 rows 147 | 90 | 57, 25 | 18; 4096 rows 150 | 92 | 60, 54 | -
-// and 8192 x 8192 at one row by 16 x 64 | 16 x 16 split 30 | 28, at 64 rows 50 | 68.  8-bit integers take
-// longer in large tiles, which the power of the matrix cores bounds.
 template <class T, int kForm>
 hipError_t launch_rows(ProductArgs p, hipStream_t s) {
   if (p.rows.rows == 0) return hipSuccess;
   const int ns = kForm == kForward ? p.O : p.I, ks = kForm == kForward ? p.I : p.O;
   const int64_t unit = 16 / (int64_t)sizeof(typename T::elem);
-  const int slabs = tiles_of(ks, ROW_BYTES / (int)sizeof(typename T::elem));
+  const int slabs = (int)tiles_of(ks, ROW_BYTES / (int)sizeof(typename T::elem));
   p.vector_out = four_at_once(p.out, p.out_dtype, ns);
   const bool tight = p.O % (kForm == kForward ? 1 : unit) == 0 && p.I % unit == 0 && aligned16(p.a) && aligned16(p.b);
-  constexpr double kMore = T::kDtype < 0 ? 1.4 : 1;
-  const TileCost large[] = {{256, 256, 3, 1.15 * kMore, 1.6 * kMore}, {128, 256, 2, 0.7 * kMore, 0.95 * kMore},
-                            {64, 256, 1.5, 0.43 * kMore, 0.72 * kMore}};
-  // from any addresses (I 4001, O 8190; 64 x 64 split | 128 x 128): 64 rows 32 | 72, 512 rows 118 | 78, 4096 rows
-  // 866 | 378
-  const TileCost loose[] = {{128, 128, 2, kForm == kForward ? 0.85 : 2.0, kForm == kForward ? 0.75 : 1.05}};
-  const TileCost small_loose[] = {{64, 64, 1, 0.17, 0.42}, {64, 16, 1, 0.1, 0.21}, {16, 64, 1, 0.07, 0.15}, {16, 16, 0.5, 0.025, 0.08}};
-  const TileCost small[] = {{64, 64, 1, 0.165, 0.22}, {64, 16, 1, 0.1, 0.115}, {16, 64, 1, 0.06, 0.1}, {16, 16, 0.5, 0.02, 0.055}};
-  double best = 1e30;
-  RowsPlan plan = cheapest(p.rows, ns, slabs, tight ? small : small_loose, true, best, RowsPlan{});
-  if (tight) plan = cheapest(p.rows, ns, slabs, large, false, best, plan);
-  if (!tight) {
-    plan = cheapest(p.rows, ns, slabs, loose, false, best, plan);
-    if (plan.split) return launch_rows_split<T, kForm, true>(p, plan, s);
+  const RowsPlan plan = plan_rows(p.rows.rows, p.rows.groups, ns, slabs, tight, kForm == kInputGrad, T::kDtype < 0);
+  if (plan.split) return tight ? launch_rows_split<T, kForm, false>(p, plan, s) : launch_rows_split<T, kForm, true>(p, plan, s);
+  if (!tight)
     return launch_lds<k_rows_loose<T, kForm>>(most_panels(p.rows, Quarter::TM) * tiles_of(ns, Quarter::TN), 256,
                                               Quarter::LDS, s, p);
-  }
-  if (plan.split) return launch_rows_split<T, kForm, false>(p, plan, s);
   p.height = plan.height;
   return launch_ring<k_rows_tile<T, kForm>>(most_panels(p.rows, p.height) * tiles_of(ns, Whole::TN), s, p);
 }
@@ -366,45 +343,23 @@ hipError_t launch_rows(ProductArgs p, hipStream_t s) {
 template <class T, class Out, bool kGram>
 hipError_t launch_sums(ProductArgs p, hipStream_t s) {
   p.vector_out = four_at_once(p.out, p.out_dtype, p.I);
-  const auto count = [&](int64_t tile) {
-    const int64_t tm = tiles_of(p.O, tile), tn = tiles_of(p.I, tile);
-    return p.rows.groups * (kGram ? (tn + 1) / 2 * (tn + 1) : tm * tn);
-  };
   const bool tight = p.O % 8 == 0 && p.I % 8 == 0 && aligned16(p.a) && aligned16(p.b);
-  // Whole workgroups on 256 x 256 or 128 x 128 tiles, or wavefronts that share the sum of 64 x 64 or 32 x 32 ones:
-  // the cheapest by a tile's start and slabs, fitted to dW of one group (us, 256 | 128 | 64 | 32):
-  //   256 x 256: 4096 rows 96 | - | 14 | 8; 16384 rows 318 | - | 49 | 42
-  //   1024 x 1024: 4096 rows 95 | 34 | 19 | 38; 16384 rows 319 | 121 | 62 | 177
-  //   2048 x 2048: 256 rows 21 | 8 | 12 | 14; 4096 rows 96 | 42 | 61 | 137; 16384 rows 318 | 133 | 304 | 850
-  //   4096 x 4096: 64 rows - | 17 | 18 | -; 256 rows 21 | 19 | 38 | 46; 4096 rows 105 | 120 | 235 | 514; 16384 rows
-  //     401 | 527 | 1451 | -
-  //   8192 x 8192: 256 rows 72 | 66 | 138 | 170; 4096 rows 432 | 475 | 883 | 2120; 16384 rows 1607 | 2516 | - | -
-  // and H, which stores most tiles twice: 4096 x 4096 from 1024 rows 57 | 39 | 57 | 83, 8192 x 8192 from 64 rows
-  // - | 59 | 51 | -, 1024 rows 156 | 106 | 202 | 306, 16384 rows 1093 | 1857 | - | -.
-  const double slabs = (double)p.rows.rows / 64 / p.rows.groups;
-  const auto cost = [&](int64_t tile, double start, double more_start, double alone, double full) {
-    const double rounds = count(tile) / 256.0, load = std::min(1.0, rounds);
-    const double whole = p.rows.groups == 1 && tile != Quarter::TM ? std::ceil(rounds) : rounds;
-    return std::max(1.0, whole) * (start + more_start * load + (slabs + 0.5) * (alone + (full - alone) * load));
-  };
-  const double far = slabs > 100 ? 1.25 : 1;   // what the L2 holds of a long sum's operands no longer serves small tiles
-  const double us_whole = !tight ? 1e30 : cost(Whole::TM, kGram ? 20 : 9, kGram ? 12 : 3.5, 1.2, kGram ? 1.35 : 1.5);
-  const double us_quarter = cost(Quarter::TM, kGram ? 6.5 : 2, 0, 0.45 * far, 0.5 * far);
-  const double us_64 = cost(64, kGram ? 1.4 : 0.7, 0, 0.17, 0.23), us_32 = cost(32, kGram ? 0.3 : 0.15, 0, 0.08, 0.14);
-  if (us_whole < std::min(us_quarter, std::min(us_64, us_32)))
-    return launch_lds<k_sums_tile<T, Out, kGram, Whole, false>>(count(Whole::TM), 256, Whole::LDS, s, p);
-  if (us_quarter < std::min(us_64, us_32))
-    return tight ? launch_lds<k_sums_tile<T, Out, kGram, Quarter, false>>(count(Quarter::TM), 256, Quarter::LDS, s, p)
-                 : launch_lds<k_sums_tile<T, Out, kGram, Quarter, true>>(count(Quarter::TM), 256, Quarter::LDS, s, p);
+  const SumsPlan plan = plan_sums(p.rows.rows, p.rows.groups, p.O, p.I, tight, kGram);
+  const int64_t tiles = sum_tiles(p.rows.groups, p.O, p.I, kGram, plan.size);
+  if (!plan.split && plan.size == Whole::TM)
+    return launch_lds<k_sums_tile<T, Out, kGram, Whole, false>>(tiles, 256, Whole::LDS, s, p);
+  if (!plan.split)
+    return tight ? launch_lds<k_sums_tile<T, Out, kGram, Quarter, false>>(tiles, 256, Quarter::LDS, s, p)
+                 : launch_lds<k_sums_tile<T, Out, kGram, Quarter, true>>(tiles, 256, Quarter::LDS, s, p);
   const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(kSplitWaves, (p.rows.rows + 63) / 64));
   const auto launch = [&](auto size, auto loose) {
     constexpr int S = decltype(size)::value;
-    return launch_lds<k_sums_split<T, Out, kGram, S, decltype(loose)::value>>(count(S), 64 * waves, (size_t)waves * 2 * S * ROW_BYTES,
+    return launch_lds<k_sums_split<T, Out, kGram, S, decltype(loose)::value>>(tiles, 64 * waves, (size_t)waves * 2 * S * ROW_BYTES,
                                                                          s, p);
   };
   using Is64 = std::integral_constant<int, 64>;
   using Is32 = std::integral_constant<int, 32>;
-  if (us_32 < us_64) return tight ? launch(Is32{}, std::false_type{}) : launch(Is32{}, std::true_type{});
+  if (plan.size == 32) return tight ? launch(Is32{}, std::false_type{}) : launch(Is32{}, std::true_type{});
   return tight ? launch(Is64{}, std::false_type{}) : launch(Is64{}, std::true_type{});
 }
 

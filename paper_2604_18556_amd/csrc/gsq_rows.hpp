@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "gsq_plan.h"
 #include "gsq_product.h"
 
 namespace gsq {
@@ -103,10 +104,7 @@ __device__ __forceinline__ bool find_panel(const GroupRows& g, int height, int64
   return false;
 }
 
-// Most panels there can be, for the grid.
-inline int64_t most_panels(const GroupRows& g, int64_t height) {
-  return g.rows / height + (g.rows < g.groups ? g.rows : g.groups);
-}
+inline int64_t most_panels(const GroupRows& g, int64_t height) { return gsq::most_panels(g.rows, g.groups, height); }
 
 }  // namespace
 }  // namespace gsq

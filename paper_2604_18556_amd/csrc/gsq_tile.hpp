@@ -7,6 +7,7 @@
 #include <type_traits>
 #include <utility>
 
+#include "gsq_plan.h"
 #include "gsq_rows.hpp"
 #include "gsq_slab.hpp"
 
@@ -479,42 +480,6 @@ hipError_t launch_ring(int64_t blocks, hipStream_t s, const Args&... args) {
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-
-int tiles_of(int n, int tile) { return (n + tile - 1) / tile; }
-
-// How a product of rows is cut: panels of `height` rows and `width` columns, by whole workgroups (ring) or by
-// wavefronts that share the sum (split).
-struct RowsPlan {
-  bool split;
-  int height, width;
-};
-
-// Microseconds of a tile: its start, and each slab (128 bytes of k) on an empty GPU and with a tile on each of
-// 256 CUs.
-struct TileCost {
-  int height, width;
-  double start, alone, full;
-};
-
-// The cheapest of several tiles: a launch, and a tile's time for each round of 256 tiles.  The groups' last
-// panels are taken to be half full.
-template <int N>
-RowsPlan cheapest(const GroupRows& r, int cols, int slabs, const TileCost (&costs)[N], bool split, double& best,
-                  RowsPlan plan) {
-  const double few = (double)(r.rows < r.groups ? r.rows : r.groups);
-  for (const TileCost& c : costs) {
-    const double panels = r.groups == 1 ? (double)((r.rows + c.height - 1) / c.height) : r.rows / (double)c.height + few / 2;
-    const double tiles = panels * tiles_of(cols, c.width), rounds = tiles / 256;
-    const double whole = rounds < 1 ? 1 : r.groups == 1 ? (double)(int64_t)(rounds + 0.999) : rounds;
-    const double each = c.alone + (c.full - c.alone) * (rounds < 1 ? rounds : 1);
-    const double us = 4 + whole * (c.start + slabs * each);
-    if (us < best) {
-      best = us;
-      plan = {split, c.height, c.width};
-    }
-  }
-  return plan;
-}
 
 // Results can be stored four at a time: whole rows of them, at aligned addresses.
 bool four_at_once(const void* out, int32_t dtype, int32_t cols) {
