@@ -1,0 +1,144 @@
+"""The products' large tiles, each at sizes where the rules choose it (product_cases.py).
+
+Inputs are small whole numbers, and the packed weights have powers of two as scales, so that every product and sum
+is exact in fp32: the outputs must be the 64-bit reference's, rounded once, bit for bit.
+"""
+import numpy as np
+import pytest
+
+from oracle import pack as refpack
+from paper_2604_18556_amd import binding as B
+
+import product_cases as cases
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
+DTYPES = pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+FIRST, BEHIND = 5, 9         # rows before the first group and behind the last
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    B.load()
+    return torch.device("cuda:0")
+
+
+def generator(dev, *seed):
+    return torch.Generator(device=dev).manual_seed(sum(17 ** k * v for k, v in enumerate(seed)))
+
+
+def numbers(gen, *shape, top=1):
+    return torch.randint(-top, top + 1, shape, generator=gen, device=gen.device, dtype=torch.int8)
+
+
+def moved(t, shift):
+    """A copy of t that begins `shift` elements past an aligned address."""
+    m = torch.zeros(t.numel() + shift, dtype=t.dtype, device=t.device)[shift:].view(t.shape)
+    return m.copy_(t)
+
+
+def offsets_of(counts, dev):
+    return torch.tensor([FIRST] + list(counts)).cumsum(0).to(dev)
+
+
+def groups_of(counts):
+    ends = np.cumsum([FIRST] + list(counts)).tolist()
+    return list(zip(ends, ends[1:]))
+
+
+@DTYPES
+@pytest.mark.parametrize("case", cases.ROWS, ids=cases.label)
+def test_rows(dev, case, dtype):
+    kind, counts, o, i, shift, _ = case
+    print(f"rows {case} {dtype}", flush=True)
+    gen, e, rows = generator(dev, o, i, sum(counts)), len(counts), FIRST + sum(counts) + BEHIND
+    ks, ns = (o, i) if kind == "input_grad" else (i, o)
+    # sums of whole numbers stay below 2^11, which fp16 holds exactly, but are rounded in bf16
+    a, w = numbers(gen, rows, ks, top=2), numbers(gen, e, o, i, top=2)
+    out = torch.full((rows, ns), 7.0, dtype=dtype, device=dev)
+    off = offsets_of(counts, dev)
+    if kind == "int8":
+        ones = torch.ones(max(rows, e * o), device=dev)
+        B.grouped_forward_i8(moved(a, shift), ones[:rows], moved(w, shift), ones[:e * o].view(e, o), out, offsets=off)
+    else:
+        call = B.grouped_forward if kind == "forward" else B.grouped_input_grad
+        call(moved(a.to(dtype), shift), moved(w.to(dtype), shift), out, offsets=off)
+    for k, (first, end) in enumerate(groups_of(counts)):
+        we = w[k].double() if kind == "input_grad" else w[k].double().t()
+        assert torch.equal(out[first:end], (a[first:end].double() @ we).to(dtype)), k
+    assert (out[:FIRST] == 7).all() and (out[rows - BEHIND:] == 7).all()
+
+
+@DTYPES
+@pytest.mark.parametrize("case", cases.SUMS, ids=cases.label)
+def test_sums(dev, case, dtype):
+    """dW in both types and H, and both added to what is there."""
+    kind, counts, o, i, shift, _ = case
+    print(f"sums {case} {dtype}", flush=True)
+    gen, e, rows = generator(dev, o, i, sum(counts)), len(counts), FIRST + sum(counts) + BEHIND
+    x, off = numbers(gen, rows, i), offsets_of(counts, dev)
+    xd = moved(x.to(dtype), shift)
+    if kind == "gram":
+        y, yd, ends = x, xd, (FP32,)
+    else:
+        y, ends = numbers(gen, rows, o), (dtype, FP32)
+        yd = moved(y.to(dtype), shift)
+
+    def call(out, **how):
+        if kind == "gram":
+            B.gram(xd, out, offsets=off, **how)
+        else:
+            B.grouped_weight_grad(yd, xd, out, offsets=off, **how)
+
+    for end in ends:
+        out = torch.full((e, y.shape[1], i), 7.0, dtype=end, device=dev)
+        call(out)
+        refs = [y[a:b].double().t() @ x[a:b].double() for a, b in groups_of(counts)]
+        for k, ref in enumerate(refs):
+            assert torch.equal(out[k], ref.to(end)), k
+    out.fill_(3.0)
+    call(out, accumulate=True)
+    for k, ref in enumerate(refs):
+        assert torch.equal(out[k], (ref + 3).float()), k
+
+
+def packed_layer(layout, levels, group, batch, o, i, gen):
+    """Random codes, scales that are powers of two, their packed bytes (by the oracle), and the weights."""
+    codes = torch.randint(0, len(levels), (batch, o, i), generator=gen, dtype=torch.uint8)
+    c = codes.numpy()
+    power = lambda lo, hi, *shape: 2.0 ** torch.randint(lo, hi + 1, shape, generator=gen).float()
+    if layout == "superblock":
+        d, sc = power(-4, -3, batch, o, i // 256), power(0, 3, batch, o, i // 16)
+        eff = d.repeat_interleave(16, -1) * sc
+        packed = refpack.pack_superblock(c, d.half().numpy(), sc.numpy().astype(np.uint8))
+    else:
+        eff = power(-4, -1, batch, o, i // group)
+        s = eff.half().numpy()
+        packed = refpack.pack_base3(c, s) if layout == "base3" else refpack.pack_plain(c, s, len(levels), group)
+    w = torch.tensor(levels)[codes.int()]
+    w.view(batch, o, i // group, group).mul_(eff[..., None])
+    return torch.from_numpy(np.ascontiguousarray(packed)), w
+
+
+@pytest.mark.parametrize("case", cases.PACKED, ids=cases.label)
+def test_packed(dev, case):
+    """One handle for rows of both types."""
+    layout, levels, group, counts, o, i, shift, _ = case
+    print(f"packed {case}", flush=True)
+    e, rows = len(counts), FIRST + sum(counts) + BEHIND
+    packed, w = packed_layer(layout, levels, group, e, o, i, generator("cpu", o, i, len(levels)))
+    kept = {"group": B.LAYOUT_GROUP, "base3": B.LAYOUT_BASE3, "superblock": B.LAYOUT_SUPERBLOCK}[layout]
+    lin = B.Linear(B.LayerConfig(o, i, levels, group, e, kept,
+                                 relaxation=B.RELAX_SHIFT if len(levels) > 8 else B.RELAX_GRID), packed.to(dev))
+    x, off, w = numbers(generator(dev, o, i, sum(counts)), rows, i, top=2), offsets_of(counts, dev), w.to(dev)
+    for dtype in (BF16, FP16):
+        y = torch.full((rows, o), 7.0, dtype=dtype, device=dev)
+        lin.forward(moved(x.to(dtype), shift), y, offsets=off)
+        for k, (a, b) in enumerate(groups_of(counts)):
+            assert torch.equal(y[a:b], (x[a:b].double() @ w[k].double().t()).to(dtype)), (dtype, k)
+        assert (y[:FIRST] == 7).all() and (y[rows - BEHIND:] == 7).all()
+    lin.destroy()

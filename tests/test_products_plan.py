@@ -1,0 +1,73 @@
+"""The rules that cut the products into tiles, compiled on their own with the host compiler: the plan of each
+case that the GPU tests run to have a kernel tested."""
+import os
+import subprocess
+
+import pytest
+
+import product_cases as cases
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+PLAN = r"""
+#include "gsq_plan.h"
+#include <cstdio>
+#include <cstring>
+int main() {
+  char kind[32];
+  long long r, g, o, i;
+  int tight;
+  while (std::scanf("%31s %lld %lld %lld %lld %d", kind, &r, &g, &o, &i, &tight) == 6) {
+    const auto is = [&](const char* s) { return !std::strcmp(kind, s); };
+    if (is("weight_grad") || is("gram")) {
+      const gsq::SumsPlan p = gsq::plan_sums(r, g, is("gram") ? i : o, i, tight, is("gram"));
+      std::printf("%s %d\n", p.split ? "split" : "ring", p.size);
+      continue;
+    }
+    const int slabs = (int)gsq::tiles_of(is("input_grad") ? o : i, is("int8") ? 128 : 64);
+    const gsq::RowsPlan p = is("packed") ? gsq::plan_packed(r, g, o, (int)gsq::tiles_of(i, 128), tight)
+                                         : gsq::plan_rows(r, g, is("input_grad") ? i : o, slabs, tight,
+                                                          is("input_grad"), is("int8"));
+    std::printf("%s %dx%d\n", p.split ? "split" : "ring", p.height, p.width);
+  }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def plans(tmp_path_factory):
+    """(kind, rows, groups, O, I, tight) of many products to their plans."""
+    folder = tmp_path_factory.mktemp("plan")
+    src, exe = folder / "plan.cpp", folder / "plan"
+    src.write_text(PLAN)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", os.path.join(ROOT, "paper_2604_18556_amd", "csrc"), str(src),
+                    "-o", str(exe)], check=True, capture_output=True, text=True)
+
+    def ask(products):
+        text = "".join(" ".join(str(int(v) if isinstance(v, bool) else v) for v in p) + "\n" for p in products)
+        return subprocess.run([str(exe)], input=text, check=True, capture_output=True, text=True).stdout.splitlines()
+    return ask
+
+
+def test_plans_of_the_tested_cases(plans):
+    listed = [(c[0], sum(c[1]), len(c[1]), c[2], c[3], cases.tight(c[0], *c[2:5])) for c in cases.ROWS + cases.SUMS]
+    listed += [("packed", sum(c[3]), len(c[3]), c[4], c[5], c[6] == 0) for c in cases.PACKED]
+    want = [c[-1] for c in cases.ROWS + cases.SUMS + cases.PACKED]
+    got = plans(listed)
+    wrong = [(p, g, w) for p, g, w in zip(listed, got, want) if g != w]
+    assert len(got) == len(want) and not wrong
+
+
+def test_every_large_tile_has_a_case():
+    rows = {(c[0], c[-1]) for c in cases.ROWS}
+    for kind in ("forward", "input_grad", "int8"):
+        for plan in ("ring 256x256", "ring 128x256", "ring 64x256", "ring 128x128"):
+            assert (kind, plan) in rows, (kind, plan)
+    sums = {(c[0], c[-1], cases.tight(c[0], *c[2:5])) for c in cases.SUMS}
+    for kind in ("weight_grad", "gram"):
+        assert {(kind, "ring 256", True), (kind, "ring 128", True), (kind, "ring 128", False)} <= sums
+    bits = {2: 1, 3: 2, 4: 2, 8: 3, 16: 4}
+    packed = {(3 if c[0] == "superblock" else bits[len(c[1])], c[0] == "superblock" or c[2] == 16) for c in cases.PACKED}
+    assert packed == {(b, fine) for b in (1, 2, 3, 4) for fine in (False, True)}
+    for b in (2, 3, 4):
+        assert {c[-1] for c in cases.PACKED if bits[len(c[1])] == b} >= {"ring 256x256", "ring 128x256", "ring 64x256"}
