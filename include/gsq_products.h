@@ -17,9 +17,10 @@
  * same device, though not between the two sides of a size rule.  Infinities and NaN go through as the
  * arithmetic has them, within the rows and channels they belong to.  Pointers need the alignment of their
  * elements only; arrays with 16-byte aligned bases and rows are read faster.  Limits (GSQ_EINVAL):
- * groups <= 65535, rows <= 2^29, out_features and in_features <= 2^21, and the tiles of one launch (an
- * output of more than 2^32 elements may pass them).  The device that the pointers belong to has to be
- * current.
+ * groups <= 65535, rows <= 2^29, out_features and in_features <= 2^21, and the tiles of one launch.  Those
+ * are never too many while (rows / 64 + min(rows, groups)) ceil(n / 64) < 2^23, n being the columns of the
+ * output, or for sums over rows (dW, H) groups ceil(O / 64) ceil(I / 64) < 2^23.  The device that the
+ * pointers belong to has to be current.
  */
 #ifndef GSQ_PRODUCTS_H
 #define GSQ_PRODUCTS_H

@@ -15,8 +15,15 @@ inline int64_t most_panels(int64_t rows, int64_t groups, int64_t height) {
   return rows / height + std::min(rows, groups);
 }
 
+// What one launch holds: fewer than 2^32 threads in the grid's one dimension.
+inline bool fits_launch(int64_t tiles, int64_t threads) { return tiles * threads < (int64_t)1 << 32; }
+
+// Wavefronts that share a tile's sum, at most: one for each of its slabs (packed codes: units) up to these.  Whole
+// workgroups have four.
+constexpr int kSplitWaves = 8, kFewWaves = 16, kRingWaves = 4;
+
 // How a product of rows is cut: panels of `height` rows and `width` columns, by whole workgroups (ring) or by
-// wavefronts that share the sum (split).
+// wavefronts that share the sum (split).  No height: nothing fits a launch.
 struct RowsPlan {
   bool split;
   int height, width;
@@ -29,13 +36,14 @@ struct TileCost {
   double start, alone, full;
 };
 
-// The cheapest of several tiles: a launch, and a tile's time for each round of 256 tiles.  The groups' last
-// panels are taken to be half full.
+// The cheapest of several tiles of `waves` wavefronts that fit one launch: a launch, and a tile's time for each round
+// of 256 tiles.  The groups' last panels are taken to be half full.
 template <int N>
-RowsPlan cheapest(int64_t rows, int64_t groups, int cols, int slabs, const TileCost (&costs)[N], bool split, double& best,
-                  RowsPlan plan) {
+RowsPlan cheapest(int64_t rows, int64_t groups, int cols, int slabs, const TileCost (&costs)[N], bool split, int waves,
+                  double& best, RowsPlan plan) {
   const double few = (double)std::min(rows, groups);
   for (const TileCost& c : costs) {
+    if (!fits_launch(most_panels(rows, groups, c.height) * tiles_of(cols, c.width), 64 * waves)) continue;
     const double panels = groups == 1 ? (double)tiles_of(rows, c.height) : rows / (double)c.height + few / 2;
     const double tiles = panels * tiles_of(cols, c.width), rounds = tiles / 256;
     const double whole = rounds < 1 ? 1 : groups == 1 ? (double)(int64_t)(rounds + 0.999) : rounds;
@@ -59,21 +67,22 @@ RowsPlan cheapest(int64_t rows, int64_t groups, int cols, int slabs, const TileC
 // and 8192 x 8192 at one row by 16 x 64 | 16 x 16 split 30 | 28, at 64 rows 50 | 68.  8-bit integers take
 // longer in large tiles, which the power of the matrix cores bounds.
 inline RowsPlan plan_rows(int64_t rows, int64_t groups, int cols, int slabs, bool tight, bool across, bool bytes) {
+  const int waves = std::min(slabs, kSplitWaves);
   double best = 1e30;
   if (!tight) {
     // from any addresses (I 4001, O 8190; 64 x 64 split | 128 x 128): 64 rows 32 | 72, 512 rows 118 | 78, 4096 rows
     // 866 | 378
     const TileCost small[] = {{64, 64, 1, 0.17, 0.42}, {64, 16, 1, 0.1, 0.21}, {16, 64, 1, 0.07, 0.15}, {16, 16, 0.5, 0.025, 0.08}};
     const TileCost large[] = {{128, 128, 2, across ? 2.0 : 0.85, across ? 1.05 : 0.75}};
-    const RowsPlan plan = cheapest(rows, groups, cols, slabs, small, true, best, RowsPlan{});
-    return cheapest(rows, groups, cols, slabs, large, false, best, plan);
+    const RowsPlan plan = cheapest(rows, groups, cols, slabs, small, true, waves, best, RowsPlan{});
+    return cheapest(rows, groups, cols, slabs, large, false, kRingWaves, best, plan);
   }
   const double more = bytes ? 1.4 : 1;
   const TileCost small[] = {{64, 64, 1, 0.165, 0.22}, {64, 16, 1, 0.1, 0.115}, {16, 64, 1, 0.06, 0.1}, {16, 16, 0.5, 0.02, 0.055}};
   const TileCost large[] = {{256, 256, 3, 1.15 * more, 1.6 * more}, {128, 256, 2, 0.7 * more, 0.95 * more},
                             {64, 256, 1.5, 0.43 * more, 0.72 * more}};
-  const RowsPlan plan = cheapest(rows, groups, cols, slabs, small, true, best, RowsPlan{});
-  return cheapest(rows, groups, cols, slabs, large, false, best, plan);
+  const RowsPlan plan = cheapest(rows, groups, cols, slabs, small, true, waves, best, RowsPlan{});
+  return cheapest(rows, groups, cols, slabs, large, false, kRingWaves, best, plan);
 }
 
 // y with the packed codes, by the same reckoning (us at 2 bits; 16 | 64 channels shared | panels of 64 | 128 | 256
@@ -86,24 +95,32 @@ inline RowsPlan plan_rows(int64_t rows, int64_t groups, int cols, int slabs, boo
 // 3 bits take 4 to 10 % longer, 4 bits 15 to 40 %.
 inline RowsPlan plan_packed(int64_t rows, int64_t groups, int O, int blocks, bool tight) {
   const double each = (double)rows / std::min(rows, groups);   // rows of a group
-  const int slabs = 2 * blocks;
+  const int slabs = 2 * blocks, few_waves = std::min(blocks, kFewWaves);
   const TileCost large[] = {{256, 256, 3, 1.4, 1.65}, {128, 256, 2, 1.0, 1.15}, {64, 256, 1.5, 0.72, 0.95}};
   const TileCost shared[] = {{64, 64, 1, each <= 16 ? 0.07 : each <= 32 ? 0.095 : 0.15,
                               each <= 16 ? 0.09 : each <= 32 ? 0.12 : 0.2}};
-  const TileCost few[] = {{16, 16, 0.7, 0.02, 0.03}};
   double best = 1e30;
-  RowsPlan plan = cheapest(rows, groups, O, slabs, few, true, best, RowsPlan{});
-  if (tight) {
-    plan = cheapest(rows, groups, O, slabs, shared, true, best, plan);
-    plan = cheapest(rows, groups, O, slabs, large, false, best, plan);
+  if (!tight) {
+    // x from any address (2 bits; 16 x 16 shared | 128 rows by workgroups):
+    //   I 4096, O 4096: 1 row 8 | 83; 64 rows 25 | 83; 256 rows 90 | 85; 2001 rows 683 | 99 (aligned 81); 4096 rows
+    //     1386 | 184
+    //   I 4096, O 14336: 64 rows 78 | 84; 512 rows 611 | 97.  I 14336, O 4096: 1 row 18 | 267; 256 rows 246 | 295
+    // (3 bits 2 to 8 % longer, 4 bits 5 to 25 %)
+    const TileCost few[] = {{16, 16, 0.7, 0.04, 0.068}};
+    const TileCost loose[] = {{128, 256, 2, 1.2, 1.42}};
+    const RowsPlan plan = cheapest(rows, groups, O, slabs, few, true, few_waves, best, RowsPlan{});
+    return cheapest(rows, groups, O, slabs, loose, false, kRingWaves, best, plan);
   }
-  return plan;
+  const TileCost few[] = {{16, 16, 0.7, 0.02, 0.03}};
+  RowsPlan plan = cheapest(rows, groups, O, slabs, few, true, few_waves, best, RowsPlan{});
+  plan = cheapest(rows, groups, O, slabs, shared, true, std::min(blocks, kSplitWaves), best, plan);
+  return cheapest(rows, groups, O, slabs, large, false, kRingWaves, best, plan);
 }
 
-// How a sum over rows is cut: tiles of `size` x `size`.
+// How a sum over rows is cut: tiles of `size` x `size`.  Where nothing fits a launch, one that does not.
 struct SumsPlan {
   bool split;
-  int size;
+  int size, waves;
 };
 
 // Tiles of the sums of all groups; of H those on and above the diagonal, two rows of them taken as one.
@@ -124,8 +141,11 @@ inline int64_t sum_tiles(int64_t groups, int O, int I, bool gram, int size) {
 // - | 59 | 51 | -, 1024 rows 156 | 106 | 202 | 306, 16384 rows 1093 | 1857 | - | -.
 inline SumsPlan plan_sums(int64_t rows, int64_t groups, int O, int I, bool tight, bool gram) {
   const double slabs = (double)rows / 64 / groups;
+  const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(kSplitWaves, tiles_of(rows, 64)));
   const auto cost = [&](int size, double start, double more_start, double alone, double full) {
-    const double rounds = sum_tiles(groups, O, I, gram, size) / 256.0, load = std::min(1.0, rounds);
+    const int64_t tiles = sum_tiles(groups, O, I, gram, size);
+    if (!fits_launch(tiles, 64 * (size < 128 ? waves : kRingWaves))) return 1e30;
+    const double rounds = tiles / 256.0, load = std::min(1.0, rounds);
     const double whole = groups == 1 && size != 128 ? std::ceil(rounds) : rounds;
     return std::max(1.0, whole) * (start + more_start * load + (slabs + 0.5) * (alone + (full - alone) * load));
   };
@@ -134,9 +154,9 @@ inline SumsPlan plan_sums(int64_t rows, int64_t groups, int O, int I, bool tight
   const double us_quarter = cost(128, gram ? 6.5 : 2, 0, 0.45 * far, 0.5 * far);
   const double us_64 = cost(64, gram ? 1.4 : 0.7, 0, 0.17, 0.23), us_32 = cost(32, gram ? 0.3 : 0.15, 0, 0.08, 0.14);
   const double us_split = std::min(us_64, us_32);
-  if (us_whole < std::min(us_quarter, us_split)) return {false, 256};
-  if (us_quarter < us_split) return {false, 128};
-  return {true, us_32 < us_64 ? 32 : 64};
+  if (us_whole < std::min(us_quarter, us_split)) return {false, 256, kRingWaves};
+  if (us_quarter < us_split) return {false, 128, kRingWaves};
+  return {true, us_32 < us_64 ? 32 : 64, waves};
 }
 
 }  // namespace gsq

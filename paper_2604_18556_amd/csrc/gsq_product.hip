@@ -332,6 +332,7 @@ hipError_t launch_rows(ProductArgs p, hipStream_t s) {
   p.vector_out = four_at_once(p.out, p.out_dtype, ns);
   const bool tight = p.O % (kForm == kForward ? 1 : unit) == 0 && p.I % unit == 0 && aligned16(p.a) && aligned16(p.b);
   const RowsPlan plan = plan_rows(p.rows.rows, p.rows.groups, ns, slabs, tight, kForm == kInputGrad, T::kDtype < 0);
+  if (!plan.height) return hipErrorInvalidConfiguration;
   if (plan.split) return tight ? launch_rows_split<T, kForm, false>(p, plan, s) : launch_rows_split<T, kForm, true>(p, plan, s);
   if (!tight)
     return launch_lds<k_rows_loose<T, kForm>>(most_panels(p.rows, Quarter::TM) * tiles_of(ns, Quarter::TN), 256,
@@ -351,7 +352,7 @@ hipError_t launch_sums(ProductArgs p, hipStream_t s) {
   if (!plan.split)
     return tight ? launch_lds<k_sums_tile<T, Out, kGram, Quarter, false>>(tiles, 256, Quarter::LDS, s, p)
                  : launch_lds<k_sums_tile<T, Out, kGram, Quarter, true>>(tiles, 256, Quarter::LDS, s, p);
-  const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(kSplitWaves, (p.rows.rows + 63) / 64));
+  const int waves = plan.waves;
   const auto launch = [&](auto size, auto loose) {
     constexpr int S = decltype(size)::value;
     return launch_lds<k_sums_split<T, Out, kGram, S, decltype(loose)::value>>(tiles, 64 * waves, (size_t)waves * 2 * S * ROW_BYTES,

@@ -12,8 +12,6 @@
 namespace gsq {
 namespace {
 
-constexpr int kSplitWaves = 8;       // at most, for one tile
-
 // 16 bytes from any address, of which the first n (<= 16 / sizeof(E)) elements are in bounds and the others
 // become zero.
 template <class E>

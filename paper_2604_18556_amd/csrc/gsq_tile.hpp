@@ -457,7 +457,7 @@ __device__ __forceinline__ bool find_rows_tile(const GroupRows& rows, int height
 // A kernel that uses more LDS than the default limit needs leave for it, once on each device.
 template <auto kKernel, class... Args>
 hipError_t launch_lds(int64_t blocks, int threads, size_t lds, hipStream_t s, const Args&... args) {
-  if (blocks * threads >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;   // the limit of grid.x
+  if (!fits_launch(blocks, threads)) return hipErrorInvalidConfiguration;
   if (lds > 64 * 1024) {
     static std::atomic<uint64_t> leave{0};   // a bit per device
     int dev = 0;

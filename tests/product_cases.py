@@ -62,6 +62,16 @@ PACKED = [
     ("group", L16, 16, [900, 30, 0, 200, 370, 77], 8200, 176, 0, "ring 256x256"),
     ("group", L16, 128, [1100], 4100, 1152, 0, "ring 128x256"),
     ("group", L16, 256, [1000], 4090, 768, 0, "ring 64x256"),
+    # x from an odd address
+    ("group", L2, 128, [1100], 4100, 1280, 1, "ring 128x256"),
+    ("group", L2, 16, [2100], 8201, 48, 1, "ring 128x256"),
+    ("base3", L3, 64, [900, 30, 0, 200, 370, 77], 4104, 320, 3, "ring 128x256"),
+    ("group", L4, 16, [700], 4100, 560, 1, "ring 128x256"),
+    ("group", L8, 64, [900, 30, 0, 200, 370, 77], 4104, 576, 7, "ring 128x256"),
+    ("superblock", L8, 16, [900, 30, 0, 200, 370, 77], 4104, 256, 1, "ring 128x256"),
+    ("group", L16, 64, [1100], 4100, 64, 1, "ring 128x256"),
+    ("group", L16, 16, [700], 4111, 176, 2, "ring 128x256"),
+    ("group", L8, 128, [70, 40, 0, 5, 17], 520, 640, 1, "split 16x16"),
 ]
 
 

@@ -142,3 +142,23 @@ def test_packed(dev, case):
             assert torch.equal(y[a:b], (x[a:b].double() @ w[k].double().t()).to(dtype)), (dtype, k)
         assert (y[:FIRST] == 7).all() and (y[rows - BEHIND:] == 7).all()
     lin.destroy()
+
+
+def test_packed_rows_beyond_small_tiles(dev):
+    """2^30 results of an x that begins at an odd element: as many 16 x 16 tiles would pass a launch."""
+    rows, o, i = 1 << 16, 1 << 14, 2048
+    levels = (-1.5, -0.5, 0.5, 1.5)
+    cfg = B.LayerConfig(o, i, levels, 256)
+    packed = torch.randint(0, 256, (B.packed_size(cfg),), generator=generator(dev, 3), device=dev, dtype=torch.uint8)
+    packed[-2 * o * i // 256:] = torch.ones(o * i // 256, dtype=FP16, device=dev).view(torch.uint8)
+    lin = B.Linear(cfg, packed)
+    x = numbers(generator(dev, 4), rows, i).to(BF16)
+    want, got = torch.empty(rows, o, dtype=BF16, device=dev), torch.empty(rows, o, dtype=BF16, device=dev)
+    lin.forward(x, want)
+    lin.forward(moved(x, 1), got)
+    assert torch.equal(got, want)
+    code = packed[:o * i // 4].view(o, i // 4, 1) >> torch.tensor([0, 2, 4, 6], dtype=torch.uint8, device=dev) & 3
+    w = torch.tensor(levels, device=dev)[code.int()].view(o, i)
+    for r in (0, 1, 777, rows - 2, rows - 1):
+        assert torch.equal(got[r], (w.double() @ x[r].double()).to(BF16))
+    lin.destroy()

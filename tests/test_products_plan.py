@@ -71,3 +71,52 @@ def test_every_large_tile_has_a_case():
     assert packed == {(b, fine) for b in (1, 2, 3, 4) for fine in (False, True)}
     for b in (2, 3, 4):
         assert {c[-1] for c in cases.PACKED if bits[len(c[1])] == b} >= {"ring 256x256", "ring 128x256", "ring 64x256"}
+    odd = {(3 if c[0] == "superblock" else bits[len(c[1])], c[0] == "superblock" or c[2] == 16)
+           for c in cases.PACKED if c[6] and c[-1] == "ring 128x256"}
+    assert odd == packed
+
+
+LIMITS = r"""
+#include "gsq_plan.h"
+#include <cstdio>
+#include <random>
+std::mt19937_64 gen(1);
+int64_t draw(double bits) { return (int64_t)std::exp2(std::uniform_real_distribution<double>(0, bits)(gen)); }
+int main() {
+  long taken = 0, wrong = 0;
+  const auto note = [&](const char* what, bool must, bool fits, int64_t r, int64_t g, int64_t o, int64_t i) {
+    taken += must;
+    if (must && !fits && ++wrong < 10)
+      std::printf("%s rows %lld groups %lld O %lld I %lld\n", what, (long long)r, (long long)g, (long long)o, (long long)i);
+  };
+  for (int k = 0; k < 400000; ++k) {
+    const int64_t r = draw(29.01), g = k & 1 ? 1 : draw(16), o = draw(21.01), i = draw(21.01);
+    const bool tight = gen() & 1, flag = gen() & 1, bytes = gen() & 1;
+    using namespace gsq;
+    const auto rows_fit = [&](const RowsPlan& p, int waves) {
+      return p.height && fits_launch(most_panels(r, g, p.height) * tiles_of(o, p.width), 64 * (p.split ? waves : 4));
+    };
+    const bool must = (r / 64 + std::min(r, g)) * tiles_of(o, 64) < (int64_t)1 << 23;
+    const int slabs = (int)tiles_of(i, bytes ? 128 : 64), blocks = (int)tiles_of(i, 128);
+    note("rows", must, rows_fit(plan_rows(r, g, o, slabs, tight, flag && !bytes, bytes), std::min(slabs, 8)), r, g, o, i);
+    const RowsPlan p = plan_packed(r, g, o, blocks, tight);
+    note("packed", must, rows_fit(p, std::min(blocks, p.height == 16 ? 16 : 8)), r, g, o, i);
+    const SumsPlan s = plan_sums(r, g, flag ? i : o, i, tight, flag);
+    note("sums", g * tiles_of(flag ? i : o, 64) * tiles_of(i, 64) < (int64_t)1 << 23,
+         fits_launch(sum_tiles(g, flag ? i : o, i, flag, s.size), 64 * s.waves), r, g, o, i);
+  }
+  std::printf("%ld %ld\n", taken, wrong);
+}
+"""
+
+
+def test_products_below_the_stated_limit_fit_a_launch(tmp_path):
+    """The header's bound on the tiles, over sizes up to its limits: what is below it has a plan that one launch
+    holds."""
+    src, exe = tmp_path / "limits.cpp", tmp_path / "limits"
+    src.write_text(LIMITS)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", os.path.join(ROOT, "paper_2604_18556_amd", "csrc"), str(src),
+                    "-o", str(exe)], check=True, capture_output=True, text=True)
+    *faults, last = subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.splitlines()
+    taken, wrong = map(int, last.split())
+    assert taken > 100000 and wrong == 0, faults
