@@ -48,12 +48,15 @@ __device__ __forceinline__ uint32_t packed_code(const uint8_t* p, int layout, in
 
 __device__ __forceinline__ uint16_t two_bytes(const uint8_t* p) { return p[0] | (uint16_t)(p[1] << 8); }
 
-// One thread per lane of a unit: its 32 codes.
-__global__ __launch_bounds__(256) void k_unpack_codes(const uint8_t* __restrict__ packed, int layout,
-                                                      int packed_bits, PackedLayer L, int64_t lanes,
-                                                      uint32_t* __restrict__ codes) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= lanes) return;
+// A thread's elements of `count`, with unpack_blocks() workgroups.
+template <class F>
+__device__ __forceinline__ void each_of(int64_t count, F f) {
+  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < count; at += (int64_t)gridDim.x * 256) f(at);
+}
+
+// A lane of a unit: its 32 codes.
+__device__ __forceinline__ void unpack_codes(const uint8_t* packed, int layout, int packed_bits, const PackedLayer& L,
+                                             int64_t at, uint32_t* codes) {
   const int lane = (int)(at & 63);
   const int64_t unit = at >> 6;
   const int kb = (int)(unit % L.blocks);
@@ -67,6 +70,11 @@ __global__ __launch_bounds__(256) void k_unpack_codes(const uint8_t* __restrict_
       place_code(words, L.bits, j, min(c, (uint32_t)L.n_levels - 1));
     }
   for (int k = 0; k < L.bits; ++k) codes[at * L.bits + k] = words[k];
+}
+__global__ __launch_bounds__(256) void k_unpack_codes(const uint8_t* __restrict__ packed, int layout,
+                                                      int packed_bits, PackedLayer L, int64_t lanes,
+                                                      uint32_t* __restrict__ codes) {
+  each_of(lanes, [&](int64_t at) { unpack_codes(packed, layout, packed_bits, L, at, codes); });
 }
 
 // Where the scale of channel n of a tile and inputs 16 j .. is kept: for groups of 16 with the unit's lanes,
@@ -86,38 +94,38 @@ __device__ __forceinline__ void place_of_scale(const PackedLayer& L, bool fine, 
   }
 }
 
-// One thread per kept scale, zero where there is no channel or group.
+// The kept scales, zero where there is no channel or group.
 __global__ __launch_bounds__(256) void k_unpack_scales(const uint8_t* __restrict__ packed, int layout,
                                                        PackedLayer L, int64_t at_byte, int64_t count,
                                                        uint16_t* __restrict__ scales) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= count) return;
-  int64_t tile;
-  int n, g;
-  place_of_scale(L, L.gs == 16, at, tile, n, g);
-  const int64_t e = tile / L.tiles, o = (tile % L.tiles) * 16 + n;
-  uint16_t v = 0;
-  if (o < L.O && g < L.I / L.gs) {
-    const int64_t k = (e * L.O + o) * (L.I / L.gs) + g;
-    v = two_bytes(layout == GSQ_LAYOUT_SUPERBLOCK ? packed + k * 110 : packed + at_byte + 2 * k);
-  }
-  scales[at] = v;
+  each_of(count, [&](int64_t at) {
+    int64_t tile;
+    int n, g;
+    place_of_scale(L, L.gs == 16, at, tile, n, g);
+    const int64_t e = tile / L.tiles, o = (tile % L.tiles) * 16 + n;
+    uint16_t v = 0;
+    if (o < L.O && g < L.I / L.gs) {
+      const int64_t k = (e * L.O + o) * (L.I / L.gs) + g;
+      v = two_bytes(layout == GSQ_LAYOUT_SUPERBLOCK ? packed + k * 110 : packed + at_byte + 2 * k);
+    }
+    scales[at] = v;
+  });
 }
 
 __global__ __launch_bounds__(256) void k_unpack_sub(const uint8_t* __restrict__ packed, PackedLayer L,
                                                     int64_t count, uint8_t* __restrict__ sub) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= count) return;
-  int64_t tile;
-  int n, g;
-  place_of_scale(L, true, at, tile, n, g);
-  const int64_t e = tile / L.tiles, o = (tile % L.tiles) * 16 + n;
-  uint32_t v = 0;
-  if (o < L.O && g < L.I / 16) {
-    const int64_t rec = (e * L.O + o) * (L.I / 256) + g / 16;
-    v = bit_field(packed + rec * 110 + 2, (g & 15) * 6, 6);
-  }
-  sub[at] = (uint8_t)v;
+  each_of(count, [&](int64_t at) {
+    int64_t tile;
+    int n, g;
+    place_of_scale(L, true, at, tile, n, g);
+    const int64_t e = tile / L.tiles, o = (tile % L.tiles) * 16 + n;
+    uint32_t v = 0;
+    if (o < L.O && g < L.I / 16) {
+      const int64_t rec = (e * L.O + o) * (L.I / 256) + g / 16;
+      v = bit_field(packed + rec * 110 + 2, (g & 15) * 6, 6);
+    }
+    sub[at] = (uint8_t)v;
+  });
 }
 
 // scale * level rounded to fp32, for a second rounding to the type of x.  The empty asm keeps the compiler
@@ -418,17 +426,20 @@ __global__ __launch_bounds__(256, 1) void k_packed_loose(PackedLayer L, GroupRow
 
 hipError_t launch_unpack_layer(const gsq_config& cfg, const uint8_t* packed, const PackedLayer& L,
                                hipStream_t s) {
-  const auto blocks = [](int64_t n) { return (unsigned)((n + 255) / 256); };
   const int64_t tiles = (int64_t)cfg.batch * L.tiles, weights = (int64_t)cfg.batch * L.O * L.I;
   const int packed_bits = cfg.layout == GSQ_LAYOUT_SUPERBLOCK ? 3 : L.bits;
   const int64_t lanes = tiles * L.blocks * 64;
   const int64_t scales = tiles * (L.gs == 16 ? (int64_t)L.blocks * 128 : (int64_t)L.scale_groups * 16);
-  k_unpack_codes<<<blocks(lanes), 256, 0, s>>>(packed, cfg.layout, packed_bits, L, lanes,
-                                               const_cast<uint32_t*>(L.codes));
+  k_unpack_codes<<<unpack_blocks(lanes), 256, 0, s>>>(packed, cfg.layout, packed_bits, L, lanes,
+                                                      const_cast<uint32_t*>(L.codes));
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   const int64_t at_byte = cfg.layout == GSQ_LAYOUT_BASE3 ? (weights + 4) / 5 : weights * packed_bits / 8;
-  k_unpack_scales<<<blocks(scales), 256, 0, s>>>(packed, cfg.layout, L, at_byte, scales,
-                                                 const_cast<uint16_t*>(L.scales));
-  if (L.sub) k_unpack_sub<<<blocks(lanes * 2), 256, 0, s>>>(packed, L, lanes * 2, const_cast<uint8_t*>(L.sub));
+  k_unpack_scales<<<unpack_blocks(scales), 256, 0, s>>>(packed, cfg.layout, L, at_byte, scales,
+                                                        const_cast<uint16_t*>(L.scales));
+  e = hipGetLastError();
+  if (e != hipSuccess || !L.sub) return e;
+  k_unpack_sub<<<unpack_blocks(lanes * 2), 256, 0, s>>>(packed, L, lanes * 2, const_cast<uint8_t*>(L.sub));
   return hipGetLastError();
 }
 

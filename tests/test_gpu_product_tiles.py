@@ -162,3 +162,46 @@ def test_packed_rows_beyond_small_tiles(dev):
     for r in (0, 1, 777, rows - 2, rows - 1):
         assert torch.equal(got[r], (w.double() @ x[r].double()).to(BF16))
     lin.destroy()
+
+
+def fields(data, width, count):
+    """`count` little-endian fields of `width` bits in the bytes of the last dimension."""
+    word = torch.zeros(data.shape[:-1], dtype=torch.int64, device=data.device)
+    for k in range(data.shape[-1]):
+        word |= data[..., k].long() << (8 * k)
+    return word[..., None] >> torch.arange(count, device=data.device) * width & (1 << width) - 1
+
+
+@pytest.mark.parametrize("layout,levels,group,i", [("group", L, g, i) for L, g, i in ((cases.L2, 64, 8192), (cases.L4, 16, 4096))]
+                         + [("superblock", cases.L8, 16, 4096)])
+def test_large_packed_layers_are_laid_out_whole(dev, layout, levels, group, i):
+    """More codes, scales or sub-scales than threads lay out: the last layer's weights as much as the first's."""
+    e, o = 5, 4096
+    super_block = layout == "superblock"
+    cfg = B.LayerConfig(o, i, levels, group, e, B.LAYOUT_SUPERBLOCK if super_block else B.LAYOUT_GROUP)
+    assert e * o * i // 32 * (1 if len(levels) == 2 else 2) > 16384 * 256
+    packed = torch.randint(0, 256, (B.packed_size(cfg),), generator=generator(dev, i, group), device=dev, dtype=torch.uint8)
+    power = lambda n: (2.0 ** torch.randint(-4, 0, (n, 1), generator=generator(dev, 7), device=dev)).half().view(torch.uint8)
+    if super_block:
+        rec = packed.view(-1, 110)
+        rec[:, :2] = power(rec.shape[0])
+        rec = rec.view(e, -1, 110)
+    else:
+        width = 1 if len(levels) == 2 else 2
+        codes, scales = packed[:e * o * i * width // 8].view(e, -1, width), packed[e * o * i * width // 8:]
+        scales.copy_(power(e * o * i // group).view(-1))
+        scales = scales.view(torch.float16).view(e, -1)
+    lin = B.Linear(cfg, packed)
+    x = numbers(generator(dev, 5), 2 * e, i).to(BF16)
+    y = torch.empty(2 * e, o, dtype=BF16, device=dev)
+    lin.forward(x, y, offsets=torch.arange(0, 2 * e + 1, 2, device=dev))
+    for k in (0, e - 1):
+        if super_block:
+            s = rec[k, :, :2].contiguous().view(torch.float16).float() * fields(rec[k, :, 2:14].view(-1, 4, 3), 6, 4).view(-1, 16)
+            c = fields(rec[k, :, 14:].view(-1, 32, 3), 3, 8)
+        else:
+            s, c = scales[k].float(), fields(codes[k], width, 8)
+        w = torch.tensor(levels, device=dev)[c.view(-1, group)] * s.view(-1, 1)
+        w = w.to(BF16).double().view(o, i)
+        assert torch.equal(y[2 * k:2 * k + 2], (x[2 * k:2 * k + 2].double() @ w.t()).to(BF16)), k
+    lin.destroy()

@@ -120,3 +120,28 @@ def test_products_below_the_stated_limit_fit_a_launch(tmp_path):
     *faults, last = subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.splitlines()
     taken, wrong = map(int, last.split())
     assert taken > 100000 and wrong == 0, faults
+
+
+BLOCKS = r"""
+#include "gsq_plan.h"
+#include <cstdio>
+#include <cstdlib>
+int main(int argc, char** argv) {
+  for (int k = 1; k < argc; ++k) {
+    const unsigned b = gsq::unpack_blocks(std::atoll(argv[k]));
+    std::printf("%u %d\n", b, b > 0 && gsq::fits_launch(b, 256));
+  }
+}
+"""
+
+
+def test_packed_layers_of_any_size_are_laid_out_by_one_launch(tmp_path):
+    """Elements that gsq_linear_init lays out, from one channel to its largest layer: two for each 32 weights."""
+    src, exe = tmp_path / "blocks.cpp", tmp_path / "blocks"
+    src.write_text(BLOCKS)
+    subprocess.run(["g++", "-std=c++17", "-I", os.path.join(ROOT, "paper_2604_18556_amd", "csrc"), str(src), "-o",
+                    str(exe)], check=True, capture_output=True, text=True)
+    counts = [16, 64, 256, 257, 16384 * 256, 16384 * 256 + 1, 1 << 32, 1 << 40, 65535 * (1 << 21) * (1 << 21) // 16]
+    out = subprocess.run([str(exe), *map(str, counts)], check=True, capture_output=True, text=True).stdout.split()
+    blocks, fits = list(map(int, out[::2])), list(map(int, out[1::2]))
+    assert blocks == [1, 1, 1, 2] + [16384] * 5 and all(fits)
