@@ -79,10 +79,11 @@ gsq_status gsq_grouped_forward_i8(const gsq_grouped* g, const int8_t* x, const f
 
 /*
  * A packed layer in use.  gsq_linear_init reads the bytes that gsq_pack wrote for cfg (batch, sizes,
- * levels, group_size and layout count) and lays them out for the matrix cores, at the packed size and a
- * quarter more at most (1.6-bit codes are kept in 2 bits); `packed` may be freed once the stream has
- * passed the call.  A code >= n_levels is read as n_levels - 1.  It allocates, so a capturing stream is
- * refused.
+ * levels, group_size and layout count) and lays them out for the matrix cores, in units of 16 channels x
+ * 128 inputs.  It keeps the packed bytes of the layer with its sizes rounded up to those, and a quarter
+ * more at most (1.6-bit codes take 2 bits, 6-bit scales 8): a layer of few channels or inputs takes a
+ * multiple of its own.  `packed` may be freed once the stream has passed the call.  A code >= n_levels is
+ * read as n_levels - 1.  It allocates, so a capturing stream is refused.
  *
  * gsq_linear_forward: y = x Wq_e^T for x: rows x I and y: rows x O in dtype (GSQ_DT_BF16 or GSQ_DT_FP16),
  * rows grouped by the layers of the batch.  A weight is scale * level in fp32 (SUPERBLOCK: d * sc * level,

@@ -18,6 +18,16 @@ inline int64_t most_panels(int64_t rows, int64_t groups, int64_t height) {
 // What one launch holds: fewer than 2^32 threads in the grid's one dimension.
 inline bool fits_launch(int64_t tiles, int64_t threads) { return tiles * threads < (int64_t)1 << 32; }
 
+// Bytes of a packed layer as it is kept, in units of 16 channels x 128 inputs (64 lanes with 32 codes each); `gs`:
+// inputs per fp16 scale, `super`: with sub-scales, a byte for each 16 inputs.
+struct KeptBytes {
+  int64_t codes, scales, sub;
+};
+inline KeptBytes kept_bytes(int64_t batch, int O, int I, int bits, int gs, bool super) {
+  const int64_t tiles = batch * tiles_of(O, 16), blocks = tiles_of(I, 128), lanes = tiles * blocks * 64;
+  return {lanes * bits * 4, gs == 16 ? lanes * 4 : tiles * tiles_of(blocks * 128, gs) * 32, super ? lanes * 2 : 0};
+}
+
 // Workgroups of 256 threads that lay out `count` elements of a packed layer.  From eight full GPUs' (256 CUs x 8) on
 // they pass over the rest, so that a layer of any size fits a launch.  (64 super-block experts of 2048 x 7168: 1.85 ms,
 // with a workgroup for every 256 elements 1.84, with one full GPU's 2.02.)

@@ -1,9 +1,10 @@
-// Host side of the products in gsq.h: validation, the packed layer's handle and launches.
+// Host side of the products in gsq_products.h: validation, the packed layer's handle and launches.
 #include <hip/hip_runtime.h>
 
 #include <new>
 
 #include "gsq_host.h"
+#include "gsq_plan.h"
 #include "gsq_product.h"
 
 using gsq::fail;
@@ -222,10 +223,8 @@ gsq_status gsq_linear_init(const gsq_config* cfg, const void* packed, size_t pac
     delete h;
     return gsq::hip_fail(e, "hipGetDevice");
   }
-  const int64_t tiles = (int64_t)cfg->batch * L.tiles;
-  const size_t lanes = (size_t)tiles * L.blocks * 64;
-  const size_t bytes[3] = {lanes * L.bits * 4, L.gs == 16 ? lanes * 2 * 2 : (size_t)tiles * L.scale_groups * 16 * 2,
-                           super ? lanes * 2 : 0};
+  const gsq::KeptBytes kept = gsq::kept_bytes(cfg->batch, L.O, L.I, L.bits, L.gs, super);
+  const size_t bytes[3] = {(size_t)kept.codes, (size_t)kept.scales, (size_t)kept.sub};
   for (int i = 0; i < 3; ++i) {
     if (!bytes[i]) continue;
     void* p = nullptr;

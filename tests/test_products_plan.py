@@ -6,6 +6,7 @@ import subprocess
 import pytest
 
 import product_cases as cases
+from paper_2604_18556_amd import binding as B
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -145,3 +146,44 @@ def test_packed_layers_of_any_size_are_laid_out_by_one_launch(tmp_path):
     out = subprocess.run([str(exe), *map(str, counts)], check=True, capture_output=True, text=True).stdout.split()
     blocks, fits = list(map(int, out[::2])), list(map(int, out[1::2]))
     assert blocks == [1, 1, 1, 2] + [16384] * 5 and all(fits)
+
+
+KEPT = r"""
+#include "gsq_plan.h"
+#include <cstdio>
+int main() {
+  long long b, o, i;
+  int bits, gs, super;
+  while (std::scanf("%lld %lld %lld %d %d %d", &b, &o, &i, &bits, &gs, &super) == 6) {
+    const gsq::KeptBytes k = gsq::kept_bytes(b, o, i, bits, gs, super);
+    std::printf("%lld\n", (long long)(k.codes + k.scales + k.sub));
+  }
+}
+"""
+
+
+def test_kept_bytes_of_a_packed_layer_are_as_the_header_says(tmp_path):
+    """Never more than a quarter above the packed size of the layer rounded up to whole units of 16 x 128."""
+    if not os.path.exists(B._LIB_PATH):
+        pytest.skip("libgsq.so not built (run __graft_entry__.build())")
+    src, exe = tmp_path / "kept.cpp", tmp_path / "kept"
+    src.write_text(KEPT)
+    subprocess.run(["g++", "-std=c++17", "-I", os.path.join(ROOT, "paper_2604_18556_amd", "csrc"), str(src), "-o",
+                    str(exe)], check=True, capture_output=True, text=True)
+    layers = []
+    for batch, o, units in ((1, 1, 1), (1, 5, 3), (3, 16, 1), (2, 17, 32), (1, 4096, 16), (64, 2048, 28)):
+        layers += [(B.LAYOUT_SUPERBLOCK, cases.L8, 3, 16, batch, o, 256 * units)]
+        for gs in (16, 32, 64, 128, 256):
+            layers += [(B.LAYOUT_BASE3, cases.L3, 2, gs, batch, o, gs * units)]
+            layers += [(B.LAYOUT_GROUP, levels, bits, gs, batch, o, gs * units)
+                       for levels, bits in ((cases.L2, 1), (cases.L4, 2), (cases.L8, 3), (cases.L16, 4))]
+    text = "".join(f"{b} {o} {i} {bits} {256 if lay == B.LAYOUT_SUPERBLOCK else gs} {int(lay == B.LAYOUT_SUPERBLOCK)}\n"
+                   for lay, _, bits, gs, b, o, i in layers)
+    kept = subprocess.run([str(exe)], input=text, check=True, capture_output=True, text=True).stdout.split()
+    worst = 0
+    for (lay, levels, bits, gs, b, o, i), bytes_ in zip(layers, map(int, kept), strict=True):
+        whole = B.packed_size(B.LayerConfig(-(-o // 16) * 16, -(-i // 128) * 128, levels, gs, b, lay,
+                                            relaxation=B.RELAX_SHIFT if bits == 4 else B.RELAX_GRID))
+        assert whole <= bytes_ <= 1.25 * whole, (lay, bits, gs, b, o, i)
+        worst = max(worst, bytes_ / B.packed_size(B.LayerConfig(o, i, levels, gs, b, lay, relaxation=B.RELAX_SHIFT)))
+    assert worst > 8                               # the layer's own size is no bound
