@@ -14,13 +14,13 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-// Element types: what a matrix instruction of 16 x 16 x kStep takes and sums into.
+// Element types: what a matrix instruction of 16 x 16 outputs takes and sums into.
 struct Bf16 {
   using elem = __bf16;
   using out = __bf16;
   using frag = bf16x8;
   using acc = f32x4;
-  static constexpr int kStep = 32, kDtype = GSQ_DT_BF16;
+  static constexpr int kDtype = GSQ_DT_BF16;
   static __device__ __forceinline__ acc mfma(frag a, frag b, acc c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
@@ -30,7 +30,7 @@ struct F16 {
   using out = _Float16;
   using frag = f16x8;
   using acc = f32x4;
-  static constexpr int kStep = 32, kDtype = GSQ_DT_FP16;
+  static constexpr int kDtype = GSQ_DT_FP16;
   static __device__ __forceinline__ acc mfma(frag a, frag b, acc c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
   }
@@ -41,7 +41,7 @@ struct I8 {
   using out = Out;
   using frag = i32x4;
   using acc = i32x4;
-  static constexpr int kStep = 64, kDtype = -1;
+  static constexpr int kDtype = -1;
   static __device__ __forceinline__ acc mfma(frag a, frag b, acc c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
   }
@@ -61,7 +61,7 @@ __device__ __forceinline__ void group_rows(const GroupRows& g, int e, int64_t& f
 // Where a workgroup stands when every group's rows are cut into panels of equal height, group after group.
 struct PanelPlace {
   int group;
-  int panel, panels;        // in the group
+  int panels;               // of the group
   int64_t first, end;       // rows of the group
   int64_t before;           // panels of the groups before it
 };
@@ -94,7 +94,6 @@ __device__ __forceinline__ bool find_panel(const GroupRows& g, int height, int64
       at.group = e0 + src;
       at.panels = (int)of_src(mine);
       at.before = before + of_src(upto - mine);
-      at.panel = (int)(index - at.before);
       at.first = of_src(a);
       at.end = of_src(b);
       return true;
