@@ -38,7 +38,8 @@ struct TileShape {
 // consecutive columns of a row.  The instruction is written out because the builtin gives its result other
 // registers than its accumulator input once there are 64 of these, and moves them around.  The compiler
 // then does not see when an accumulator can be read: acc_settled() waits for it.  The operands come from
-// LDS reads, whose waits the compiler sets; no vector instruction writes them.
+// LDS reads, whose waits the compiler sets; no vector instruction writes them.  Both are checked in the built
+// object code (tests/test_object_code.py).
 template <class T>
 __device__ __forceinline__ void mfma_block(typename T::acc& acc, const i32x4& b, const i32x4& a) {
   if constexpr (T::kDtype == GSQ_DT_BF16)
@@ -53,9 +54,9 @@ __device__ __forceinline__ void mfma_block(typename T::acc& acc, const i32x4& b,
 // make every transposing LDS read wait for all of them: the loop's own wait_vm() and barrier order them, and
 // they return nothing to a register.  Addresses: a uniform base with 32-bit lane offsets, or one per lane.
 // M0 holds the LDS address; nothing else in these kernels uses it (it is no register that the compiler keeps
-// values in).  A uniform base has to come from scalar instructions, as a slab's does that is reckoned from the
-// operand's: one that a vector instruction wrote needs five instructions between, which the compiler does not
-// see to here.
+// values in, nor one that it lets an asm declare).  A uniform base has to come from scalar instructions, as a
+// slab's does that is reckoned from the operand's: one that a vector instruction wrote needs five instructions
+// between, which the compiler does not see to here.  Both are checked in the built object code, too.
 __device__ __forceinline__ uint32_t lds_address(const uint8_t* lds) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)lds;
 }
