@@ -72,7 +72,7 @@ gsq_status gsq_quantize_rows(const void* x, int32_t dtype, int64_t rows, int32_t
 
 /* y[r, n] = x_scales[r] w_scales[e, n] sum_k x[r, k] w[e, n, k] for 8-bit x and w.  x: int8 R x I, x_scales:
  * fp32 R, w: int8 groups x O x I, w_scales: fp32 groups x O, y: R x O in dtype.  The sum is exact:
- * in_features <= 131071. */
+ * in_features <= 131071.  It is then scaled in fp32, by x's scale first: (sum x_scale) w_scale. */
 gsq_status gsq_grouped_forward_i8(const gsq_grouped* g, const int8_t* x, const float* x_scales,
                                   const int8_t* w, const float* w_scales, const int64_t* offsets,
                                   void* y, hipStream_t stream);

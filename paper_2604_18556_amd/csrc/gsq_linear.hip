@@ -241,8 +241,9 @@ struct LaneCodes {
 // ---- few rows, or too few tiles for whole workgroups: COLS channels and up to 64 rows, the units shared by the
 // wavefronts as tile_split() does it.  x goes through LDS, the weights from the codes to registers.
 //
-// At one row bound by the vector units, which take some three instructions for a weight of 3 bits, and by latency:
-// 4096 x 14336 (23 MB) in 11.4 us, 4096 x 4096 in 6.1.  x straight from memory to the fragments, without LDS: 12.8
+// At one row bound by latency, with one unit of codes in flight for each wavefront: 4096 x 14336 (23 MB) in 11.3 us,
+// 4096 x 4096 in 6.1, vector units busy 0.36 of the time (some three instructions for a weight of 3 bits) and wavefronts
+// waiting 0.46.  x straight from memory to the fragments, without LDS: 12.8
 // us at one row, and 23 at 16 instead of 13.
 template <class T, int BITS, bool kFine, int COLS, int TM, bool kLoose>
 __device__ __forceinline__ void packed_shared(const PackedLayer& L, const typename T::elem* x, typename T::elem* y,

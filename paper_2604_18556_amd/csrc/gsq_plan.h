@@ -153,7 +153,9 @@ inline int64_t sum_tiles(int64_t groups, int O, int I, bool gram, int size) {
 //     401 | 527 | 1451 | -
 //   8192 x 8192: 256 rows 72 | 66 | 138 | 170; 4096 rows 432 | 475 | 883 | 2120; 16384 rows 1607 | 2516 | - | -
 // and H, which stores most tiles twice: 4096 x 4096 from 1024 rows 57 | 39 | 57 | 83, 8192 x 8192 from 64 rows
-// - | 59 | 51 | -, 1024 rows 156 | 106 | 202 | 306, 16384 rows 1093 | 1857 | - | -.
+// - | 59 | 51 | -, 1024 rows 156 | 106 | 202 | 306, 16384 rows 1093 | 1857 | - | -; with whole tiles | what the rule takes:
+// 2048 x 2048 from 8192 rows 180 | 69, 4096 x 4096 from 4096 120 | 100, 8192 202 | 181, 12288 278 | 259, 6144 x 6144
+// from 8192 392 | 348, 8192 x 8192 from 4096 348 | 319; 5120 x 5120 from 8192 209 | 218, the one that it misses.
 inline SumsPlan plan_sums(int64_t rows, int64_t groups, int O, int I, bool tight, bool gram) {
   const double slabs = (double)rows / 64 / groups;
   const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(kSplitWaves, tiles_of(rows, 64)));
