@@ -408,7 +408,8 @@ def _weight_sizes(w, name="w"):
         shape = (1, *shape)
     elif len(shape) != 3:
         raise ValueError(f"{name} must be groups x O x I or O x I, got {tuple(shape)}")
-    _int32(f"the largest size of {name}", max(shape))
+    if max(shape) >= 1 << 31:
+        _int32(f"the largest size of {name}", max(shape))
     return shape
 
 
