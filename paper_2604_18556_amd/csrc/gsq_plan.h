@@ -52,15 +52,15 @@ struct TileCost {
 };
 
 // The cheapest of several tiles of `waves` wavefronts that fit one launch: a launch, and a tile's time for each round
-// of 256 tiles.  The groups' last panels are taken to be half full.
+// of 256 tiles.  The groups' last panels are taken to be half full, and `fewest` are reckoned with at least.
 template <int N>
 RowsPlan cheapest(int64_t rows, int64_t groups, int cols, int slabs, const TileCost (&costs)[N], bool split, int waves,
-                  double& best, RowsPlan plan) {
+                  double& best, RowsPlan plan, double fewest = 0) {
   const double few = (double)std::min(rows, groups);
   for (const TileCost& c : costs) {
     if (!fits_launch(most_panels(rows, groups, c.height) * tiles_of(cols, c.width), 64 * waves)) continue;
     const double panels = groups == 1 ? (double)tiles_of(rows, c.height) : rows / (double)c.height + few / 2;
-    const double tiles = panels * tiles_of(cols, c.width), rounds = tiles / 256;
+    const double tiles = std::max(panels, fewest) * tiles_of(cols, c.width), rounds = tiles / 256;
     const double whole = rounds < 1 ? 1 : groups == 1 ? (double)(int64_t)(rounds + 0.999) : rounds;
     const double each = c.alone + (c.full - c.alone) * (rounds < 1 ? rounds : 1);
     const double us = 4 + whole * (c.start + slabs * each);
@@ -120,11 +120,12 @@ inline RowsPlan plan_packed(int64_t rows, int64_t groups, int O, int blocks, boo
     //   I 4096, O 4096: 1 row 8 | 83; 64 rows 25 | 83; 256 rows 90 | 85; 2001 rows 683 | 99 (aligned 81); 4096 rows
     //     1386 | 184
     //   I 4096, O 14336: 64 rows 78 | 84; 512 rows 611 | 97.  I 14336, O 4096: 1 row 18 | 267; 256 rows 246 | 295
-    // (3 bits 2 to 8 % longer, 4 bits 5 to 25 %)
+    // (3 bits 2 to 8 % longer, 4 bits 5 to 25 %), and 64 groups of 2048 x 7168, super-blocks, where each group with rows
+    // has a panel: 128 rows 342 | 408, 512 rows 350 | 377, 1024 rows 364 | 378, 2048 rows 666 | 384
     const TileCost few[] = {{16, 16, 0.7, 0.04, 0.068}};
     const TileCost loose[] = {{128, 256, 2, 1.2, 1.42}};
     const RowsPlan plan = cheapest(rows, groups, O, slabs, few, true, few_waves, best, RowsPlan{});
-    return cheapest(rows, groups, O, slabs, loose, false, kRingWaves, best, plan);
+    return cheapest(rows, groups, O, slabs, loose, false, kRingWaves, best, plan, (double)std::min(rows, groups));
   }
   const TileCost few[] = {{16, 16, 0.7, 0.02, 0.03}};
   RowsPlan plan = cheapest(rows, groups, O, slabs, few, true, few_waves, best, RowsPlan{});

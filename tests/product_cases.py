@@ -72,6 +72,8 @@ PACKED = [
     ("group", L16, 64, [1100], 4100, 64, 1, "ring 128x256"),
     ("group", L16, 16, [700], 4111, 176, 2, "ring 128x256"),
     ("group", L8, 128, [70, 40, 0, 5, 17], 520, 640, 1, "split 16x16"),
+    ("superblock", L8, 16, [8] * 64, 72, 256, 1, "split 16x16"),   # experts, eight tokens each
+    ("superblock", L8, 16, [32] * 64, 2048, 256, 1, "ring 128x256"),
 ]
 
 
