@@ -218,3 +218,17 @@ def test_streams_of_another_device_are_refused():
     assert B._raw_stream(SimpleNamespace(cuda_stream=64, device_index=1), 1) == 64
     with pytest.raises(ValueError, match="stream is on device 1"):
         B._raw_stream(SimpleNamespace(cuda_stream=64, device_index=1), 0)
+
+
+@pytest.mark.parametrize("helper", ["lin_of", "tile_at", "swz", "load_rows", "wait_vm", "slab_barrier"])
+def test_helpers_that_two_files_have_are_the_same(helper):
+    """The contraction has its own copy of these, as its measured traffic is recorded for its exact source: a
+    change to one belongs in both."""
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2604_18556_amd", "csrc")
+    bodies = []
+    for name in ("gsq_slab.hpp", "gsq_contract.hip"):
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(csrc, name)).read())
+        body = re.search(r"(template <[^>]*>\s*)?__device__ __forceinline__ \w+ " + helper + r"\(.*?\}\n", text, re.S)
+        assert body, (name, helper)
+        bodies.append(" ".join(body[0].split()))
+    assert bodies[0] == bodies[1]
