@@ -151,7 +151,7 @@ def work(case):
         t, r, c = case["tokens"], _rows(case), case["width"]
         slots = 4.0 * t * case["top_k"]
         if kind == "exchange":
-            return {"bytes": size * c * (2.0 * t + 2.0 * r) + 3 * slots, "flops": 2.0 * r * c}
+            return {"bytes": size * c * (2.0 * t + 2.0 * r) + 2 * slots + 4.0 * t * case["top_k"], "flops": 2.0 * r * c}
         return {"bytes": size * c * (2.0 * t + 3.0 * r) + 3 * slots, "flops": 4.0 * r * c}
     r, o, i, q = case["rows"], case["out"], case["in"], case["rank"]
     used = min(case["adapters"], case["segments"])
@@ -305,7 +305,7 @@ def _run_own(state):
         B.route_grad(state["routing"], state["logits"], state["ids"], state["dw"], state["dlogits"])
         return state["dlogits"]
     if kind == "exchange":
-        B.gather_rows(state["x"], state["sources"], state["xs"], copies=case["top_k"])
+        B.dispatch_rows(state["x"], state["slots"], state["xs"])
         B.combine_rows(state["ys"], state["slots"], state["y"], weights=state["weights"])
         return {"xs": state["xs"], "y": state["y"]}
     if kind == "exchange-grad":
