@@ -1,4 +1,4 @@
-"""ctypes binding of include/gsq.h and include/gsq_products.h: argument marshalling only.
+"""ctypes binding of include/gsq.h, gsq_products.h and gsq_routing.h: argument marshalling only.
 
 Every computation runs in ``libgsq.so``; this module passes device pointers
 (``tensor.data_ptr()``) and the current HIP stream to it and turns status codes
@@ -19,6 +19,8 @@ PREC_FP32, PREC_BF16 = 0, 1
 DT_FP32, DT_BF16, DT_FP16 = 0, 1, 2
 OPT_ADAM, OPT_LION = 0, 1
 MAX_SAMPLES = 16            # GSQ_MAX_SAMPLES
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+GROUP_MAX, GROUP_TOP2 = 0, 1
 STATUS_NAMES = {0: "GSQ_OK", -1: "GSQ_EINVAL", -2: "GSQ_ENOMEM", -3: "GSQ_EHIP",
                 -4: "GSQ_ENONFINITE", -5: "GSQ_EUNSUPPORTED"}
 
@@ -28,6 +30,8 @@ EXPORTS = ("gsq_layer_init", "gsq_step", "gsq_step_static", "gsq_harden", "gsq_p
 PRODUCT_EXPORTS = ("gsq_grouped_forward", "gsq_grouped_input_grad", "gsq_grouped_weight_grad", "gsq_gram",
                    "gsq_quantize_rows", "gsq_grouped_forward_i8", "gsq_linear_init", "gsq_linear_forward",
                    "gsq_linear_destroy")
+ROUTING_EXPORTS = ("gsq_route", "gsq_route_grad", "gsq_group_rows", "gsq_dispatch_rows", "gsq_combine_rows",
+                   "gsq_combine_rows_grad")
 KERNEL_NAMES = ("init", "forward", "contract", "reduce", "backward", "harden", "pack")
 
 
@@ -65,6 +69,18 @@ class CStepParams(ctypes.Structure):
 class CGrouped(ctypes.Structure):
     _fields_ = [("groups", ctypes.c_int32), ("out_features", ctypes.c_int32),
                 ("in_features", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rows", ctypes.c_int64)]
+
+
+class CRouting(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("experts", ctypes.c_int32), ("top_k", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("top_groups", ctypes.c_int32), ("score", ctypes.c_int32),
+                ("group_score", ctypes.c_int32), ("renormalise", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("dtype", ctypes.c_int32)]
+
+
+class CExchange(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("rows", ctypes.c_int64), ("copies", ctypes.c_int32),
+                ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 @dataclass
@@ -128,6 +144,24 @@ class StepParams:
                            self.kappa_next, self.optimizer, self.weight_decay, self.samples)
 
 
+@dataclass
+class Routing:
+    """How tokens choose their experts (gsq_routing)."""
+    experts: int
+    top_k: int
+    groups: int = 1
+    top_groups: int = 1
+    score: int = SCORE_SOFTMAX
+    group_score: int = GROUP_TOP2
+    renormalise: bool = True
+    scale: float = 1.0
+
+    def to_c(self, tokens, dtype):
+        return CRouting(tokens, _int32("experts", self.experts), _int32("top_k", self.top_k),
+                        _int32("groups", self.groups), _int32("top_groups", self.top_groups), self.score,
+                        self.group_score, 1 if self.renormalise else 0, self.scale, dtype)
+
+
 _lib = None
 
 
@@ -169,7 +203,14 @@ def load(path=None):
     lib.gsq_linear_init.argtypes = [ctypes.POINTER(CConfig), vp, sz, vp, ctypes.POINTER(vp)]
     lib.gsq_linear_forward.argtypes = [vp, vp, i32, i64, vp, vp, vp]
     lib.gsq_linear_destroy.argtypes = [vp]
-    for name in PRODUCT_EXPORTS:
+    rp, xp = ctypes.POINTER(CRouting), ctypes.POINTER(CExchange)
+    lib.gsq_route.argtypes = [rp, vp, vp, vp, vp, vp]
+    lib.gsq_route_grad.argtypes = [rp, vp, vp, vp, vp, vp]
+    lib.gsq_group_rows.argtypes = [vp, i64, i32, vp, vp, vp, vp]
+    lib.gsq_dispatch_rows.argtypes = [xp, vp, vp, vp, vp]
+    lib.gsq_combine_rows.argtypes = [xp, vp, vp, vp, vp, vp]
+    lib.gsq_combine_rows_grad.argtypes = [xp, vp, vp, vp, vp, vp, vp, vp]
+    for name in PRODUCT_EXPORTS + ROUTING_EXPORTS:
         getattr(lib, name).restype = ctypes.c_int
     for name in ("gsq_layer_init", "gsq_step", "gsq_step_static", "gsq_harden", "gsq_pack",
                  "gsq_get_state", "gsq_set_state", "gsq_get_intermediates", "gsq_gumbel", "gsq_check",
@@ -521,3 +562,99 @@ class Linear:
             self.destroy()
         except Exception:
             pass
+
+
+# ---- rows to the routed experts and back: logits are tokens x experts, and slots (tokens x top_k, int32) say where
+# each copy of a token stands among the rows of all experts (-1: nowhere).
+
+def _float_dtype(t):
+    import torch
+    return DT_FP32 if t.dtype is torch.float32 else _rows_dtype(t)
+
+
+def _cut(name, t):
+    if len(t.shape) != 2:
+        raise ValueError(f"{name} must have two dimensions, got {tuple(t.shape)}")
+    return t.shape
+
+
+def route(routing, logits, experts, weights, bias=None, stream=None):
+    """The ``top_k`` experts (int32) and weights (float32) of each token from its logits (tokens x experts;
+    float32, bfloat16 or float16); the float32 ``bias`` of each expert enters the choice only."""
+    import torch
+    (t, e), dt, k = _cut("logits", logits), _float_dtype(logits), routing.top_k
+    args = (("logits", logits, (t, routing.experts), (logits.dtype,)),
+            ("experts", experts, (t, k), (torch.int32,)), ("weights", weights, (t, k), (torch.float32,)))
+    if bias is not None:
+        args += (("bias", bias, (routing.experts,), (torch.float32,)),)
+    dev = _checked(args, None, 1)
+    _check(load().gsq_route(ctypes.byref(routing.to_c(t, dt)), logits.data_ptr(), _address(bias), experts.data_ptr(),
+                            weights.data_ptr(), _raw_stream(stream, dev)))
+
+
+def route_grad(routing, logits, experts, dweights, out, stream=None):
+    """out = the gradient of route's logits (their shape and type) from that of its weights, for the experts that
+    it chose."""
+    import torch
+    (t, e), dt, k = _cut("logits", logits), _float_dtype(logits), routing.top_k
+    dev = _checked((("logits", logits, (t, routing.experts), (logits.dtype,)),
+                    ("experts", experts, (t, k), (torch.int32,)), ("dweights", dweights, (t, k), (torch.float32,)),
+                    ("out", out, (t, routing.experts), (logits.dtype,))), None, 1)
+    _check(load().gsq_route_grad(ctypes.byref(routing.to_c(t, dt)), logits.data_ptr(), experts.data_ptr(),
+                                 dweights.data_ptr(), out.data_ptr(), _raw_stream(stream, dev)))
+
+
+def group_rows(ids, offsets, slots, sources, stream=None):
+    """The stable order that brings equal ids together (int32 of any shape; one group for each of ``offsets`` but the
+    last, other ids belong to none): the groups' int64 row ``offsets``, as the products take them, the int32 ``slots``
+    (shape of ids) where each id goes, and the int32 ``sources`` (one for each id) that stand at each place."""
+    import torch
+    n, groups, ints = ids.numel(), offsets.numel() - 1, (torch.int32,)
+    dev = _checked((("ids", ids, ids.shape, ints), ("slots", slots, ids.shape, ints),
+                    ("sources", sources, (n,), ints), ("offsets", offsets, (groups + 1,), (torch.int64,))), None, 1)
+    _check(load().gsq_group_rows(ids.data_ptr(), n, _int32("groups", groups), offsets.data_ptr(), slots.data_ptr(),
+                                 sources.data_ptr(), _raw_stream(stream, dev)))
+
+
+def _exchange(tokens, rows, slots, dtype):
+    """The sizes of an exchange between ``tokens`` and ``rows``, and the shape of its slots."""
+    (t, c), r, (_, k) = _cut("tokens", tokens), _row_count(rows, "rows"), _cut("slots", slots)
+    return CExchange(t, r, _int32("the slots of a token", k), _int32("the columns", c), dtype), (t, k), (t, c), (r, c)
+
+
+def dispatch_rows(x, slots, out, stream=None):
+    """out[slots[t, k]] = x[t] (float32, bfloat16 or float16); rows of out that no slot names stay as they were."""
+    import torch
+    types = (x.dtype,)
+    g, s, of_tokens, of_rows = _exchange(x, out, slots, _float_dtype(x))
+    dev = _checked((("x", x, of_tokens, types), ("slots", slots, s, (torch.int32,)), ("out", out, of_rows, types)),
+                   None, 1)
+    _check(load().gsq_dispatch_rows(ctypes.byref(g), x.data_ptr(), slots.data_ptr(), out.data_ptr(),
+                                    _raw_stream(stream, dev)))
+
+
+def combine_rows(rows, slots, out, weights=None, stream=None):
+    """out[t] = sum of weights[t, k] rows[slots[t, k]] over k (no weights: ones, which is dispatch_rows' gradient)."""
+    import torch
+    types = (rows.dtype,)
+    g, s, of_tokens, of_rows = _exchange(out, rows, slots, _float_dtype(rows))
+    args = (("rows", rows, of_rows, types), ("slots", slots, s, (torch.int32,)), ("out", out, of_tokens, types))
+    if weights is not None:
+        args += (("weights", weights, s, (torch.float32,)),)
+    dev = _checked(args, None, 1)
+    _check(load().gsq_combine_rows(ctypes.byref(g), rows.data_ptr(), slots.data_ptr(), _address(weights),
+                                   out.data_ptr(), _raw_stream(stream, dev)))
+
+
+def combine_rows_grad(dout, rows, slots, weights, drows, dweights, stream=None):
+    """combine_rows' gradients: drows[slots[t, k]] = weights[t, k] dout[t], and dweights[t, k] = the product of dout[t]
+    and rows[slots[t, k]]; rows of drows that no slot names stay as they were."""
+    import torch
+    types, floats = (dout.dtype,), (torch.float32,)
+    g, s, of_tokens, of_rows = _exchange(dout, rows, slots, _float_dtype(dout))
+    dev = _checked((("dout", dout, of_tokens, types), ("rows", rows, of_rows, types),
+                    ("slots", slots, s, (torch.int32,)), ("weights", weights, s, floats),
+                    ("drows", drows, of_rows, types), ("dweights", dweights, s, floats)), None, 1)
+    _check(load().gsq_combine_rows_grad(ctypes.byref(g), dout.data_ptr(), rows.data_ptr(), slots.data_ptr(),
+                                        weights.data_ptr(), drows.data_ptr(), dweights.data_ptr(),
+                                        _raw_stream(stream, dev)))

@@ -177,4 +177,21 @@ inline SumsPlan plan_sums(int64_t rows, int64_t groups, int O, int I, bool tight
   return {true, us_32 < us_64 ? 32 : 64, waves};
 }
 
+// How ids are brought into order: by one workgroup, or chunk by chunk, of which there are at most 128, so that a
+// workgroup counts over all of them itself.  The chunks' counts fit into a quarter of the ids' places.  `waves`
+// wavefronts count, with a histogram each in LDS (64 KB in all).
+struct OrderPlan {
+  int threads, waves, chunks;
+  int64_t chunk;
+};
+inline OrderPlan plan_order(int64_t count, int groups) {
+  constexpr int kWords = 15360;
+  const int64_t chunk = std::max({(int64_t)2048, (int64_t)4 * groups, tiles_of(tiles_of(count, 128), 64) * 64});
+  if (count <= std::max((int64_t)8192, chunk)) {
+    const int waves = (int)std::min<int64_t>({16, kWords / groups - 1, tiles_of(count, 64)});
+    return {std::max(64 * waves, groups > 256 ? 1024 : 256), waves, 1, count};
+  }
+  return {512, std::min(8, kWords / groups), (int)tiles_of(count, chunk), chunk};
+}
+
 }  // namespace gsq

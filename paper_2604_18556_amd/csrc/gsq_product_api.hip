@@ -3,11 +3,11 @@
 
 #include <new>
 
-#include "gsq_host.h"
+#include "gsq_check.h"
 #include "gsq_plan.h"
 #include "gsq_product.h"
 
-using gsq::fail;
+using namespace gsq;
 
 struct gsq_linear {
   gsq::PackedLayer L;
@@ -19,28 +19,7 @@ struct gsq_linear {
 
 namespace {
 
-constexpr int64_t kMostRows = (int64_t)1 << 29, kMostFeatures = (int64_t)1 << 21;
-constexpr int32_t kMostGroups = 65535, kMostExactI8 = 131071;   // 128^2 131071 < 2^31
-
-bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-bool sixteen_bits(int32_t dtype) { return dtype == GSQ_DT_BF16 || dtype == GSQ_DT_FP16; }
-
-gsq_status check_sizes(int32_t groups, int64_t rows, const int64_t* offsets) {
-  if (groups < 1 || groups > kMostGroups)
-    return fail(GSQ_EINVAL, "groups must be in [1, %d], got %d", kMostGroups, groups);
-  if (rows < 0 || rows > kMostRows)
-    return fail(GSQ_EINVAL, "rows must be in [0, %lld], got %lld", (long long)kMostRows, (long long)rows);
-  if (!offsets && groups > 1) return fail(GSQ_EINVAL, "offsets is NULL with %d groups", groups);
-  if (!aligned(offsets, 8)) return fail(GSQ_EINVAL, "offsets is not aligned to 8 bytes");
-  return GSQ_OK;
-}
-
-gsq_status check_features(const char* name, int32_t n) {
-  if (n < 1 || n > kMostFeatures)
-    return fail(GSQ_EINVAL, "%s must be in [1, %lld], got %d", name, (long long)kMostFeatures, n);
-  return GSQ_OK;
-}
+constexpr int32_t kMostExactI8 = 131071;   // 128^2 131071 < 2^31
 
 gsq_status check_grouped(const gsq_grouped* g, const int64_t* offsets, bool out_used) {
   if (!g) return fail(GSQ_EINVAL, "the sizes are NULL");
@@ -49,26 +28,6 @@ gsq_status check_grouped(const gsq_grouped* g, const int64_t* offsets, bool out_
   if (st == GSQ_OK && out_used) st = check_features("out_features", g->out_features);
   return st == GSQ_OK ? check_sizes(g->groups, g->rows, offsets) : st;
 }
-
-// An array that holds elements (`any`) must have an address, aligned to them.
-gsq_status check_array(const char* name, const void* p, size_t elem, bool any) {
-  if (any && !p) return fail(GSQ_EINVAL, "%s is NULL", name);
-  if (!aligned(p, elem)) return fail(GSQ_EINVAL, "%s is not aligned to %zu bytes", name, elem);
-  return GSQ_OK;
-}
-
-// A launch's outcome.  Its grid is checked before anything is enqueued.
-gsq_status launched(hipError_t e, const char* what) {
-  if (e == hipSuccess) return GSQ_OK;
-  if (e == hipErrorInvalidConfiguration) return fail(GSQ_EINVAL, "%s: more tiles than one launch holds", what);
-  return gsq::hip_fail(e, what);
-}
-
-#define GSQ_TRY(call)                    \
-  do {                                   \
-    const gsq_status st_ = (call);       \
-    if (st_ != GSQ_OK) return st_;       \
-  } while (0)
 
 gsq::ProductArgs product_args(const gsq_grouped* g, const int64_t* offsets, const void* a, const void* b,
                               void* out, int32_t out_dtype) {
