@@ -1,4 +1,4 @@
-"""ctypes binding of include/gsq.h, gsq_products.h and gsq_routing.h: argument marshalling only.
+"""ctypes binding of include/gsq.h, gsq_products.h, gsq_routing.h and gsq_adapters.h: argument marshalling only.
 
 Every computation runs in ``libgsq.so``; this module passes device pointers
 (``tensor.data_ptr()``) and the current HIP stream to it and turns status codes
@@ -32,6 +32,7 @@ PRODUCT_EXPORTS = ("gsq_grouped_forward", "gsq_grouped_input_grad", "gsq_grouped
                    "gsq_linear_destroy")
 ROUTING_EXPORTS = ("gsq_route", "gsq_route_grad", "gsq_group_rows", "gsq_dispatch_rows", "gsq_combine_rows",
                    "gsq_combine_rows_grad")
+ADAPTER_EXPORTS = ("gsq_adapter_forward", "gsq_adapter_input_grad", "gsq_adapter_weight_grad")
 KERNEL_NAMES = ("init", "forward", "contract", "reduce", "backward", "harden", "pack")
 
 
@@ -81,6 +82,12 @@ class CRouting(ctypes.Structure):
 class CExchange(ctypes.Structure):
     _fields_ = [("tokens", ctypes.c_int64), ("rows", ctypes.c_int64), ("copies", ctypes.c_int32),
                 ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class CAdapters(ctypes.Structure):
+    _fields_ = [("segments", ctypes.c_int32), ("adapters", ctypes.c_int32), ("rank", ctypes.c_int32),
+                ("out_features", ctypes.c_int32), ("in_features", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("rows", ctypes.c_int64)]
 
 
 @dataclass
@@ -210,7 +217,11 @@ def load(path=None):
     lib.gsq_dispatch_rows.argtypes = [xp, vp, vp, vp, vp]
     lib.gsq_combine_rows.argtypes = [xp, vp, vp, vp, vp, vp]
     lib.gsq_combine_rows_grad.argtypes = [xp, vp, vp, vp, vp, vp, vp, vp]
-    for name in PRODUCT_EXPORTS + ROUTING_EXPORTS:
+    ap = ctypes.POINTER(CAdapters)
+    lib.gsq_adapter_forward.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.gsq_adapter_input_grad.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.gsq_adapter_weight_grad.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp]
+    for name in PRODUCT_EXPORTS + ROUTING_EXPORTS + ADAPTER_EXPORTS:
         getattr(lib, name).restype = ctypes.c_int
     for name in ("gsq_layer_init", "gsq_step", "gsq_step_static", "gsq_harden", "gsq_pack",
                  "gsq_get_state", "gsq_set_state", "gsq_get_intermediates", "gsq_gumbel", "gsq_check",
@@ -658,3 +669,87 @@ def combine_rows_grad(dout, rows, slots, weights, drows, dweights, stream=None):
     _check(load().gsq_combine_rows_grad(ctypes.byref(g), dout.data_ptr(), rows.data_ptr(), slots.data_ptr(),
                                         weights.data_ptr(), drows.data_ptr(), dweights.data_ptr(),
                                         _raw_stream(stream, dev)))
+
+
+# ---- low-rank adapters of many requests beside a shared projection: rows request by request, with device int64
+# ``offsets`` of the requests (None: one), the int32 adapter ``index`` of each (-1: none; None: request i has adapter
+# i), a: adapters x rank x I, b: adapters x O x rank, and float32 ``scales`` of the adapters (None: ones).
+
+def _adapter_sizes(a, b, rows, dtype, offsets, index):
+    """The sizes of a call from the shapes of a and b (or of their gradients), which have to fit each other."""
+    if len(a) != 3 or len(b) != 3:
+        raise ValueError(f"a must be adapters x rank x I and b adapters x O x rank, got {tuple(a)} and {tuple(b)}")
+    (n, q, i), o = a, b[1]
+    segments = 1 if offsets is None else offsets.numel() - 1
+    if max(n, q, i, o, segments) >= 1 << 31:
+        _int32("the largest size of the adapters", max(n, q, i, o, segments))
+    if index is None and n != segments:
+        raise ValueError(f"{n} adapters for {segments} requests need an index")
+    if tuple(b) != (n, o, q):
+        raise ValueError(f"b must have the shape {(n, o, q)}, got {tuple(b)}")
+    return CAdapters(segments, n, q, o, i, dtype, rows)
+
+
+def _adapter_args(g, index, scales):
+    import torch
+    args = ()
+    if index is not None:
+        args += (("index", index, (g.segments,), (torch.int32,)),)
+    if scales is not None:
+        args += (("scales", scales, (g.adapters,), (torch.float32,)),)
+    return args
+
+
+def adapter_forward(x, a, b, hidden, out, offsets=None, index=None, scales=None, base=None, stream=None):
+    """out[r] = base[r] + scale B (A x[r]) with the adapter of the row's request, hidden[r] = A x[r] (float32, rows x
+    rank); x, a, b, base, out: bfloat16 or float16.  ``base`` is the shared projection's output: None for zeros, or
+    out itself."""
+    import torch
+    r, dt, types = _row_count(x, "x"), _rows_dtype(x), (x.dtype,)
+    g = _adapter_sizes(a.shape, b.shape, r, dt, offsets, index)
+    q, o, i = g.rank, g.out_features, g.in_features
+    args = (("x", x, (r, i), types), ("a", a, a.shape, types), ("b", b, b.shape, types),
+            ("hidden", hidden, (r, q), (torch.float32,)), ("out", out, (r, o), types))
+    if base is not None:
+        args += (("base", base, (r, o), types),)
+    dev = _checked(args + _adapter_args(g, index, scales), offsets, g.segments)
+    _check(load().gsq_adapter_forward(ctypes.byref(g), x.data_ptr(), a.data_ptr(), b.data_ptr(), _address(offsets),
+                                      _address(index), _address(scales), _address(base), hidden.data_ptr(),
+                                      out.data_ptr(), _raw_stream(stream, dev)))
+
+
+def adapter_input_grad(dy, a, b, dhidden, out, offsets=None, index=None, scales=None, base=None, stream=None):
+    """out[r] = base[r] + A^T dhidden[r], dhidden[r] = scale B^T dy[r] (float32, rows x rank): the gradients of
+    adapter_forward's x and hidden.  ``base`` is the shared projection's gradient of x: None for zeros, or out
+    itself."""
+    import torch
+    r, dt, types = _row_count(dy, "dy"), _rows_dtype(dy), (dy.dtype,)
+    g = _adapter_sizes(a.shape, b.shape, r, dt, offsets, index)
+    q, o, i = g.rank, g.out_features, g.in_features
+    args = (("dy", dy, (r, o), types), ("a", a, a.shape, types), ("b", b, b.shape, types),
+            ("dhidden", dhidden, (r, q), (torch.float32,)), ("out", out, (r, i), types))
+    if base is not None:
+        args += (("base", base, (r, i), types),)
+    dev = _checked(args + _adapter_args(g, index, scales), offsets, g.segments)
+    _check(load().gsq_adapter_input_grad(ctypes.byref(g), dy.data_ptr(), a.data_ptr(), b.data_ptr(),
+                                         _address(offsets), _address(index), _address(scales), _address(base),
+                                         dhidden.data_ptr(), out.data_ptr(), _raw_stream(stream, dev)))
+
+
+def adapter_weight_grad(dy, x, hidden, dhidden, da, db, offsets=None, index=None, scales=None, accumulate=False,
+                        stream=None):
+    """da = sum of dhidden[r]^T x[r] and db = scale times the sum of dy[r]^T hidden[r] over each adapter's rows, in the
+    type of x or in float32; ``accumulate`` adds to float32 ones."""
+    import torch
+    r, dt, types, floats = _row_count(x, "x"), _rows_dtype(x), (x.dtype,), (torch.float32,)
+    g = _adapter_sizes(da.shape, db.shape, r, dt, offsets, index)
+    q, o, i = g.rank, g.out_features, g.in_features
+    args = (("dy", dy, (r, o), types), ("x", x, (r, i), types), ("hidden", hidden, (r, q), floats),
+            ("dhidden", dhidden, (r, q), floats), ("da", da, da.shape, types + floats),
+            ("db", db, db.shape, (da.dtype,)))
+    dev = _checked(args + _adapter_args(g, index, scales), offsets, g.segments)
+    _check(load().gsq_adapter_weight_grad(ctypes.byref(g), dy.data_ptr(), x.data_ptr(), hidden.data_ptr(),
+                                          dhidden.data_ptr(), _address(offsets), _address(index), _address(scales),
+                                          da.data_ptr(), db.data_ptr(),
+                                          DT_FP32 if da.dtype is torch.float32 else dt, 1 if accumulate else 0,
+                                          _raw_stream(stream, dev)))

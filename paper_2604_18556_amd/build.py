@@ -15,7 +15,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libgsq.so")
 SOURCES = ["gsq_linear.hip", "gsq_product.hip", "gsq_elem.hip", "gsq_elem64.hip", "gsq_contract.hip",
-           "gsq_api.hip", "gsq_route.hip", "gsq_product_api.hip", "gsq_exchange.hip", "gsq_route_api.hip"]   # those that take longest first
+           "gsq_adapter.hip", "gsq_api.hip", "gsq_route.hip", "gsq_product_api.hip", "gsq_exchange.hip",
+           "gsq_route_api.hip", "gsq_adapter_api.hip"]   # those that take longest first
 
 # -packed-fp32-ops: keep the compiler from emitting packed fp32 arithmetic
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

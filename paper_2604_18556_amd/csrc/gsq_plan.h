@@ -133,6 +133,15 @@ inline RowsPlan plan_packed(int64_t rows, int64_t groups, int O, int blocks, boo
   return cheapest(rows, groups, O, slabs, large, false, kRingWaves, best, plan);
 }
 
+// hidden and dhidden of the adapters: rows times a matrix of `rank` columns by wavefronts that share the sum, at the
+// costs of plan_rows.
+inline RowsPlan plan_adapter(int64_t rows, int64_t segments, int rank, int slabs, bool tight) {
+  const TileCost aligned[] = {{64, 64, 1, 0.165, 0.22}, {64, 16, 1, 0.1, 0.115}, {16, 64, 1, 0.06, 0.1}, {16, 16, 0.5, 0.02, 0.055}};
+  const TileCost loose[] = {{64, 64, 1, 0.17, 0.42}, {64, 16, 1, 0.1, 0.21}, {16, 64, 1, 0.07, 0.15}, {16, 16, 0.5, 0.025, 0.08}};
+  double best = 1e30;
+  return cheapest(rows, segments, rank, slabs, tight ? aligned : loose, true, std::min(slabs, kSplitWaves), best, RowsPlan{});
+}
+
 // How a sum over rows is cut: tiles of `size` x `size`.  Where nothing fits a launch, one that does not.
 struct SumsPlan {
   bool split;
