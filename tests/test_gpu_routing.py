@@ -344,7 +344,8 @@ def combine_ref(rows, slots, weights):
 
 
 EXCHANGES = [(1, 1, 1), (3, 2, 7), (5, 3, 8), (70, 8, 64), (33, 9, 203), (2, 33, 24), (19, 4, 1000), (9, 8, 7168),
-             (300, 6, 72), (4, 2, 20001), (17, 1, 2048)]
+             (300, 6, 72), (4, 2, 20001), (17, 1, 2048),
+             (7, 8, 520), (5, 8, 516), (3, 10, 2056), (6, 8, 264), (40, 1, 3), (9, 2, 5)]
 
 
 @pytest.mark.parametrize("dtype", [FP32, BF16, FP16], ids=["fp32", "bf16", "fp16"])
@@ -389,6 +390,40 @@ def test_exchange(dev, t, k, c, shift, dtype):
         prod = picked * dy.double()[:, None]
         assert ((dw.cpu().double() - prod.sum(-1)).abs() <= c * 2 * U * prod.abs().sum(-1)).all()
         assert not dw.cpu()[~some].any()
+
+
+@pytest.mark.parametrize("t,k,c", [(1100, 4, 4096), (5000, 1, 4104)])
+def test_exchanges_that_no_cache_holds(dev, t, k, c):
+    """Against the same sums by torch on the GPU, from the bounds above; rows that no slot names stay."""
+    gen = torch.Generator(device=dev).manual_seed(t)
+    n = t * k + 5
+    slots = torch.randperm(n, generator=gen, device=dev)[:t * k].view(t, k).int()
+    slots[3, 0], slots[t - 1, k - 1] = -1, n
+    some = (slots >= 0) & (slots < n)
+    at = torch.where(some, slots, 0).long()
+    x, rows = (torch.randn(m, c, generator=gen, device=dev).to(BF16) for m in (t, n))
+    w = torch.randn(t, k, generator=gen, device=dev)
+    out, y = torch.full((n, c), 7.0, dtype=BF16, device=dev), torch.empty(t, c, dtype=BF16, device=dev)
+    B.dispatch_rows(x, slots, out)
+    B.combine_rows(rows, slots, y, weights=w)
+    drows, dw = torch.full((n, c), 7.0, dtype=BF16, device=dev), torch.empty(t, k, device=dev)
+    B.combine_rows_grad(x, rows, slots, w, drows, dw)
+    named = torch.zeros(n, dtype=torch.bool, device=dev)
+    named[slots[some].long()] = True
+    assert (out[~named] == 7).all() and (drows[~named] == 7).all()
+    ref, mag = torch.zeros(t, c, dtype=torch.float64, device=dev), torch.zeros(t, c, dtype=torch.float64, device=dev)
+    for j in range(k):
+        on = some[:, j]
+        assert torch.equal(out[at[on, j]], x[on])
+        got, want = drows[at[on, j]].double(), w[on, j:j + 1].double() * x[on].double()
+        assert ((got - want).abs() <= want.abs() * (U + half_step(BF16) * (1 + U)) + smallest(BF16)).all()
+        part = rows[at[:, j]].double() * on[:, None]
+        ref += part * w[:, j:j + 1]
+        mag += (part * w[:, j:j + 1]).abs()
+        prod = part * x.double()
+        assert ((dw[:, j].double() - prod.sum(-1)).abs() <= c * 2 * U * prod.abs().sum(-1)).all()
+    err = (k + 1) * U * mag
+    assert ((y.double() - ref).abs() <= err + half_step(BF16) * (ref.abs() + err) + smallest(BF16)).all()
 
 
 def test_exchange_gradients_are_differences(dev):
