@@ -20,7 +20,7 @@ struct AdapterArgs {
   void* out;
   void *da, *db;
   int32_t out_dtype, accumulate;
-  int32_t vector_hidden, vector_out;   // hidden four at a time; out and base 16 bytes at a time
+  int32_t vector_hidden;       // hidden may be stored four at a time
 };
 
 hipError_t launch_adapter_rows(int form, int dtype, const AdapterArgs& p, hipStream_t s);   // kForward, kInputGrad

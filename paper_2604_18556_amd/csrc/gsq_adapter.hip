@@ -78,8 +78,12 @@ __device__ __forceinline__ void down_tile(const AdapterArgs& p, int e, int64_t f
   }
 }
 
+// Wavefronts that share a tile: as many as the LDS holds slabs for, sixteen at most.
+template <int TM, int TN>
+constexpr int kDownWaves = (TM + TN) * ROW_BYTES * 16 < (int)LDS_BYTES ? 16 : 8;
+
 template <class T, int kForm, int TM, int TN, bool kLoose>
-__global__ __launch_bounds__(64 * kSplitWaves) void k_adapter_down(AdapterArgs p) {
+__global__ __launch_bounds__((64 * kDownWaves<TM, TN>)) void k_adapter_down(AdapterArgs p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   const int tiles_n = (p.q + TN - 1) / TN;
   PanelPlace at;
@@ -98,8 +102,15 @@ __global__ __launch_bounds__(64 * kSplitWaves) void k_adapter_down(AdapterArgs p
 // ------------------------------------------------------------------ y = base + s B hidden, dx = base + A^T dhidden
 // hidden is split into two 16-bit parts, so that the product keeps 16 bits of its mantissa (bf16; fp16 22) and runs at
 // the matrix cores' 16-bit rate twice: by fp32 instructions it would take eight times as long.  fp16 rows are taken
-// times a power of two that brings their largest value to 2^14, as its exponent would not hold both parts.
-constexpr int kUpRows = 64, kUpCols = 64, kUpWaves = 4;
+// times a power of two that brings their largest value to 2^13 .. 2^14, as its exponent would not hold both parts.
+//
+// 64 columns of the adapter's matrix are the instructions' rows, in four blocks: row 4 g + c of block j is column
+// up_column(g, j) + c, so that a lane's results are twice eight neighbouring columns of one row of y, and four lanes
+// store 64 bytes of it together (with 16 neighbouring columns to a lane, 4096 rows of 14336 took 99 us, XX now).
+constexpr int kUpCols = 64, kUpWaves = 4, kUpRows = 16 * kUpWaves;
+constexpr int kUpBlock = 32 * kUpCols * 2;     // bytes of 32 of the rank for these columns
+
+__device__ __forceinline__ int up_column(int g, int j) { return 32 * (j >> 1) + 8 * g + 4 * (j & 1); }
 
 // Eight hidden values of a row from k on, those from q on zeros.
 __device__ __forceinline__ void load_hidden(const float* row, int k, int q, float (&v)[8]) {
@@ -111,9 +122,30 @@ __device__ __forceinline__ void load_hidden(const float* row, int k, int q, floa
   }
 }
 
+// The power of two that a row is taken by: found by the four lanes that share the row.
 template <class T>
-__device__ __forceinline__ void split_hidden(const float (&v)[8], float by, typename T::frag& hi, typename T::frag& lo) {
+__device__ __forceinline__ float hidden_power(const float* row, int q) {
+  if constexpr (T::kDtype != GSQ_DT_FP16) return 1.f;
+  float top = 0.f;
+  for (int k = 8 * ((threadIdx.x & 63) >> 4); k < q; k += 32) {
+    float v[8];
+    load_hidden(row, k, q, v);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) top = fmaxf(top, fabsf(v[c]));
+  }
+  top = fmaxf(top, __shfl_xor(top, 16, 64));
+  top = fmaxf(top, __shfl_xor(top, 32, 64));
+  // infinities pass as they are (and NaN, which fmaxf leaves out); what is very small, as far as it goes
+  if (!(top > 0.f && top < __builtin_huge_valf())) return 1.f;
+  return exp2f((float)(13 - max((int)(__float_as_uint(top) >> 23) - 127, -100)));
+}
+
+template <class T>
+__device__ __forceinline__ void split_hidden(const float* row, int k, int q, float by, typename T::frag& hi,
+                                             typename T::frag& lo) {
   using E = typename T::elem;
+  float v[8];
+  load_hidden(row, k + 8 * ((threadIdx.x & 63) >> 4), q, v);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float x = v[i] * by;
@@ -124,195 +156,307 @@ __device__ __forceinline__ void split_hidden(const float (&v)[8], float by, type
   }
 }
 
-// 16 values of a row: as whole 16 bytes, or those that there are.
-template <class E>
-struct Sixteen {
-  E v[16];
-  __device__ __forceinline__ void load(const E* p, int n, bool whole) {
-    if (whole) {
-      const i32x4* q = reinterpret_cast<const i32x4*>(p);
-      const i32x4 a = q[0], b = q[1];
-      __builtin_memcpy(v, &a, 16);
-      __builtin_memcpy(v + 8, &b, 16);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = i < n ? p[i] : (E)0.f;
-    }
-  }
-  __device__ __forceinline__ void store(E* p, int n, bool whole) const {
-    if (whole) {
-      i32x4 a, b;
-      __builtin_memcpy(&a, v, 16);
-      __builtin_memcpy(&b, v + 8, 16);
-      reinterpret_cast<i32x4*>(p)[0] = a;
-      reinterpret_cast<i32x4*>(p)[1] = b;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (i < n) p[i] = v[i];
-    }
-  }
-};
-
-// A wavefront's columns of the adapter's matrix, as the instructions' rows: row 4 g + c of block j is column 16 g +
-// 4 j + c, so that a lane's results are 16 neighbouring columns of a row.
-// B, whose rows run along the rank: straight from memory.
+// 64 columns of the matrix in LDS, in blocks of 32 of the rank; 256 lanes fill a block together, 16 bytes each: at() says
+// where the lane's 16 bytes of a block come from (16-byte aligned arrays; nullptr: zeros), held() what they hold else.
+// B, whose rows run along the rank: a column has 64 bytes of a block, its four chunks turned so that fragment reads
+// fall on distinct banks.
 template <class T>
 struct UpAlong {
   using E = typename T::elem;
-  static constexpr size_t LDS = 0;
-  const E* w;                  // the first column's row
+  const E* w;                  // the adapter's
   int cols, q;
-  __device__ __forceinline__ void begin(int, uint8_t*) {}
-  __device__ __forceinline__ typename T::frag frag(int k, int j) const {
-    const int lane = threadIdx.x & 63, i = lane & 15, n = 16 * (i >> 2) + 4 * j + (i & 3), at = k + 8 * (lane >> 4);
-    return __builtin_bit_cast(typename T::frag, load_chunk(w + (int64_t)min(n, cols - 1) * q + at, q - at));
+  static __device__ __forceinline__ int turn(int col) { return -(col >> 3) & 3; }
+  __device__ __forceinline__ const E* place(int n0, int k, int t, int& left) const {
+    const int col = t >> 2, at = k + 8 * ((t & 3) ^ turn(col));
+    left = q - at;
+    return w + (int64_t)min(n0 + col, cols - 1) * q + at;
+  }
+  static __device__ __forceinline__ typename T::frag frag(const uint8_t* block, int j) {
+    const int lane = threadIdx.x & 63, i = lane & 15, col = up_column(i >> 2, j) + (i & 3);
+    return *reinterpret_cast<const typename T::frag*>(block + col * 64 + (((lane >> 4) ^ turn(col)) << 4));
   }
 };
-// A, whose rows are the rank: 64 of them and 64 columns in LDS, read by transposing reads.
-template <class T, bool kLoose>
+// A, whose rows are the rank: 32 rows of 64 columns, read by transposing reads.
+template <class T>
 struct UpAcross {
   using E = typename T::elem;
-  using Tight = SlabAcross<kUpCols, 8>;
-  static constexpr size_t LDS = 64 * Tight::PITCH;
-  const E* w;                  // the first column
-  int64_t ld;
+  using Slab = SlabAcross<kUpCols>;
+  const E* w;
   int cols, q;
-  uint8_t* lds = nullptr;
-  __device__ __forceinline__ void begin(int k, uint8_t* own) {
-    lds = own;
-    if (k % kSlabRows) return;
-    wait_reads();              // of the slab before
-    if constexpr (kLoose) {
-      LooseAcross<E, kUpCols> s(w + k * ld, ld, cols, q - k, 0);
-      s.fetch(0, own);
-      s.commit(own);
-    } else {
-      Copied<Tight> s(w + k * ld, ld * 2, cols, q - k, 0, threadIdx.x & 63);
-      s.fetch(0, own);
-    }
-    wait_all();
+  __device__ __forceinline__ const E* place(int n0, int k, int t, int& left) const {
+    int row, chunk;
+    Slab::place(t, row, chunk);
+    const int col = n0 + chunk * 8;
+    left = k + row < q ? cols - col : 0;
+    return w + (int64_t)(k + row) * cols + col;
   }
-  __device__ __forceinline__ typename T::frag frag(int k, int j) const {
+  static __device__ __forceinline__ typename T::frag frag(const uint8_t* block, int j) {
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-    const int lane = threadIdx.x & 63, r = k % kSlabRows + (lane >> 4) * 8 + ((lane & 15) >> 2);
-    const uint8_t* at = lds + r * Tight::PITCH + (((lane & 3) ^ Tight::turn(r)) << 5) + j * 8;
+    const int lane = threadIdx.x & 63, r = (lane >> 4) * 8 + ((lane & 15) >> 2);
+    const int col = up_column(lane & 3, j);
+    const uint8_t* at = block + r * Slab::PITCH + (((col >> 4) ^ Slab::turn(r)) << 5) + (col & 15) * 2;
     union { s16x4 s[2]; typename T::frag v; } u;
     u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at);
-    u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * Tight::PITCH));
+    u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * Slab::PITCH));
     return u.v;
   }
 };
 
-// SUB x 16 rows and 64 columns by one wavefront.
-template <class T, int SUB, class W>
-__device__ __forceinline__ void up_tile(const AdapterArgs& p, W w, float scale, int64_t first, int ms, int n0, int ns,
-                                        uint8_t* own) {
-  using E = typename T::elem;
-  const int lane = threadIdx.x & 63, m = lane & 15, col = n0 + 16 * (lane >> 4);
-  const E* base = static_cast<const E*>(p.base);
-  E* out = static_cast<E*>(p.out);
-  const bool whole = p.vector_out && col + 16 <= ns;
-  Sixteen<E> old[SUB];
-#pragma unroll
-  for (int i = 0; i < SUB; ++i) {
-    const int r = i * 16 + m;
-    old[i].load(base + (first + r) * ns + col, base && r < ms ? ns - col : 0, whole && base && r < ms);
+// One block of the matrix to LDS: copied directly (kCopied: 16-byte aligned), or by way of registers.
+template <class W, bool kCopied>
+struct UpBlock {
+  i32x4 held;
+  __device__ __forceinline__ void fetch(const W& w, int n0, int k, uint8_t* block) {
+    int left;
+    const int t = threadIdx.x % (64 * kUpWaves);
+    const auto* from = w.place(n0, k, t, left);
+    if constexpr (kCopied)
+      copy_to_lds(left > 0 ? reinterpret_cast<const uint8_t*>(from) : zeros(), block + (t & ~63) * 16);
+    else
+      held = load_chunk(from, left);
   }
-  const float* h[SUB];
-  float by[SUB];
+  __device__ __forceinline__ void commit(uint8_t* block) const {
+    if constexpr (!kCopied) *reinterpret_cast<i32x4*>(block + (threadIdx.x % (64 * kUpWaves)) * 16) = held;
+  }
+};
+
+// How y is gone through: value by value, by 16 bytes (rows are whole pieces), or by these past the caches.
+enum { kNarrow = 0, kWide = 1, kStream = 2 };
+
+// Of 16 rows of y, 64 columns: a lane has columns 8 g .. and 32 + 8 g .., eight each, of row m = lane % 16 (g = lane /
+// 16).  In memory the lane goes to two half-rows of 64 bytes, those of rows m % 8 and m % 8 + 8, so that eight lanes
+// have a row's whole 128 bytes at once; the lanes 8 apart exchange what is the other's.
+template <class E, int kBy>
+struct Sixteen {
+  typedef E vec __attribute__((ext_vector_type(8)));
+  i32x4 part[2];
+  static __device__ __forceinline__ void exchange(i32x4& a, i32x4& b) {
+    const bool high = threadIdx.x & 8;
+    i32x4 mine = high ? a : b, other;
 #pragma unroll
-  for (int i = 0; i < SUB; ++i) {
-    h[i] = p.hidden + (first + min(i * 16 + m, ms - 1)) * p.q;
-    by[i] = 1.f;
-    if constexpr (T::kDtype == GSQ_DT_FP16) {
-      float top = 0.f;
-      for (int k = 8 * (lane >> 4); k < p.q; k += 32) {
-        float v[8];
-        load_hidden(h[i], k, p.q, v);
+    for (int i = 0; i < 4; ++i) other[i] = __builtin_amdgcn_update_dpp(0, mine[i], 0x128, 0xf, 0xf, true);   // row_ror:8
+    a = high ? other : a;
+    b = high ? b : other;
+  }
+  // `first`: row 0's element at column 0; columns n .. below cols, rows below `rows` (none: zeros)
+  __device__ __forceinline__ void load(const E* first, int64_t ld, int rows, int n, int cols) {
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) top = fmaxf(top, fabsf(v[c]));
+    for (int h = 0; h < 2; ++h) {
+      if constexpr (kBy != kNarrow) {
+        const int r = (m & 7) + 8 * h, c = n + 32 * (m >> 3) + 8 * g;
+        const i32x4* from = reinterpret_cast<const i32x4*>(first + r * ld + c);
+        part[h] = i32x4{};
+        if (r < rows && c < cols) part[h] = kBy == kStream ? __builtin_nontemporal_load(from) : *from;
+      } else {
+        const int c = n + 32 * h + 8 * g;
+        vec v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = m < rows && c + i < cols ? first[m * ld + c + i] : (E)0.f;
+        part[h] = __builtin_bit_cast(i32x4, v);
       }
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      // infinities (and NaN, which fmaxf leaves out) pass as they are; what is very small, as far as it goes
-      if (top > 0.f && top < __builtin_huge_valf()) by[i] = exp2f((float)(13 - max((int)(__float_as_uint(top) >> 23) - 127, -100)));
     }
   }
-  f32x4 acc[SUB][4] = {};
-  for (int k = 0; k < p.q; k += 32) {
-    w.begin(k, own);
-    typename T::frag f[4];
+  // sums times s and what was loaded, rounded once
+  __device__ __forceinline__ void store(const f32x4 (&acc)[4], float s, E* first, int64_t ld, int rows, int n, int cols) const {
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+    i32x4 old[2] = {part[0], part[1]}, res[2];
+    if constexpr (kBy != kNarrow) exchange(old[0], old[1]);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) f[j] = w.frag(k, j);
+    for (int h = 0; h < 2; ++h) {
+      const vec o = __builtin_bit_cast(vec, old[h]);
+      vec r;
 #pragma unroll
-    for (int i = 0; i < SUB; ++i) {
-      float v[8];
-      load_hidden(h[i], k + 8 * (lane >> 4), p.q, v);
-      typename T::frag hi, lo;
-      split_hidden<T>(v, by[i], hi, lo);
+      for (int i = 0; i < 8; ++i) r[i] = (E)fmaf(acc[2 * h + i / 4][i % 4], s, (float)o[i]);
+      res[h] = __builtin_bit_cast(i32x4, r);
+    }
+    if constexpr (kBy != kNarrow) exchange(res[0], res[1]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = T::mfma(f[j], hi, acc[i][j]);
+    for (int h = 0; h < 2; ++h) {
+      if constexpr (kBy != kNarrow) {
+        const int r = (m & 7) + 8 * h, c = n + 32 * (m >> 3) + 8 * g;
+        i32x4* to = reinterpret_cast<i32x4*>(first + r * ld + c);
+        if (r < rows && c < cols) {
+          if constexpr (kBy == kStream)
+            __builtin_nontemporal_store(res[h], to);
+          else
+            *to = res[h];
+        }
+      } else {
+        const int c = n + 32 * h + 8 * g;
+        const vec r = __builtin_bit_cast(vec, res[h]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = T::mfma(f[j], lo, acc[i][j]);
+        for (int i = 0; i < 8; ++i)
+          if (m < rows && c + i < cols) first[m * ld + c + i] = r[i];
+      }
     }
   }
-#pragma unroll
-  for (int i = 0; i < SUB; ++i) {
-    const int r = i * 16 + m;
-    if (r >= ms || col >= ns) continue;
-    const float s = scale / by[i];           // by is a power of two
-    Sixteen<E> res;
-#pragma unroll
-    for (int c = 0; c < 16; ++c) res.v[c] = (E)fmaf(acc[i][c / 4][c % 4], s, (float)old[i].v[c]);
-    res.store(out + (first + r) * ns + col, ns - col, whole);
-  }
-}
+};
 
 // Rows without an adapter: the base, or zeros.
 template <class E>
-__device__ __forceinline__ void copy_base(const AdapterArgs& p, int64_t first, int ms, int n0, int ns) {
+__device__ __forceinline__ void copy_base(const AdapterArgs& p, int64_t first, int ms, int n0, int cols, int ns) {
   if (p.base == p.out) return;
-  const int cols = min(ns - n0, kUpCols), lane = threadIdx.x & 63;
-  if (lane >= cols) return;
-  for (int r = 0; r < ms; ++r) {
-    const int64_t at = (first + r) * ns + n0 + lane;
-    static_cast<E*>(p.out)[at] = p.base ? static_cast<const E*>(p.base)[at] : (E)0.f;
+  for (int r = threadIdx.x >> 6; r < ms; r += blockDim.x >> 6)
+    for (int c = threadIdx.x & 63; c < cols; c += 64) {
+      const int64_t at = (first + r) * ns + n0 + c;
+      static_cast<E*>(p.out)[at] = p.base ? static_cast<const E*>(p.base)[at] : (E)0.f;
+    }
+}
+
+// Waits until the blocks that this wavefront has copied are there, of whose later accesses `after` are at least on
+// their way still.
+__device__ __forceinline__ void wait_blocks(int after) {
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  if (after == 4)
+    wait_vm<4>();
+  else if (after == 2)
+    wait_vm<2>();
+  else
+    wait_vm<0>();
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+}
+
+// Panels of 64 rows (16 to a wavefront) and `steps` times 64 columns.  A panel's hidden stays in registers as long as its
+// rank fits KS blocks.  While a step is multiplied, the matrix of the next is on its way to LDS, and the base of the next
+// two to registers.
+template <class T, int kForm, int KS, bool kCopied, int kBy>
+__global__ __launch_bounds__(64 * kUpWaves) void k_adapter_up(AdapterArgs p, int steps, int chunks) {
+  using E = typename T::elem;
+  using W = std::conditional_t<kForm == kForward, UpAlong<T>, UpAcross<T>>;
+  __shared__ __attribute__((aligned(16))) uint8_t smem[2][KS * kUpBlock];
+  const int ns = kForm == kForward ? p.O : p.I;
+  PanelPlace at;
+  if (!find_panel(p.rows, kUpRows, blockIdx.x / (unsigned)chunks, at)) return;
+  const int64_t first = at.first + (blockIdx.x / (unsigned)chunks - at.before) * kUpRows;
+  const int ms = (int)min(at.end - first, (int64_t)kUpRows), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n0 = (blockIdx.x % (unsigned)chunks) * steps * kUpCols, n1 = min(n0 + steps * kUpCols, ns);
+  const int e = adapter_of(p, at.group);
+  if (e < 0) return copy_base<E>(p, first, ms, n0, n1 - n0, ns);
+  const W w{static_cast<const E*>(kForm == kForward ? p.b : p.a) + (int64_t)e * p.q * ns, ns, p.q};
+  const float scale = kForm == kForward ? scale_of(p, e) : 1.f;
+
+  const int rows = ms - 16 * wave;             // of this wavefront, if any
+  const float* hid = p.hidden + (first + min(16 * wave + (int)(threadIdx.x & 15), ms - 1)) * p.q;
+  const E* base = static_cast<const E*>(p.base) + (first + 16 * wave) * ns;
+  E* out = static_cast<E*>(p.out) + (first + 16 * wave) * ns;
+  const int base_rows = p.base ? rows : 0;
+  const int passes = (p.q + 32 * KS - 1) / (32 * KS);
+
+  UpBlock<W, kCopied> blocks[KS];
+  Sixteen<E, kBy> even, odd;
+  even.load(base, ns, base_rows, n0, n1);
+  odd.load(base, ns, base_rows, n0 + kUpCols, n1);
+#pragma unroll
+  for (int s = 0; s < KS; ++s) blocks[s].fetch(w, n0, 32 * s, smem[0] + s * kUpBlock);
+  const float by = hidden_power<T>(hid, p.q), undo = scale / by;     // by is a power of two
+  typename T::frag hi[KS], lo[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) split_hidden<T>(hid, 32 * s, p.q, by, hi[s], lo[s]);
+#pragma unroll
+  for (int s = 0; s < KS; ++s) blocks[s].commit(smem[0] + s * kUpBlock);
+  int parity = 0, after = 0;
+  const auto step = [&](int n, Sixteen<E, kBy>& old) {
+    f32x4 acc[4] = {};
+    for (int pass = 0; pass < passes; ++pass) {
+      uint8_t* const here = smem[parity];
+      uint8_t* const there = smem[parity ^ 1];
+      if constexpr (kCopied) wait_blocks(after);
+      slab_barrier();
+      const bool last = pass == passes - 1, more = !last || n + kUpCols < n1;
+      if (more)
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+          blocks[s].fetch(w, last ? n + kUpCols : n, (last ? 0 : pass + 1) * 32 * KS + 32 * s, there + s * kUpBlock);
+      if (rows > 0) {
+        if (passes > 1)
+#pragma unroll
+          for (int s = 0; s < KS; ++s) split_hidden<T>(hid, (pass * KS + s) * 32, p.q, by, hi[s], lo[s]);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          typename T::frag f[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) f[j] = W::frag(here + s * kUpBlock, j);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[j] = T::mfma(f[j], hi[s], acc[j]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[j] = T::mfma(f[j], lo[s], acc[j]);
+        }
+      }
+      if (!kCopied && more)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) blocks[s].commit(there + s * kUpBlock);
+      parity ^= 1;
+      after = 0;
+    }
+    if (rows <= 0) return;
+    old.store(acc, undo, out, ns, rows, n, n1);
+    const int ahead = n + 2 * kUpCols;
+    if (ahead < n1) old.load(base, ns, base_rows, ahead, n1);
+    // with more than eight rows two stores, and two loads unless the columns end within that step
+    if (kBy != kNarrow && rows > 8) after = base_rows && ahead + kUpCols <= n1 ? 4 : 2;
+  };
+  for (int n = n0; n < n1; n += 2 * kUpCols) {
+    step(n, even);
+    if (n + kUpCols < n1) step(n + kUpCols, odd);
   }
 }
 
-template <class T, int kForm, bool kLoose>
-__global__ __launch_bounds__(64 * kUpWaves) void k_adapter_up(AdapterArgs p) {
+// Segments of few rows: panels of 16 and 64 columns to a wavefront, straight from memory; no wavefront waits for another.
+template <class T, int kForm, int kBy>
+__global__ __launch_bounds__(64 * kUpWaves) void k_adapter_up_few(AdapterArgs p) {
   using E = typename T::elem;
-  using W = std::conditional_t<kForm == kForward, UpAlong<T>, UpAcross<T, kLoose>>;
-  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  using W = std::conditional_t<kForm == kForward, UpAlong<T>, UpAcross<T>>;
+  __shared__ __attribute__((aligned(16))) uint8_t smem[kForm == kForward ? 1 : kUpWaves][kUpBlock];
   const int ns = kForm == kForward ? p.O : p.I, wide = kUpCols * kUpWaves, tiles_n = (ns + wide - 1) / wide;
   PanelPlace at;
-  if (!find_panel(p.rows, kUpRows, blockIdx.x / (unsigned)tiles_n, at)) return;
-  int tm, tn;
-  tile_at(lin_of((int)(blockIdx.x - at.before * tiles_n), at.panels * tiles_n), at.panels, tiles_n, tm, tn);
-  const int64_t first = at.first + (int64_t)tm * kUpRows;
-  const int ms = (int)min(at.end - first, (int64_t)kUpRows), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n0 = tn * wide + wave * kUpCols;
-  if (n0 >= ns) return;                        // no barrier follows
-  const int e = adapter_of(p, at.group);
-  if (e < 0) return copy_base<E>(p, first, ms, n0, ns);
-  W w;
-  if constexpr (kForm == kForward) {
-    w.w = static_cast<const E*>(p.b) + ((int64_t)e * p.O + n0) * p.q;
-  } else {
-    w.w = static_cast<const E*>(p.a) + (int64_t)e * p.q * p.I + n0;
-    w.ld = p.I;
+  if (!find_panel(p.rows, 16, blockIdx.x / (unsigned)tiles_n, at)) return;
+  const int64_t first = at.first + (blockIdx.x / (unsigned)tiles_n - at.before) * 16;
+  const int ms = (int)min(at.end - first, (int64_t)16), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int e = adapter_of(p, at.group), n_all = (blockIdx.x % (unsigned)tiles_n) * wide;
+  if (e < 0) return copy_base<E>(p, first, ms, n_all, min(ns - n_all, wide), ns);
+  const int n0 = n_all + wave * kUpCols;
+  if (n0 >= ns) return;
+  const W w{static_cast<const E*>(kForm == kForward ? p.b : p.a) + (int64_t)e * p.q * ns, ns, p.q};
+  const int lane = threadIdx.x & 63;
+  const float* hid = p.hidden + (first + min(lane & 15, ms - 1)) * p.q;
+  Sixteen<E, kBy> old;
+  old.load(static_cast<const E*>(p.base) + first * ns, ns, p.base ? ms : 0, n0, ns);
+  const float by = hidden_power<T>(hid, p.q);
+  f32x4 acc[4] = {};
+  for (int k = 0; k < p.q; k += 32) {
+    typename T::frag f[4], hi, lo;
+    if constexpr (kForm == kForward) {
+      const int i = lane & 15, at_k = k + 8 * (lane >> 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int c = min(n0 + up_column(i >> 2, j) + (i & 3), ns - 1);
+        f[j] = __builtin_bit_cast(typename T::frag, load_chunk(w.w + (int64_t)c * p.q + at_k, p.q - at_k));
+      }
+    } else {
+      uint8_t* const own = smem[wave];
+      i32x4 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        int left;
+        const E* from = w.place(n0, k, u * 64 + lane, left);
+        v[u] = load_chunk(from, left);
+      }
+      wait_reads();                            // of the block before
+#pragma unroll
+      for (int u = 0; u < 4; ++u) *reinterpret_cast<i32x4*>(own + (u * 64 + lane) * 16) = v[u];
+      wait_reads();
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] = W::frag(own, j);
+    }
+    split_hidden<T>(hid, k, p.q, by, hi, lo);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = T::mfma(f[j], hi, acc[j]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = T::mfma(f[j], lo, acc[j]);
   }
-  w.cols = ns - n0;
-  w.q = p.q;
-  const float scale = kForm == kForward ? scale_of(p, e) : 1.f;
-  uint8_t* own = smem + wave * W::LDS;
-  if (ms <= 16)
-    up_tile<T, 1>(p, w, scale, first, ms, n0, ns, own);
-  else
-    up_tile<T, kUpRows / 16>(p, w, scale, first, ms, n0, ns, own);
+  old.store(acc, (kForm == kForward ? scale_of(p, e) : 1.f) / by, static_cast<E*>(p.out) + first * ns, ns, ms, n0, ns);
 }
 
 // ------------------------------------------------------------------ dA, dB: sums over an adapter's rows
@@ -404,7 +548,7 @@ __global__ __launch_bounds__(64 * kWeightWaves) void k_adapter_weights(AdapterAr
 
 template <class T, int kForm, int TM, int TN, bool kLoose>
 hipError_t launch_down(const AdapterArgs& p, hipStream_t s) {
-  const int nk = (int)tiles_of(kForm == kForward ? p.I : p.O, kSlabRows), waves = std::min(nk, kSplitWaves);
+  const int nk = (int)tiles_of(kForm == kForward ? p.I : p.O, kSlabRows), waves = std::min(nk, kDownWaves<TM, TN>);
   return launch_lds<k_adapter_down<T, kForm, TM, TN, kLoose>>(most_panels(p.rows, TM) * tiles_of(p.q, TN), 64 * waves,
                                                               (size_t)waves * (TM + TN) * ROW_BYTES, s, p);
 }
@@ -419,25 +563,36 @@ hipError_t launch_rows(const AdapterArgs& p, const RowsPlan& plan, hipStream_t s
   return e;
 }
 
+constexpr int64_t kStreamBytes = (int64_t)32 << 20;   // of y, as much as the eight L2s hold
+
+template <class T, int kForm, bool kCopied, int kBy>
+hipError_t launch_up(const AdapterArgs& p, const UpPlan& plan, hipStream_t s) {
+  const int ns = kForm == kForward ? p.O : p.I;
+  if (!plan.steps)
+    return launch_lds<k_adapter_up_few<T, kForm, kBy == kNarrow ? kNarrow : kWide>>(plan.blocks, 64 * kUpWaves, 0, s, p);
+  const int chunks = (int)tiles_of(tiles_of(ns, kUpCols), plan.steps);
+  if (p.q <= 32) return launch_lds<k_adapter_up<T, kForm, 1, kCopied, kBy>>(plan.blocks, 64 * kUpWaves, 0, s, p, plan.steps, chunks);
+  if (p.q <= 64) return launch_lds<k_adapter_up<T, kForm, 2, kCopied, kBy>>(plan.blocks, 64 * kUpWaves, 0, s, p, plan.steps, chunks);
+  return launch_lds<k_adapter_up<T, kForm, 4, kCopied, kBy>>(plan.blocks, 64 * kUpWaves, 0, s, p, plan.steps, chunks);
+}
+
 template <class T, int kForm>
 hipError_t launch_both(AdapterArgs p, hipStream_t s) {
   if (p.rows.rows == 0) return hipSuccess;
   const int ks = kForm == kForward ? p.I : p.O, ns = kForm == kForward ? p.O : p.I;
   p.vector_hidden = four_at_once(p.hidden, GSQ_DT_FP32, p.q);
-  p.vector_out = ns % 8 == 0 && aligned16(p.out) && aligned16(p.base);
+  const bool wide = ns % 8 == 0 && aligned16(p.out) && aligned16(p.base);
   const bool tight = kForm == kForward ? p.I % 8 == 0 && aligned16(p.x) && aligned16(p.a)
                                        : p.O % 8 == 0 && p.q % 8 == 0 && aligned16(p.dy) && aligned16(p.b);
+  const bool copied = kForm == kForward ? p.q % 8 == 0 && aligned16(p.b) : p.I % 8 == 0 && aligned16(p.a);
   const RowsPlan plan = plan_adapter(p.rows.rows, p.rows.groups, p.q, (int)tiles_of(ks, kSlabRows), tight);
-  const int64_t up = most_panels(p.rows, kUpRows) * tiles_of(ns, kUpCols * kUpWaves);
-  if (!plan.height || !fits_launch(up, 64 * kUpWaves)) return hipErrorInvalidConfiguration;
+  const UpPlan up = plan_adapter_up(p.rows.rows, p.rows.groups, ns);
+  if (!plan.height || !fits_launch(up.blocks, 64 * kUpWaves)) return hipErrorInvalidConfiguration;
   const hipError_t e = tight ? launch_rows<T, kForm, false>(p, plan, s) : launch_rows<T, kForm, true>(p, plan, s);
   if (e != hipSuccess) return e;
-  if constexpr (kForm == kForward)
-    return launch_lds<k_adapter_up<T, kForm, false>>(up, 64 * kUpWaves, 0, s, p);
-  else if (p.I % 8 == 0 && aligned16(p.a))
-    return launch_lds<k_adapter_up<T, kForm, false>>(up, 64 * kUpWaves, kUpWaves * UpAcross<T, false>::LDS, s, p);
-  else
-    return launch_lds<k_adapter_up<T, kForm, true>>(up, 64 * kUpWaves, kUpWaves * UpAcross<T, true>::LDS, s, p);
+  if (!copied) return wide ? launch_up<T, kForm, false, kWide>(p, up, s) : launch_up<T, kForm, false, kNarrow>(p, up, s);
+  if (wide && p.rows.rows * ns * 2 >= kStreamBytes) return launch_up<T, kForm, true, kStream>(p, up, s);
+  return wide ? launch_up<T, kForm, true, kWide>(p, up, s) : launch_up<T, kForm, true, kNarrow>(p, up, s);
 }
 
 template <class T, class Out>

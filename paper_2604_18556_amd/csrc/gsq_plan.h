@@ -142,6 +142,28 @@ inline RowsPlan plan_adapter(int64_t rows, int64_t segments, int rank, int slabs
   return cheapest(rows, segments, rank, slabs, tight ? aligned : loose, true, std::min(slabs, kSplitWaves), best, RowsPlan{});
 }
 
+// y and dx from hidden: no steps: panels of 16 rows and 256 columns, for segments of 16 rows and fewer; else panels of 64
+// rows and `steps` times 64 columns, such that whole rounds of 1024 workgroups (four on each of 256 CUs) with a start as
+// long as three steps take least.
+struct UpPlan {
+  int steps;
+  int64_t blocks;
+};
+inline UpPlan plan_adapter_up(int64_t rows, int64_t segments, int cols) {
+  if (rows <= 16 * segments) return {0, most_panels(rows, segments, 16) * tiles_of(cols, 256)};
+  const int64_t all = tiles_of(cols, 64), panels = rows / 64 + (std::min(rows, segments) + 1) / 2;
+  int64_t best = INT64_MAX;
+  int steps = 1;
+  for (int n = 1; n <= 32; ++n) {
+    const int64_t cost = tiles_of(panels * tiles_of(all, n), 1024) * (n + 3);
+    if (cost < best) {
+      best = cost;
+      steps = n;
+    }
+  }
+  return {steps, most_panels(rows, segments, 64) * tiles_of(all, steps)};
+}
+
 // How a sum over rows is cut: tiles of `size` x `size`.  Where nothing fits a launch, one that does not.
 struct SumsPlan {
   bool split;
