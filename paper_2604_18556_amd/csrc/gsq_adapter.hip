@@ -460,81 +460,191 @@ __global__ __launch_bounds__(64 * kUpWaves) void k_adapter_up_few(AdapterArgs p)
 }
 
 // ------------------------------------------------------------------ dA, dB: sums over an adapter's rows
-// fp32 matrix instructions of 16 x 16 outputs and four rows: a lane has one row of each operand, so that nothing is
-// transposed, and hidden keeps its 32 bits.  A lane's 16 bytes of x (or dy) are eight columns, which go to eight
-// blocks; the instructions' rows are the rank.
-constexpr int kWeightWaves = 8, kWeightCols = 128;
+// The instructions' rows are the rank, their columns those of x (or dy), and both run across their arrays.  x comes to
+// LDS in slabs of 32 rows, two of them for each wavefront so that one is on its way while the other is used, and is read
+// by transposing reads; a lane reads its eight hidden values of a column itself.
+// fp32 instructions would need no transposing, but take five times as long as the bf16 ones of the exact parts that
+// hidden is split into, three of 8 bits (fp16 x: two parts, and the product of the two smallest is left out, 2^-25 of
+// the whole): with them 4096 rows of 4096 + 14336 at rank 32 took 92 us.
+constexpr int kWeightCols = 128, kWeightBlocks = kWeightCols / 16;
+constexpr int kWeightRows = 32, kWeightSlab = kWeightRows * kWeightCols * 2;
 
-template <class T, int QB, class Out>
-__global__ __launch_bounds__(64 * kWeightWaves) void k_adapter_weights(AdapterArgs p, int tiles_a, int tiles_b, int parts) {
+// The slabs of an adapter's rows, of which each wavefront takes every waves-th.
+struct AdapterSlabs {
+  const AdapterArgs& p;
+  int e, s0 = 0;
+  uint64_t mine = 0;           // segments from s0 on that are left
+  int64_t at = 0, end = 0;     // rows of the present segment that are left
+  int64_t skip;                // slabs to the next
+  bool more = true;
+
+  __device__ __forceinline__ AdapterSlabs(const AdapterArgs& args, int adapter, int wave) : p(args), e(adapter), skip(wave) {
+    if (!p.index) {
+      if (e < p.rows.groups) group_rows(p.rows, e, at, end);
+    } else {
+      look();
+    }
+  }
+  __device__ __forceinline__ void look() {
+    const int lane = threadIdx.x & 63, s = min(s0 + lane, p.rows.groups - 1);
+    mine = __ballot(s0 + lane < p.rows.groups && p.index[s] == e);
+  }
+  // The next slab: its first row and how many it has.
+  __device__ __forceinline__ bool next(int64_t& first, int& rows) {
+    while (true) {
+      const int64_t left = (end - at + kWeightRows - 1) / kWeightRows;
+      if (skip < left) {
+        first = at + skip * kWeightRows;
+        rows = (int)min(end - first, (int64_t)kWeightRows);
+        at = first;
+        skip = blockDim.x >> 6;
+        return true;
+      }
+      skip -= left;
+      if (!p.index) return false;
+      while (!mine) {
+        s0 += 64;
+        if (s0 >= p.rows.groups) return false;
+        look();
+      }
+      group_rows(p.rows, s0 + __builtin_ctzll(mine), at, end);
+      mine &= mine - 1;
+    }
+  }
+};
+
+// Parts of 8 bits, cut off one after another, that add up to v exactly (24 bits in three; what is not finite makes the
+// later ones NaN).
+template <int N>
+__device__ __forceinline__ void exact_parts(const float (&v)[8], bf16x8 (&part)[N]) {
+  uint32_t rest[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) rest[i] = __float_as_uint(v[i]);
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    i32x4 pairs;                               // the upper halves of two values each
+#pragma unroll
+    for (int i = 0; i < 4; ++i) pairs[i] = (int)__builtin_amdgcn_perm(rest[2 * i + 1], rest[2 * i], 0x07060302u);
+    part[k] = __builtin_bit_cast(bf16x8, pairs);
+    if (k + 1 < N)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        rest[i] = __float_as_uint(__uint_as_float(rest[i]) - __uint_as_float(rest[i] & 0xffff0000u));
+  }
+}
+
+template <class T, int QB, class Out, bool kLoose>
+__global__ __launch_bounds__(64 * kSplitWaves) void k_adapter_weights(AdapterArgs p, int tiles_a, int tiles_b, int parts) {
   using E = typename T::elem;
-  __shared__ f32x4 s_sum[kWeightWaves][8][64];
-  constexpr int AHEAD = 4;                     // loads of rows in flight
+  constexpr int kCopies = kWeightSlab / 1024;
+  using Slab = std::conditional_t<kLoose, LooseAcross<E, kWeightCols, kCopies>, Copied<SlabAcross<kWeightCols, kCopies>>>;
+  constexpr int NB = kWeightBlocks, XP = T::kDtype == GSQ_DT_FP16 ? 2 : 1, HP = 3;
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   const int tiles = (tiles_a + tiles_b) * parts;
   const int e = blockIdx.x / (unsigned)tiles, tile = blockIdx.x % (unsigned)tiles / parts, part = blockIdx.x % (unsigned)parts;
   const bool of_a = tile < tiles_a;
   const int ns = of_a ? p.I : p.O, n0 = (of_a ? tile : tile - tiles_a) * kWeightCols, j0 = part * QB * 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const E* in = static_cast<const E*>(of_a ? p.x : p.dy);
+  const E* in = static_cast<const E*>(of_a ? p.x : p.dy) + n0;
   const float* hid = of_a ? p.dh : p.h;
-  const int col = n0 + 8 * (lane & 15), left = ns - col, kk = lane >> 4;
-  const int rank = j0 + (lane & 15);
-  f32x4 acc[QB][8] = {};
+  uint8_t* const own = smem + wave * 2 * kWeightSlab;
+  f32x4 acc[QB][NB] = {};
 
-  const auto sum_segment = [&](int segment) {
-    int64_t first, end;
-    group_rows(p.rows, segment, first, end);
-    for (int64_t r0 = first + 4 * wave; r0 < end; r0 += 4 * kWeightWaves * AHEAD) {
-      i32x4 v[AHEAD];
-      float h[AHEAD][QB];
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        const int64_t r = r0 + u * 4 * kWeightWaves + kk;
-        const bool some = r < end;
-        v[u] = load_chunk(in + r * ns + col, some ? left : 0);
-#pragma unroll
-        for (int b = 0; b < QB; ++b) h[u][b] = some && rank + 16 * b < p.q ? hid[r * p.q + rank + 16 * b] : 0.f;
-      }
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        E x[8];
-        __builtin_memcpy(x, &v[u], 16);
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-#pragma unroll
-          for (int b = 0; b < QB; ++b)
-            acc[b][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(h[u][b], (float)x[c], acc[b][c], 0, 0, 0);
-      }
-    }
+  const auto slab_of = [&](int64_t first, int rows) {
+    if constexpr (kLoose)
+      return Slab(in + first * ns, ns, ns - n0, rows, 0);
+    else
+      return Slab(in + first * ns, (int64_t)ns * 2, ns - n0, rows, 0, lane);
   };
-  if (!p.index) {
-    if (e < p.rows.groups) sum_segment(e);
-  } else {
-    for (int s0 = 0; s0 < p.rows.groups; s0 += 64) {
-      uint64_t mine = __ballot(s0 + lane < p.rows.groups && p.index[min(s0 + lane, p.rows.groups - 1)] == e);
-      while (mine) {
-        sum_segment(s0 + __builtin_ctzll(mine));
-        mine &= mine - 1;
-      }
+  struct Item {
+    Slab x;
+    float v[QB][8];            // hidden of rows 8 g .. and column j0 + 16 b + lane % 16
+  };
+  AdapterSlabs slabs(p, e, wave);
+  // The next slab and its hidden are asked for, hidden first: what comes last are the copies, and only they.  Rows past
+  // the last one meet zeros of x, ranks past the last one are not stored, so that others are read in their place.
+  const auto ask = [&](Item& it, uint8_t* lds) {
+    int64_t first;
+    int rows;
+    if (!slabs.next(first, rows)) return false;
+    const float* from = hid + first * p.q;
+#pragma unroll
+    for (int b = 0; b < QB; ++b)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        it.v[b][i] = from[(int64_t)min(8 * (lane >> 4) + i, rows - 1) * p.q + min(j0 + 16 * b + (lane & 15), p.q - 1)];
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    it.x = slab_of(first, rows);
+    it.x.fetch(0, lds);
+    return true;
+  };
+  // Multiplies a slab and asks for the one after the next in its place.  `other`: the next is on its way.
+  const auto use = [&](Item& it, uint8_t* lds, bool other) {
+    if constexpr (kLoose) {
+      it.x.commit(lds);
+      wait_reads();
+    } else {
+      __atomic_signal_fence(__ATOMIC_SEQ_CST);
+      if (other)
+        wait_vm<kCopies>();
+      else
+        wait_vm<0>();
+      __atomic_signal_fence(__ATOMIC_SEQ_CST);
     }
+    i32x4 f[NB];
+#pragma unroll
+    for (int c = 0; c < NB; ++c) f[c] = Slab::frag(lds, c * 16, 0, lane);
+    bf16x8 h[QB][HP];
+#pragma unroll
+    for (int b = 0; b < QB; ++b) exact_parts(it.v[b], h[b]);
+    wait_reads();
+    const bool more = ask(it, lds);
+#pragma unroll
+    for (int c = 0; c < NB; ++c) {
+      bf16x8 xp[XP];
+      if constexpr (XP == 1) {
+        xp[0] = __builtin_bit_cast(bf16x8, f[c]);
+      } else {
+        const f16x8 x = __builtin_bit_cast(f16x8, f[c]);
+        float w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = (float)x[i];
+        exact_parts(w, xp);
+      }
+#pragma unroll
+      for (int b = 0; b < QB; ++b)
+#pragma unroll
+        for (int k = HP - 1; k >= 0; --k)
+#pragma unroll
+          for (int y = XP - 1; y >= 0; --y)
+            if (k + y < HP) acc[b][c] = Bf16::mfma(h[b][k], xp[y], acc[b][c]);
+    }
+    return more;
+  };
+  Item even{slab_of(0, 0)}, odd{slab_of(0, 0)};
+  bool has_even = ask(even, own), has_odd = ask(odd, own + kWeightSlab);
+  while (has_even) {
+    has_even = use(even, own, has_odd);
+    if (!has_odd) break;
+    has_odd = use(odd, own + kWeightSlab, has_even);
   }
 
   // the wavefronts' sums, added in their order; a lane has rows 4 (lane / 16) + i of the rank, and of block c column
-  // 8 (lane % 16) + c
+  // 16 c + lane % 16
   const float scale = of_a ? 1.f : scale_of(p, e);
   Out* out = static_cast<Out*>(of_a ? p.da : p.db) + (int64_t)e * p.q * ns;
+  f32x4* const sums = reinterpret_cast<f32x4*>(smem);
 #pragma unroll
   for (int b = 0; b < QB; ++b) {
-    if (b) __syncthreads();
-#pragma unroll
-    for (int c = 0; c < 8; ++c) s_sum[wave][c][lane] = acc[b][c];
     __syncthreads();
-    for (int f = threadIdx.x; f < 8 * 64; f += 64 * kWeightWaves) {
+#pragma unroll
+    for (int c = 0; c < NB; ++c) sums[(wave * NB + c) * 64 + lane] = acc[b][c];
+    __syncthreads();
+    for (int f = threadIdx.x; f < NB * 64; f += blockDim.x) {
       const int c = f / 64, l = f % 64;
       f32x4 v = {};
-#pragma unroll
-      for (int w = 0; w < kWeightWaves; ++w) v += s_sum[w][c][l];
-      const int n = n0 + 8 * (l & 15) + c, j = j0 + 16 * b + 4 * (l >> 4);
+      for (int w = 0; w < (int)(blockDim.x >> 6); ++w) v += sums[w * NB * 64 + f];
+      const int n = n0 + 16 * c + (l & 15), j = j0 + 16 * b + 4 * (l >> 4);
       if (n >= ns) continue;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -598,15 +708,21 @@ hipError_t launch_both(AdapterArgs p, hipStream_t s) {
 template <class T, class Out>
 hipError_t launch_weights(const AdapterArgs& p, hipStream_t s) {
   const int64_t ta = tiles_of(p.I, kWeightCols), tb = tiles_of(p.O, kWeightCols);
-  const auto launch = [&](auto qb) {
+  const bool tight = p.I % 8 == 0 && p.O % 8 == 0 && aligned16(p.x) && aligned16(p.dy);
+  const int waves = plan_adapter_weights(p.rows.rows, p.rows.groups, p.adapters);
+  const auto launch = [&](auto qb, auto loose) {
     constexpr int QB = decltype(qb)::value;
     const int64_t parts = tiles_of(p.q, 16 * QB);
-    return launch_lds<k_adapter_weights<T, QB, Out>>(p.adapters * (ta + tb) * parts, 64 * kWeightWaves, 0, s, p, (int)ta,
-                                                     (int)tb, (int)parts);
+    return launch_lds<k_adapter_weights<T, QB, Out, decltype(loose)::value>>(
+        p.adapters * (ta + tb) * parts, 64 * waves, (size_t)waves * 2 * kWeightSlab, s, p, (int)ta, (int)tb, (int)parts);
   };
-  if (p.q <= 16) return launch(std::integral_constant<int, 1>{});
-  if (p.q <= 32) return launch(std::integral_constant<int, 2>{});
-  return launch(std::integral_constant<int, 4>{});
+  using One = std::integral_constant<int, 1>;
+  using Two = std::integral_constant<int, 2>;
+  // as much of the rank together as leaves two workgroups for each of 256 CUs; slabs that pass through registers leave
+  // room for one block of it
+  const auto enough = [&](int qb) { return p.q > 8 * qb && p.adapters * (ta + tb) * tiles_of(p.q, 16 * qb) >= 512; };
+  if (!tight) return launch(One{}, std::true_type{});
+  return enough(2) ? launch(Two{}, std::false_type{}) : launch(One{}, std::false_type{});
 }
 
 }  // namespace

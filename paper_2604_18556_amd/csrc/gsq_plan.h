@@ -164,6 +164,13 @@ inline UpPlan plan_adapter_up(int64_t rows, int64_t segments, int cols) {
   return {steps, most_panels(rows, segments, 64) * tiles_of(all, steps)};
 }
 
+// Wavefronts that share the sums of dA and dB: half as many again as an adapter has pairs of slabs of 32
+// rows on average.
+inline int plan_adapter_weights(int64_t rows, int64_t segments, int64_t adapters) {
+  const int64_t slabs = most_panels(rows, segments, 64) * 3 / 2;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(kSplitWaves, (slabs + adapters - 1) / adapters));
+}
+
 // How a sum over rows is cut: tiles of `size` x `size`.  Where nothing fits a launch, one that does not.
 struct SumsPlan {
   bool split;
