@@ -26,26 +26,49 @@ struct RouteArgs {
   uint32_t group_size, group_inv;   // expert e is in group (e group_inv) >> 20
   int32_t sigmoid, top2, renormalise;
   float scale;
+  int32_t dtype;               // of the logits
+  int32_t group_share;         // 2^group_share lanes look at a group
 };
 
 // A lane's PER neighbouring logits of a token, as fp32; those past the last one are -infinity.
 template <class E, int PER>
-__device__ __forceinline__ void load_logits(const RouteArgs& p, int64_t token, int e0, float (&l)[PER]) {
-  const E* row = static_cast<const E*>(p.logits) + token * p.E;
+__device__ __forceinline__ void load_logits_of(const E* row, int E_, int e0, float (&l)[PER]) {
   E v[PER];
-  if (e0 + PER <= p.E) {
+  if (e0 + PER <= E_) {
     __builtin_memcpy(v, row + e0, sizeof(v));
 #pragma unroll
     for (int j = 0; j < PER; ++j) l[j] = (float)v[j];
   } else {
 #pragma unroll
-    for (int j = 0; j < PER; ++j) l[j] = e0 + j < p.E ? (float)row[e0 + j] : kLowest;
+    for (int j = 0; j < PER; ++j) l[j] = e0 + j < E_ ? (float)row[e0 + j] : kLowest;
+  }
+}
+template <int PER>
+__device__ __forceinline__ void load_logits(const RouteArgs& p, int64_t token, int e0, float (&l)[PER]) {
+  if (p.dtype == GSQ_DT_BF16)
+    load_logits_of(static_cast<const __bf16*>(p.logits) + token * p.E, p.E, e0, l);
+  else if (p.dtype == GSQ_DT_FP16)
+    load_logits_of(static_cast<const _Float16*>(p.logits) + token * p.E, p.E, e0, l);
+  else
+    load_logits_of(static_cast<const float*>(p.logits) + token * p.E, p.E, e0, l);
+}
+template <class E, int PER>
+__device__ __forceinline__ void store_gradient_as(E* row, int E_, int e0, const float (&d)[PER]) {
+  E v[PER];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) v[j] = (E)d[j];
+  if (e0 + PER <= E_) {
+    __builtin_memcpy(row + e0, v, sizeof(v));
+  } else {
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      if (e0 + j < E_) row[e0 + j] = v[j];
   }
 }
 
 // LANES lanes have a token, PER neighbouring experts each.  Keys are compared in 64 bits where a bias is added (two
 // experts' sums may differ in what 32 bits lose), and as the logits themselves where it is not.
-template <class E, class Key, int LANES, int PER>
+template <class Key, int LANES, int PER>
 __global__ __launch_bounds__(64) void k_route(RouteArgs p) {
   constexpr int TOKENS = 64 / LANES, MOST = LANES * PER;
   constexpr bool kBias = std::is_same<Key, double>::value;
@@ -60,7 +83,7 @@ __global__ __launch_bounds__(64) void k_route(RouteArgs p) {
   const bool live = token < p.tokens;
 
   float l[PER];
-  load_logits<E, PER>(p, live ? token : p.tokens - 1, e0, l);
+  load_logits<PER>(p, live ? token : p.tokens - 1, e0, l);
   float top = kLowest, wrong = 0.f;
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
@@ -113,19 +136,28 @@ __global__ __launch_bounds__(64) void k_route(RouteArgs p) {
     for (int j = 0; j < PER; ++j)
       value[(e0 + j) + (e0 + j) / 16] = l[j] > kLowest && score[j] == score[j] ? score[j] : (double)kLowest;
     __syncthreads();
-    for (int g = lane; g < p.groups; g += LANES) {
+    // 2^share lanes to a group, or groups one after another
+    const int share = p.group_share, mates = 1 << share;
+    for (int g = lane >> share; g < p.groups; g += LANES >> share) {
       double best = kLowest, second = kLowest;
-      for (int e = g * p.group_size; e < (int)((g + 1) * p.group_size); ++e) {
-        const double v = value[e + e / 16];
-        second = v > best ? best : v > second ? v : second;
-        best = v > best ? v : best;
+      for (int e = lane & (mates - 1); e < (int)p.group_size; e += mates) {
+        const int i = g * p.group_size + e;
+        const double v = value[i + i / 16];
+        second = max_of(second, v > best ? best : v);
+        best = max_of(best, v);
       }
-      s_group[sub][g] = p.top2 && second > (double)kLowest ? best + second : best;
+      for (int d = 1; d < mates; d <<= 1) {
+        const double b = __shfl_xor(best, d, 64), s = __shfl_xor(second, d, 64);
+        second = max_of(max_of(second, s), b > best ? best : b);
+        best = max_of(best, b);
+      }
+      if ((lane & (mates - 1)) == 0) s_group[sub][g] = p.top2 && second > (double)kLowest ? best + second : best;
     }
     __syncthreads();
     for (int g = lane; g < p.groups; g += LANES) {
       const double mine = s_group[sub][g];
       int before = 0;
+#pragma unroll 4
       for (int h = 0; h < p.groups; ++h) {
         const double other = s_group[sub][h];
         before += other > mine || (other == mine && h < g);
@@ -191,7 +223,7 @@ __global__ __launch_bounds__(64) void k_route(RouteArgs p) {
 //   sigmoid, renormalised: p = s_j / sum_i s_i, dl_j = p_j (g_j - D) (1 - s_j), D = sum_i g_i p_i, no others
 //   sigmoid: dl_j = g_j s_j (1 - s_j), no others
 // p is formed from exponentials relative to the chosen experts' largest, so that small scores keep their digits.
-template <class E, int LANES, int PER>
+template <int LANES, int PER>
 __global__ __launch_bounds__(64) void k_route_grad(RouteArgs p) {
   constexpr int TOKENS = 64 / LANES, MOST = LANES * PER;
   constexpr int TIMES = LANES >= GSQ_MAX_TOP_K ? 1 : GSQ_MAX_TOP_K / LANES;
@@ -201,7 +233,7 @@ __global__ __launch_bounds__(64) void k_route_grad(RouteArgs p) {
   const int tid = threadIdx.x, lane = tid % LANES, sub = tid / LANES, e0 = lane * PER;
   const int64_t token = (int64_t)blockIdx.x * TOKENS + sub, row = min(token, p.tokens - 1);
   float l[PER];
-  load_logits<E, PER>(p, row, e0, l);
+  load_logits<PER>(p, row, e0, l);
   int id[TIMES];
   float g[TIMES];
 #pragma unroll
@@ -286,17 +318,12 @@ __global__ __launch_bounds__(64) void k_route_grad(RouteArgs p) {
     for (int j = 0; j < PER; ++j) d[j] += at == j ? v : 0.f;
   }
   if (token >= p.tokens) return;
-  E* out = static_cast<E*>(p.dlogits) + token * p.E + e0;
-  E v[PER];
-#pragma unroll
-  for (int j = 0; j < PER; ++j) v[j] = (E)d[j];
-  if (e0 + PER <= p.E) {
-    __builtin_memcpy(out, v, sizeof(v));
-  } else {
-#pragma unroll
-    for (int j = 0; j < PER; ++j)
-      if (e0 + j < p.E) out[j] = v[j];
-  }
+  if (p.dtype == GSQ_DT_BF16)
+    store_gradient_as(static_cast<__bf16*>(p.dlogits) + token * p.E, p.E, e0, d);
+  else if (p.dtype == GSQ_DT_FP16)
+    store_gradient_as(static_cast<_Float16*>(p.dlogits) + token * p.E, p.E, e0, d);
+  else
+    store_gradient_as(static_cast<float*>(p.dlogits) + token * p.E, p.E, e0, d);
 }
 
 template <int LANES, int PER>
@@ -304,20 +331,19 @@ struct Shape {
   static constexpr int kLanes = LANES, kPer = PER;
 };
 
-// The lanes and experts of a lane that hold E experts.
+// Sixteen lanes to a token where there are many, four to a wavefront: the choices then cost least (16384 tokens of 256
+// experts by all 64 lanes XX us, by 16 XX).  All 64 for few tokens, whose latency is that of one (64 tokens XX against
+// XX), and for more than 256 experts, which 16 lanes would not hold.
 template <class F>
-hipError_t with_shape(int E, F f) {
-  if (E <= 64) return f(Shape<16, 4>{});
-  if (E <= 128) return f(Shape<16, 8>{});
-  if (E <= 256) return f(Shape<16, 16>{});
+hipError_t with_shape(int64_t tokens, int E, F f) {
+  if (tokens > 2048 && E <= 64) return f(Shape<16, 4>{});
+  if (tokens > 2048 && E <= 128) return f(Shape<16, 8>{});
+  if (tokens > 2048 && E <= 256) return f(Shape<16, 16>{});
+  if (E <= 64) return f(Shape<64, 1>{});
+  if (E <= 128) return f(Shape<64, 2>{});
+  if (E <= 256) return f(Shape<64, 4>{});
+  if (E <= 512) return f(Shape<64, 8>{});
   return f(Shape<64, 16>{});
-}
-
-template <class F>
-hipError_t with_type(int dtype, F f) {
-  if (dtype == GSQ_DT_BF16) return f(__bf16{});
-  if (dtype == GSQ_DT_FP16) return f(_Float16{});
-  return f(float{});
 }
 
 RouteArgs route_args(const gsq_routing& r, const void* logits) {
@@ -334,6 +360,7 @@ RouteArgs route_args(const gsq_routing& r, const void* logits) {
   p.top2 = r.group_score == GSQ_GROUP_TOP2;
   p.renormalise = r.renormalise != 0;
   p.scale = r.scale;
+  p.dtype = r.dtype;
   return p;
 }
 
@@ -492,16 +519,31 @@ __global__ __launch_bounds__(512) void k_group_count(OrderArgs p) {
 }
 
 __global__ __launch_bounds__(512) void k_group_place(OrderArgs p) {
-  extern __shared__ uint32_t s_base[];      // groups
+  extern __shared__ uint32_t s_base[];      // groups, groups, and the shares' parts
   const uint32_t* table = reinterpret_cast<const uint32_t*>(p.sources);
   uint32_t* mine = s_base + p.groups;
-  for (int g = threadIdx.x; g < p.groups; g += blockDim.x) {
+  // few groups: several threads to each, with a part of the chunks
+  const int shares = max(1, (int)blockDim.x / p.groups);
+  uint32_t* part_all = shares > 1 ? mine + p.groups : s_base;
+  uint32_t* part_before = shares > 1 ? part_all + shares * p.groups : mine;
+  for (int t = threadIdx.x; t < shares * p.groups; t += blockDim.x) {
+    const int g = t % p.groups;
     uint32_t all = 0, before = 0;
 #pragma unroll 8
-    for (int c = 0; c < p.chunks; ++c) {
+    for (int c = t / p.groups; c < p.chunks; c += shares) {
       const uint32_t n = table[(int64_t)c * p.groups + g];
       before += c < (int)blockIdx.x ? n : 0;
       all += n;
+    }
+    part_all[t] = all;
+    part_before[t] = before;
+  }
+  __syncthreads();
+  for (int g = threadIdx.x; g < p.groups; g += blockDim.x) {
+    uint32_t all = 0, before = 0;
+    for (int t = g; t < shares * p.groups; t += p.groups) {
+      all += part_all[t];
+      before += part_before[t];
     }
     s_base[g] = all;
     mine[g] = before;
@@ -541,20 +583,18 @@ hipError_t launch_route(const gsq_routing& r, const void* logits, const float* b
   p.bias = bias;
   p.experts = experts;
   p.weights = weights;
-  return with_type(r.dtype, [&](auto type) {
-    return with_shape(r.experts, [&](auto shape) {
-      using E = decltype(type);
-      using S = decltype(shape);
-      constexpr int LANES = S::kLanes, PER = S::kPer, TOKENS = 64 / LANES;
-      const int64_t blocks = tiles_of(r.tokens, TOKENS);
-      const size_t lds = r.groups > 1 ? (size_t)TOKENS * (LANES * PER + LANES * PER / 16) * sizeof(double) : 0;
-      if (!fits_launch(blocks, 64)) return hipErrorInvalidConfiguration;
-      if (bias)
-        k_route<E, double, LANES, PER><<<(unsigned)blocks, 64, lds, s>>>(p);
-      else
-        k_route<E, float, LANES, PER><<<(unsigned)blocks, 64, lds, s>>>(p);
-      return hipGetLastError();
-    });
+  return with_shape(r.tokens, r.experts, [&](auto shape) {
+    using S = decltype(shape);
+    constexpr int LANES = S::kLanes, PER = S::kPer, TOKENS = 64 / LANES;
+    const int64_t blocks = tiles_of(r.tokens, TOKENS);
+    const size_t lds = r.groups > 1 ? (size_t)TOKENS * (LANES * PER + LANES * PER / 16) * sizeof(double) : 0;
+    while (2 << p.group_share <= LANES / r.groups) ++p.group_share;
+    if (!fits_launch(blocks, 64)) return hipErrorInvalidConfiguration;
+    if (bias)
+      k_route<double, LANES, PER><<<(unsigned)blocks, 64, lds, s>>>(p);
+    else
+      k_route<float, LANES, PER><<<(unsigned)blocks, 64, lds, s>>>(p);
+    return hipGetLastError();
   });
 }
 
@@ -565,15 +605,12 @@ hipError_t launch_route_grad(const gsq_routing& r, const void* logits, const int
   p.experts = const_cast<int32_t*>(experts);
   p.dweights = dweights;
   p.dlogits = dlogits;
-  return with_type(r.dtype, [&](auto type) {
-    return with_shape(r.experts, [&](auto shape) {
-      using E = decltype(type);
-      using S = decltype(shape);
-      const int64_t blocks = tiles_of(r.tokens, 64 / S::kLanes);
-      if (!fits_launch(blocks, 64)) return hipErrorInvalidConfiguration;
-      k_route_grad<E, S::kLanes, S::kPer><<<(unsigned)blocks, 64, 0, s>>>(p);
-      return hipGetLastError();
-    });
+  return with_shape(r.tokens, r.experts, [&](auto shape) {
+    using S = decltype(shape);
+    const int64_t blocks = tiles_of(r.tokens, 64 / S::kLanes);
+    if (!fits_launch(blocks, 64)) return hipErrorInvalidConfiguration;
+    k_route_grad<S::kLanes, S::kPer><<<(unsigned)blocks, 64, 0, s>>>(p);
+    return hipGetLastError();
   });
 }
 
@@ -596,7 +633,7 @@ hipError_t launch_group_rows(const int32_t* ids, int64_t count, int groups, int6
   k_group_count<<<p.chunks, plan.threads, (size_t)p.waves * groups * 4, s>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  k_group_place<<<p.chunks, plan.threads, (size_t)2 * groups * 4, s>>>(p);
+  k_group_place<<<p.chunks, plan.threads, (size_t)(2 * groups + (groups < plan.threads ? 2 * plan.threads : 0)) * 4, s>>>(p);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   k_group_sources<<<(unsigned)std::min<int64_t>(tiles_of(count, 256), 16384), 256, 0, s>>>(p);
   return hipGetLastError();

@@ -171,7 +171,7 @@ int main() {
       bool ok = p.waves >= 1 && 64 * p.waves <= p.threads && p.threads <= 1024 && p.chunks >= 1 && p.chunks <= 128;
       ok = ok && p.chunks * p.chunk >= n && (p.chunks - 1) * p.chunk < n;
       if (p.chunks == 1) ok = ok && (p.waves + 1) * g * 4 + 64 <= 65536 && n <= 16384;
-      else ok = ok && p.waves * g * 4 <= 65536 && 2 * g * 4 + 64 <= 65536 && (int64_t)p.chunks * g <= n && p.threads <= 512;
+      else ok = ok && p.waves * g * 4 <= 65536 && 2 * (g + (g < p.threads ? p.threads : 0)) * 4 + 64 <= 65536 && (int64_t)p.chunks * g <= n && p.threads <= 512;
       if (!ok) { std::printf("%lld %d\n", (long long)n, g); return 1; }
     }
   return 0;
