@@ -146,6 +146,39 @@ def test_adapters_of_whole_numbers_are_exact(dev, counts, index, n, o, i, q, dty
     assert torch.equal(da.cpu(), ref.da.to(dtype)) and torch.equal(db.cpu(), ref.db.to(dtype))
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("counts,index,n,o,i,q", [([1500, 30], [1, 0], 2, 12296, 1040, 24), ([900, 0, 800], None, 3, 1032, 11264, 48),
+                                                  ([2000], None, 1, 9216, 9216, 200), ([3, 1700, 2], [0, -1, 1], 2, 10240, 2056, 64),
+                                                  ([5, 3] * 150, [k * 7 % 201 - 1 for k in range(300)], 200, 136, 264, 16)])
+def test_large_adapters_of_whole_numbers_are_exact(dev, counts, index, n, o, i, q, dtype):
+    """As above, against 64-bit products on the GPU: sizes that no cache holds, and more segments and adapters than a
+    wavefront has lanes.  Values up to 1 (few of them not 0), so that hidden and the sums stay exact."""
+    print(f"large {counts[:4]} {n} {o}x{i} {q} {dtype}", flush=True)
+    gen = torch.Generator(device=dev).manual_seed(o + i + q)
+    rows, off = sum(counts), offsets_of(counts)
+
+    def numbers(*shape):
+        return (torch.randint(-1, 2, shape, generator=gen, device=dev) * torch.randint(0, 2, shape, generator=gen, device=dev)).double()
+
+    x, dy, a, b = numbers(rows, i), numbers(rows, o), numbers(n, q, i), numbers(n, o, q)
+    base, dbase = numbers(rows, o) * 9, numbers(rows, i) * 9
+    c = Case(dev, dtype, x, dy, a, b, off, index, None, base, dbase)
+    c.rows()
+    c.weights()
+    da, db = torch.zeros_like(a), torch.zeros_like(b)
+    for r, e in segments(off, index, n):
+        y, dx = base[r], dbase[r]
+        h, dh = torch.zeros(2, r.stop - r.start, q, dtype=torch.float64, device=dev)
+        if e >= 0:
+            h, dh = x[r] @ a[e].t(), dy[r] @ b[e]
+            y, dx = y + h @ b[e].t(), dx + dh @ a[e]
+            da[e] += dh.t() @ x[r]
+            db[e] += dy[r].t() @ h
+        assert torch.equal(c.h[r], h.float()) and torch.equal(c.dh[r], dh.float())
+        assert torch.equal(c.y[r], y.to(dtype)) and torch.equal(c.dx[r], dx.to(dtype))
+    assert torch.equal(c.da, da.float()) and torch.equal(c.db, db.float())
+
+
 @pytest.mark.parametrize("shift", [1, 3, 4])
 @pytest.mark.parametrize("q", [5, 16, 72])
 def test_addresses_of_any_element_alignment(dev, shift, q):
