@@ -99,7 +99,7 @@ __device__ __forceinline__ Place place_of(const ExchangeArgs& p, int64_t block) 
   Place at;
   if constexpr (kWave) {
     const int64_t task = block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    at.token = task / p.parts;
+    at.token = task >> 32 ? task / p.parts : (uint32_t)task / (uint32_t)p.parts;
     // every lane stays: those past the row's end do its last piece once more
     at.piece = min((int)(task - at.token * p.parts) * 64 + (int)(threadIdx.x & 63), p.pieces - 1);
   } else {

@@ -224,7 +224,7 @@ struct OrderPlan {
 };
 inline OrderPlan plan_order(int64_t count, int groups) {
   constexpr int kWords = 15360;
-  const int64_t chunk = std::max({(int64_t)2048, (int64_t)4 * groups, tiles_of(tiles_of(count, 128), 64) * 64});
+  const int64_t chunk = std::max({(int64_t)1024, (int64_t)4 * groups, tiles_of(tiles_of(count, 128), 64) * 64});
   if (count <= std::max((int64_t)8192, chunk)) {
     const int waves = (int)std::min<int64_t>({16, kWords / groups - 1, tiles_of(count, 64)});
     return {std::max(64 * waves, groups > 256 ? 1024 : 256), waves, 1, count};

@@ -115,7 +115,7 @@ __global__ __launch_bounds__(64) void k_route(RouteArgs p) {
   } else if (!p.sigmoid && !p.renormalise) {
     float sum = 0.f;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) sum += __expf(l[j] - top);
+    for (int j = 0; j < PER; ++j) sum += expf(l[j] - top);
     total = sum_lanes<LANES>(sum);
   }
 
@@ -331,19 +331,20 @@ struct Shape {
   static constexpr int kLanes = LANES, kPer = PER;
 };
 
-// Sixteen lanes to a token where there are many, four to a wavefront: the choices then cost least (16384 tokens of 256
-// experts by all 64 lanes XX us, by 16 XX).  All 64 for few tokens, whose latency is that of one (64 tokens XX against
-// XX), and for more than 256 experts, which 16 lanes would not hold.
+// Sixteen lanes to a token where there are many, four tokens to a wavefront: the choices then cost least (16384 tokens of
+// 256 experts with their order 23.5 us, 27.4 by all 64 lanes).  All 64 for few tokens, whose latency is that of one (64
+// tokens of 256 grouped experts with a bias 7.5 us, 17.7 by 16), where more than 128 experts have groups and 64-bit keys
+// to look at (16384 of 256 42.6, 49.8 by 16), and beyond 256 experts, which 16 lanes would not hold.
 template <class F>
-hipError_t with_shape(int64_t tokens, int E, F f) {
-  if (tokens > 2048 && E <= 64) return f(Shape<16, 4>{});
-  if (tokens > 2048 && E <= 128) return f(Shape<16, 8>{});
-  if (tokens > 2048 && E <= 256) return f(Shape<16, 16>{});
+hipError_t with_shape(int64_t tokens, int E, int groups, F f) {
+  if (tokens > 2048 && E <= (groups > 1 ? 128 : 256)) {
+    if (E <= 64) return f(Shape<16, 4>{});
+    return E <= 128 ? f(Shape<16, 8>{}) : f(Shape<16, 16>{});
+  }
   if (E <= 64) return f(Shape<64, 1>{});
   if (E <= 128) return f(Shape<64, 2>{});
   if (E <= 256) return f(Shape<64, 4>{});
-  if (E <= 512) return f(Shape<64, 8>{});
-  return f(Shape<64, 16>{});
+  return E <= 512 ? f(Shape<64, 8>{}) : f(Shape<64, 16>{});
 }
 
 RouteArgs route_args(const gsq_routing& r, const void* logits) {
@@ -376,34 +377,59 @@ __device__ __forceinline__ uint64_t same_ids(int id, bool some, int bits) {
   return same;
 }
 
-// A workgroup's part of the ids: each wavefront counts a contiguous part of them, 64 at a time, in a histogram of its
-// own, and each id's number among the equal ones before it goes to `slots`.
+// A wavefront's part of the ids, 64 at a time, counted in a histogram of its own; each id's number among the equal ones
+// before it goes to `slots`, or stays in registers with the id where the part is short.
+constexpr int kIdsAhead = 4;                // batches whose ids are asked for together
+struct HeldIds {
+  int id[kIdsAhead], number[kIdsAhead];     // id: -1 of no group
+};
+__device__ __forceinline__ bool ids_fit(int64_t first, int64_t last) { return last - first <= 64 * kIdsAhead; }
+
 __device__ __forceinline__ void count_ids(const int32_t* ids, int64_t first, int64_t last, int groups, int bits,
-                                          uint32_t* hist, int32_t* slots) {
-  constexpr int AHEAD = 4;                  // batches whose ids are asked for together
+                                          uint32_t* hist, int32_t* slots, HeldIds& held) {
   const int lane = threadIdx.x & 63;
   const uint64_t below = ((uint64_t)1 << lane) - 1;
-  for (int64_t at = first; at < last; at += 64 * AHEAD) {
-    int id[AHEAD];
+  const bool keep = ids_fit(first, last);
+  for (int64_t at = first; at < last; at += 64 * kIdsAhead) {
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
+    for (int u = 0; u < kIdsAhead; ++u) {
       const int64_t i = at + u * 64 + lane;
-      id[u] = i < last ? ids[i] : -1;
+      held.id[u] = i < last ? ids[i] : -1;
     }
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
+    for (int u = 0; u < kIdsAhead; ++u) {
       const int64_t i = at + u * 64 + lane;
       if (at + u * 64 >= last) break;
-      const bool some = id[u] >= 0 && id[u] < groups;
-      const uint64_t same = same_ids(id[u], some, bits);
+      const bool some = held.id[u] >= 0 && held.id[u] < groups;
+      if (!some) held.id[u] = -1;
+      const uint64_t same = same_ids(held.id[u], some, bits);
       if (some) {
-        const uint32_t before = hist[id[u]];
+        const uint32_t before = hist[held.id[u]];
         __builtin_amdgcn_wave_barrier();
-        if ((same & below) == 0) hist[id[u]] = before + __popcll(same);
-        slots[i] = (int32_t)(before + __popcll(same & below));
+        if ((same & below) == 0) hist[held.id[u]] = before + __popcll(same);
+        held.number[u] = (int)(before + __popcll(same & below));
+        if (!keep) slots[i] = held.number[u];
       }
       __builtin_amdgcn_wave_barrier();
     }
+  }
+}
+
+// f(index, id, number) for the ids that count_ids has counted, id -1 for those of no group.
+template <class F>
+__device__ __forceinline__ void each_id(const int32_t* ids, int64_t first, int64_t last, int groups, const int32_t* slots,
+                                        const HeldIds& held, F f) {
+  const int lane = threadIdx.x & 63;
+  if (ids_fit(first, last)) {
+#pragma unroll
+    for (int u = 0; u < kIdsAhead; ++u)
+      if (first + u * 64 + lane < last) f(first + u * 64 + lane, held.id[u], held.number[u]);
+    return;
+  }
+  for (int64_t i = first + lane; i < last; i += 64) {
+    const int id = ids[i];
+    const bool some = id >= 0 && id < groups;
+    f(i, some ? id : -1, some ? slots[i] : 0);
   }
 }
 
@@ -478,22 +504,22 @@ __global__ __launch_bounds__(1024) void k_group_few(OrderArgs p) {
   __syncthreads();
   int64_t first = 0, last = p.count;
   wave_part(p, first, last);
-  count_ids(p.ids, first, last, p.groups, p.bits, s_hist + wave * p.groups, p.slots);
+  HeldIds held;
+  count_ids(p.ids, first, last, p.groups, p.bits, s_hist + wave * p.groups, p.slots, held);
   __syncthreads();
   sum_over_waves(s_hist, p.groups, p.waves, [&](int g, uint32_t n) { base[g] = n; });
   __syncthreads();
   const uint32_t all = sums_before(base, p.groups);
   for (int g = threadIdx.x; g < p.groups; g += blockDim.x) p.offsets[g] = base[g];
   if (threadIdx.x == 0) p.offsets[p.groups] = all;
-  for (int64_t i = first + (threadIdx.x & 63); i < last; i += 64) {
-    const int id = p.ids[i];
+  each_id(p.ids, first, last, p.groups, p.slots, held, [&](int64_t i, int id, int number) {
     int32_t at = -1;
-    if (id >= 0 && id < p.groups) {
-      at = p.slots[i] + (int32_t)(s_hist[wave * p.groups + id] + base[id]);
+    if (id >= 0) {
+      at = number + (int32_t)(s_hist[wave * p.groups + id] + base[id]);
       p.sources[at] = (int32_t)i;
     }
     p.slots[i] = at;
-  }
+  });
   for (int64_t k = all + threadIdx.x; k < p.count; k += blockDim.x) p.sources[k] = -1;
 }
 
@@ -506,16 +532,15 @@ __global__ __launch_bounds__(512) void k_group_count(OrderArgs p) {
   __syncthreads();
   int64_t first = blockIdx.x * p.chunk, last = min(first + p.chunk, p.count);
   wave_part(p, first, last);
-  count_ids(p.ids, first, last, p.groups, p.bits, s_hist + wave * p.groups, p.slots);
+  HeldIds held;
+  count_ids(p.ids, first, last, p.groups, p.bits, s_hist + wave * p.groups, p.slots, held);
   __syncthreads();
   uint32_t* table = reinterpret_cast<uint32_t*>(p.sources) + (int64_t)blockIdx.x * p.groups;
   sum_over_waves(s_hist, p.groups, p.waves, [&](int g, uint32_t n) { table[g] = n; });
   __syncthreads();
-  if (p.waves > 1)
-    for (int64_t i = first + (threadIdx.x & 63); i < last; i += 64) {
-      const int id = p.ids[i];
-      if (id >= 0 && id < p.groups) p.slots[i] += (int32_t)s_hist[wave * p.groups + id];
-    }
+  each_id(p.ids, first, last, p.groups, p.slots, held, [&](int64_t i, int id, int number) {
+    if (id >= 0) p.slots[i] = number + (int32_t)s_hist[wave * p.groups + id];
+  });
 }
 
 __global__ __launch_bounds__(512) void k_group_place(OrderArgs p) {
@@ -583,7 +608,7 @@ hipError_t launch_route(const gsq_routing& r, const void* logits, const float* b
   p.bias = bias;
   p.experts = experts;
   p.weights = weights;
-  return with_shape(r.tokens, r.experts, [&](auto shape) {
+  return with_shape(r.tokens, r.experts, r.groups, [&](auto shape) {
     using S = decltype(shape);
     constexpr int LANES = S::kLanes, PER = S::kPer, TOKENS = 64 / LANES;
     const int64_t blocks = tiles_of(r.tokens, TOKENS);
@@ -605,7 +630,7 @@ hipError_t launch_route_grad(const gsq_routing& r, const void* logits, const int
   p.experts = const_cast<int32_t*>(experts);
   p.dweights = dweights;
   p.dlogits = dlogits;
-  return with_shape(r.tokens, r.experts, [&](auto shape) {
+  return with_shape(r.tokens, r.experts, 1, [&](auto shape) {
     using S = decltype(shape);
     const int64_t blocks = tiles_of(r.tokens, 64 / S::kLanes);
     if (!fits_launch(blocks, 64)) return hipErrorInvalidConfiguration;
