@@ -1,5 +1,9 @@
 // Low-rank adapters of many requests: y = base + s B (A x) and its gradients, the adapter being that of the row's
 // segment.
+//
+// A product through a low rank is two products whose inner results are small: hidden goes to memory in fp32 (the gradients
+// need it again), and both kernels of a call are bound by reading x and by reading and writing y, not by the matrix cores
+// (busy 0.03 and 0.10 of the time at 4096 rows, 4096 -> 64 -> 14336: 20 us for A x, 58 us for y).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -42,7 +46,10 @@ struct HiddenColumns {
   }
 };
 
-// A tile of TM rows x TN of the rank, by wavefronts that share the sum.
+// A tile of TM rows x TN of the rank, by wavefronts that share the sum.  4096 rows of 4096 at rank 64 take 20 us (12 with
+// warm caches): 16 rows to a workgroup read the whole of A each, 0.17 GB through the L2s for 0.03 of x, and wait 0.6 of
+// the time.  Non-temporal copies of x, slabs in another order for each workgroup, and neighbouring slabs to a wavefront
+// changed nothing.
 template <class T, int kForm, int TM, int TN, bool kLoose>
 __device__ __forceinline__ void down_tile(const AdapterArgs& p, int e, int64_t first, int ms, int n0, uint8_t* smem) {
   using E = typename T::elem;
@@ -106,7 +113,7 @@ __global__ __launch_bounds__((64 * kDownWaves<TM, TN>)) void k_adapter_down(Adap
 //
 // 64 columns of the adapter's matrix are the instructions' rows, in four blocks: row 4 g + c of block j is column
 // up_column(g, j) + c, so that a lane's results are twice eight neighbouring columns of one row of y, and four lanes
-// store 64 bytes of it together (with 16 neighbouring columns to a lane, 4096 rows of 14336 took 99 us, XX now).
+// store 64 bytes of it together.
 constexpr int kUpCols = 64, kUpWaves = 4, kUpRows = 16 * kUpWaves;
 constexpr int kUpBlock = 32 * kUpCols * 2;     // bytes of 32 of the rank for these columns
 
@@ -137,7 +144,7 @@ __device__ __forceinline__ float hidden_power(const float* row, int q) {
   top = fmaxf(top, __shfl_xor(top, 32, 64));
   // infinities pass as they are (and NaN, which fmaxf leaves out); what is very small, as far as it goes
   if (!(top > 0.f && top < __builtin_huge_valf())) return 1.f;
-  return exp2f((float)(13 - max((int)(__float_as_uint(top) >> 23) - 127, -100)));
+  return ldexpf(1.f, 13 - max((int)(__float_as_uint(top) >> 23) - 127, -100));
 }
 
 template <class T>
@@ -320,7 +327,10 @@ __device__ __forceinline__ void wait_blocks(int after) {
 
 // Panels of 64 rows (16 to a wavefront) and `steps` times 64 columns.  A panel's hidden stays in registers as long as its
 // rank fits KS blocks.  While a step is multiplied, the matrix of the next is on its way to LDS, and the base of the next
-// two to registers.
+// two to registers.  4096 rows of 14336 with a base at rank 64: 58 us, 235 MB of base and y at 4.1 TB/s (a copy of as much
+// takes 45).  With cold caches 60, and 116 with the matrix read by each wavefront for itself, 92 from LDS but 32 bytes of
+// a row stored at a time, 80 with 64, 78 with whole lines that the caches keep.  Twice the columns at a step, a panel's
+// workgroups on neighbouring columns at each step, and each XCD on columns of its own changed nothing or cost a tenth.
 template <class T, int kForm, int KS, bool kCopied, int kBy>
 __global__ __launch_bounds__(64 * kUpWaves) void k_adapter_up(AdapterArgs p, int steps, int chunks) {
   using E = typename T::elem;
@@ -464,8 +474,9 @@ __global__ __launch_bounds__(64 * kUpWaves) void k_adapter_up_few(AdapterArgs p)
 // LDS in slabs of 32 rows, two of them for each wavefront so that one is on its way while the other is used, and is read
 // by transposing reads; a lane reads its eight hidden values of a column itself.
 // fp32 instructions would need no transposing, but take five times as long as the bf16 ones of the exact parts that
-// hidden is split into, three of 8 bits (fp16 x: two parts, and the product of the two smallest is left out, 2^-25 of
-// the whole): with them 4096 rows of 4096 + 14336 at rank 32 took 92 us.
+// hidden is split into, three of 8 bits (fp16 x: two parts, of whose products those below 2^-24 of the whole are left out).
+// 4096 rows of 4096 + 14336 columns in four adapters of rank 32: 45 us, 0.15 GB at 3.4 TB/s (92 by fp32 instructions, with
+// 64-row slabs one at a time 50); the largest adapter has half of the rows, and the rounds of workgroups end unevenly.
 constexpr int kWeightCols = 128, kWeightBlocks = kWeightCols / 16;
 constexpr int kWeightRows = 32, kWeightSlab = kWeightRows * kWeightCols * 2;
 

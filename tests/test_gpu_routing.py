@@ -132,7 +132,11 @@ ROUTINGS = [(1, R(1, 1)), (1, R(8, 2)), (5, R(7, 7, score=SIG)), (64, R(64, 8, r
             (9, R(64, 6, 4, 2)), (70, R(256, 8, 8, 4, SIG, TOP2, True, 2.5)), (33, R(160, 6, 8, 3, SOFT, MAX, False, 16.0)),
             (17, R(100, 10, 10, 4, SIG, MAX)), (6, R(162, 6, 9, 4)), (4, R(384, 8)), (5, R(1024, 32, 64, 16, SIG)),
             (3, R(1000, 20, 40, 1, SOFT, TOP2)), (2, R(36, 32, 3, 3, SIG, TOP2, False)), (1001, R(128, 4, 4, 4)),
-            (13, R(12, 5, 12, 6, SOFT, TOP2)), (8, R(255, 9, renormalise=False, scale=-0.5)), (3, R(16, 16, 16, 16, SIG))]
+            (13, R(12, 5, 12, 6, SOFT, TOP2)), (8, R(255, 9, renormalise=False, scale=-0.5)), (3, R(16, 16, 16, 16, SIG)),
+            # many tokens, four to a wavefront; more choices than a token has lanes
+            (2500, R(64, 20)), (2049, R(100, 6, 10, 4, SIG)), (3001, R(128, 8, 16, 5)), (2100, R(250, 17, renormalise=False)),
+            (2053, R(7, 3, score=SIG)), (2200, R(30, 6, 3, 2, SOFT, MAX)), (2070, R(256, 8, 8, 4, SIG, TOP2, True, 2.5)),
+            (2060, R(300, 32))]
 
 
 @pytest.mark.parametrize("dtype", [FP32, BF16, FP16], ids=["fp32", "bf16", "fp16"])
@@ -150,12 +154,13 @@ def test_route(dev, t, r, biased, dtype):
     assert ((w.double() - wr).abs() <= weight_bound(r, logits, wr, bias)).all()
 
 
+@pytest.mark.parametrize("times", [1, 130])
 @pytest.mark.parametrize("biased", [False, True], ids=["plain", "bias"])
 @pytest.mark.parametrize("score", [SOFT, SIG], ids=["softmax", "sigmoid"])
 @pytest.mark.parametrize("groups,top_groups,renorm", [(1, 1, True), (1, 1, False), (6, 2, True), (6, 6, False)])
-def test_route_rows_that_masks_leave_little_of(dev, groups, top_groups, renorm, score, biased):
+def test_route_rows_that_masks_leave_little_of(dev, groups, top_groups, renorm, score, biased, times):
     """Rows without an expert, with fewer than top_k, with equal logits, huge and tiny ones, and rows that are not
-    finite beside fine ones."""
+    finite beside fine ones; few and many of them (a token by all lanes of a wavefront, and by a quarter)."""
     e, k = 48, 6
     r = R(e, k, groups, top_groups, score, TOP2, renorm, 1.5)
     gen = rng_of(groups, renorm, score)
@@ -180,6 +185,7 @@ def test_route_rows_that_masks_leave_little_of(dev, groups, top_groups, renorm, 
     if biased:
         bias = torch.randn(e, generator=gen) * 0.2
         bias[11], bias[12], bias[33] = -INF, float("nan"), 5.0
+    logits = logits.repeat(times, 1)
     ids, w = route(r, logits, bias, dev)
     idr, wr = route_ref(r, logits, bias)
     assert torch.equal(ids, idr)
@@ -481,6 +487,26 @@ def test_no_tokens(dev):
     B.dispatch_rows(x, s, torch.empty(0, 16, device=dev))
     B.combine_rows(torch.empty(0, 16, device=dev), s, x)
     assert not x.any()
+
+
+def test_more_tokens_than_a_grid_has_workgroups(dev):
+    """Each workgroup goes through several tokens, one after another."""
+    c, t = 264, (1 << 24) + 5000
+    x = (torch.arange(t, device=dev) % 199).to(BF16)[:, None].expand(t, c).contiguous()
+    slots = torch.arange(t - 1, -1, -1, dtype=torch.int32, device=dev)[:, None].contiguous()
+    out = torch.zeros(t, c, dtype=BF16, device=dev)
+    B.dispatch_rows(x, slots, out)
+    assert torch.equal(out, x.flip(0))
+    y = torch.zeros_like(x)
+    B.combine_rows(out, slots, y)
+    assert torch.equal(y, x)
+    del y
+    t = (1 << 22) + 5000
+    x, out, slots = x[:t], out[-t:], slots[-t:].contiguous()      # slots t - 1 .. 0
+    w, dw, drows = torch.full((t, 1), 0.5, device=dev), torch.zeros(t, 1, device=dev), torch.zeros(t, c, dtype=BF16, device=dev)
+    B.combine_rows_grad(x, out.contiguous(), slots, w, drows, dw)
+    assert torch.equal(drows, (x * 0.5).flip(0))
+    assert torch.equal(dw[:, 0], x[:, 0].float() ** 2 * c)        # whole numbers below 2^24
 
 
 def test_rows_beyond_32_bits(dev):
