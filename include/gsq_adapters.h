@@ -19,7 +19,9 @@
  *
  * Stream, device pointers, status codes and gsq_last_error() are as gsq.h says, addresses, overlapping calls and
  * reproducibility as gsq_products.h does; nothing is allocated, synchronised or kept.  Sums are in fp32, and
- * hidden enters the second product with 16 bits of mantissa at least, so that y and dx are rounded once.
+ * hidden enters the second product with 16 bits of mantissa at least, so that y and dx are rounded once.  What is not
+ * finite stays in its rows of y and dx, and in its adapter's gradients; where the formulas have an infinity there may
+ * be NaN.
  */
 #ifndef GSQ_ADAPTERS_H
 #define GSQ_ADAPTERS_H

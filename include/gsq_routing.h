@@ -83,7 +83,7 @@ gsq_status gsq_dispatch_rows(const gsq_exchange* g, const void* x, const int32_t
 
 /* out[t] = sum_k weights[t, k] rows[slots[t, k]], in fp32 in the order of k, rounded once.  rows: R x C, weights:
  * fp32 T x K or NULL (ones), out: T x C.  A slot that names no row counts as a row of zeros (a weight that is
- * NaN shows). */
+ * not finite shows as NaN). */
 gsq_status gsq_combine_rows(const gsq_exchange* g, const void* rows, const int32_t* slots, const float* weights,
                             void* out, hipStream_t stream);
 

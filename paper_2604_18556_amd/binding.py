@@ -165,8 +165,9 @@ class Routing:
 
     def to_c(self, tokens, dtype):
         return CRouting(tokens, _int32("experts", self.experts), _int32("top_k", self.top_k),
-                        _int32("groups", self.groups), _int32("top_groups", self.top_groups), self.score,
-                        self.group_score, 1 if self.renormalise else 0, self.scale, dtype)
+                        _int32("groups", self.groups), _int32("top_groups", self.top_groups),
+                        _int32("score", self.score), _int32("group_score", self.group_score),
+                        1 if self.renormalise else 0, self.scale, dtype)
 
 
 _lib = None

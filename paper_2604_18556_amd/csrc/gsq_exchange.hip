@@ -2,9 +2,10 @@
 // gradients of the sum.
 //
 // All three are bound by memory.  A lane has 16 bytes of a token's row and asks for those of eight of its rows (two,
-// where a token has no more: 16384 rows of 4096 of one token each there and back 135 us by eights) at once; a wavefront belongs to one token (rows of more than 512 bytes) and has the slots in scalar registers, so that
-// nothing in the way of the loads is divided.  The last 16 bytes of a row overlap those before where its length is no
-// multiple of them; addresses may be any, as loads and stores of 16 bytes need no alignment.
+// where a token has no more: 16384 rows of 4096 of one token each there and back 135 us by eights) at once; a wavefront
+// belongs to one token (rows of more than 512 bytes) and has the slots in scalar registers, so that nothing in the way
+// of the loads is divided.  The last 16 bytes of a row overlap those before where its length is no multiple of them;
+// addresses may be any, as loads and stores of 16 bytes need no alignment.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -68,6 +69,15 @@ struct Piece {
       bits &= some ? -1 : 0;
     } else {
       bits = some ? bits : (E)0.f;
+    }
+  }
+  // The first n values become zeros.
+  __device__ __forceinline__ void clear(int n) {
+    if constexpr (PER > 1) {
+      vec v = __builtin_bit_cast(vec, bits);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) v[i] = i < n ? (E)0.f : v[i];
+      bits = __builtin_bit_cast(i32x4, v);
     }
   }
   __device__ __forceinline__ float at(int i) const {
@@ -197,8 +207,9 @@ __global__ __launch_bounds__(256) void k_combine(ExchangeArgs p, int64_t blocks)
 }
 
 // A workgroup has a token, its wavefronts one part after another (or, of short rows, a wavefront several tokens); the
-// products' sums are added over lanes and wavefronts in a fixed order.
-template <class F>
+// products' sums are added over lanes and wavefronts in a fixed order.  kRagged: a row's last piece overlaps the one
+// before.
+template <class F, bool kRagged>
 __global__ __launch_bounds__(512) void k_combine_grad(ExchangeArgs p, int64_t blocks) {
   using E = typename F::E;
   constexpr int PER = F::PER, AT = F::AT;
@@ -221,14 +232,21 @@ __global__ __launch_bounds__(512) void k_combine_grad(ExchangeArgs p, int64_t bl
 #pragma unroll
         for (int u = 0; u < AT; ++u)
           v[u].load(static_cast<const E*>(p.rows) + (slot[u] < 0 ? 0 : slot[u]) * p.C + c);
-        const int before = piece * PER - c;      // values that the piece before has counted
+        const int before = kRagged ? piece * PER - c : 0;      // values that the piece before has counted
         d.settle();
+        if (kRagged && before > 0)               // on both sides: an infinity times zero would be NaN
+#pragma unroll
+          for (int u = 0; u < AT; ++u) {
+            v[u].settle();
+            v[u].clear(before);
+          }
         float once[PER];
 #pragma unroll
         for (int i = 0; i < PER; ++i) once[i] = i >= before ? d.at(i) : 0.f;
 #pragma unroll
         for (int u = 0; u < AT; ++u) {
-          v[u].settle(slot[u] >= 0);
+          v[u].settle();
+          if (slot[u] < 0) continue;
           float r[PER];
 #pragma unroll
           for (int i = 0; i < PER; ++i) {
@@ -237,7 +255,7 @@ __global__ __launch_bounds__(512) void k_combine_grad(ExchangeArgs p, int64_t bl
           }
           Piece<F> to;
           to.set(r);
-          if (slot[u] >= 0) to.store(static_cast<E*>(p.out) + slot[u] * p.C + c);
+          to.store(static_cast<E*>(p.out) + slot[u] * p.C + c);
         }
       }
       if constexpr (kWave) {
@@ -352,7 +370,11 @@ hipError_t launch_combine_grad(const gsq_exchange& g, const void* dout, const vo
   p.dweights = dweights;
   return with_pieces(g.dtype, p, true,
                      [&](auto form, const ExchangeArgs& p, unsigned grid, int threads, int64_t blocks) {
-                       k_combine_grad<decltype(form)><<<grid, threads, 0, s>>>(p, blocks);
+                       using Form = decltype(form);
+                       if (!Form::kStream && p.C % Form::PER)
+                         k_combine_grad<Form, !Form::kStream><<<grid, threads, 0, s>>>(p, blocks);
+                       else
+                         k_combine_grad<Form, false><<<grid, threads, 0, s>>>(p, blocks);
                      });
 }
 

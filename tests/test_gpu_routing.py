@@ -472,6 +472,29 @@ def test_values_that_are_not_finite_stay_in_their_rows(dev):
     assert torch.equal(~torch.isfinite(y.cpu()), bad)
 
 
+@pytest.mark.parametrize("dtype", [FP32, BF16, FP16], ids=["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("c", [3, 67, 72, 523, 528, 4099])
+@pytest.mark.parametrize("k", [2, 3])
+def test_gradients_of_weights_with_values_that_are_not_finite(dev, k, c, dtype):
+    """A weight whose slot names no row has gradient 0 whatever dout is; infinities in one place of a row give infinities,
+    also in the last columns, and stay with their slots."""
+    t = 2 * c if c < 8 else 40
+    slots = torch.arange(t * k, dtype=torch.int32).view(t, k)
+    dout, rows = torch.ones(t, c, dtype=dtype), torch.ones(t * k, c, dtype=dtype)
+    want = torch.full((t, k), float(c))
+    for i in range(0, t - 1, 2):                      # infinities from the last column on backwards
+        at = c - 1 - i // 2 % c
+        rows[i * k + 1, at], want[i, 1] = -INF, -INF
+        dout[i + 1, at], want[i + 1] = INF, INF
+    slots[1, 0], slots[3, k - 1], want[1, 0], want[3, k - 1] = -1, t * k, 0, 0
+    slots[5], want[5], dout[5] = -1, 0, float("nan")
+    w, drows, dw = torch.ones(t, k, device=dev), torch.zeros(t * k, c, dtype=dtype, device=dev), torch.empty(t, k, device=dev)
+    B.combine_rows_grad(dout.to(dev), rows.to(dev), slots.to(dev), w, drows, dw)
+    assert torch.equal(dw.cpu(), want)
+    some = (slots >= 0) & (slots < t * k)
+    assert torch.equal(drows.cpu()[slots[some].long()], dout[:, None].expand(t, k, c)[some])
+
+
 def test_no_tokens(dev):
     r = R(8, 2)
     none, ids, w = torch.empty(0, 8, device=dev), torch.empty(0, 2, dtype=torch.int32, device=dev), torch.empty(0, 2, device=dev)

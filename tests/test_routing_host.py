@@ -146,6 +146,8 @@ BIG = (1 << 32) + 8          # 8 in its low 32 bits
 
 @pytest.mark.parametrize("call", [
     lambda t: B.route(B.Routing(BIG, 1), t(1, BIG), t(1, 1, dtype=torch.int32), t(1, 1)),
+    lambda t: B.route(B.Routing(8, 1, score=1 << 32), t(1, 8), t(1, 1, dtype=torch.int32), t(1, 1)),
+    lambda t: B.route(B.Routing(8, 1, group_score=1 << 32), t(1, 8), t(1, 1, dtype=torch.int32), t(1, 1)),
     lambda t: B.dispatch_rows(t(1, BIG), t(1, 1, dtype=torch.int32), t(1, BIG)),
     lambda t: B.combine_rows(t(1, 8), t(1, BIG, dtype=torch.int32), t(1, 8)),
     lambda t: B.group_rows(t(1, dtype=torch.int32), t(BIG + 1, dtype=torch.int64), t(1, dtype=torch.int32),
