@@ -40,7 +40,7 @@ struct Form {
 };
 
 // 16 bytes of a row, or one value.  kStream: of arrays that no cache holds, by accesses with the non-temporal hint
-// (aligned; 16384 rows of 7168 there and back 99 us, 120 without, their gradients 145, 158).
+// (aligned; 16384 rows of 7168 there and back 99 us, 120 without, their gradients 146, 158).
 template <class F>
 struct Piece {
   using E = typename F::E;
