@@ -301,15 +301,36 @@ struct Sixteen {
   }
 };
 
-// Rows without an adapter: the base, or zeros.
-template <class E>
+// Rows without an adapter: the base, or zeros, by pieces as y is gone through, four of a lane on their way at once (4096
+// rows of 14336 53 us with the call's first kernel, 85 value by value).
+template <class E, int kBy>
 __device__ __forceinline__ void copy_base(const AdapterArgs& p, int64_t first, int ms, int n0, int cols, int ns) {
+  using Piece = std::conditional_t<kBy == kNarrow, E, i32x4>;
+  constexpr int PER = sizeof(Piece) / sizeof(E), AHEAD = 4;
   if (p.base == p.out) return;
-  for (int r = threadIdx.x >> 6; r < ms; r += blockDim.x >> 6)
-    for (int c = threadIdx.x & 63; c < cols; c += 64) {
-      const int64_t at = (first + r) * ns + n0 + c;
-      static_cast<E*>(p.out)[at] = p.base ? static_cast<const E*>(p.base)[at] : (E)0.f;
+  const E* const base = static_cast<const E*>(p.base) + first * ns + n0;
+  E* const out = static_cast<E*>(p.out) + first * ns + n0;
+  const int pieces = cols / PER, all = ms * pieces;
+  for (int f0 = threadIdx.x; f0 < all; f0 += AHEAD * blockDim.x) {
+    Piece v[AHEAD];
+    int64_t at[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int f = min(f0 + u * (int)blockDim.x, all - 1), r = f / pieces;
+      at[u] = (int64_t)r * ns + (f - r * pieces) * PER;
+      v[u] = Piece{};
+      if (p.base) v[u] = kBy == kStream ? __builtin_nontemporal_load(reinterpret_cast<const Piece*>(base + at[u]))
+                                        : *reinterpret_cast<const Piece*>(base + at[u]);
     }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (f0 + u * (int)blockDim.x >= all) break;
+      if constexpr (kBy == kStream)
+        __builtin_nontemporal_store(v[u], reinterpret_cast<Piece*>(out + at[u]));
+      else
+        *reinterpret_cast<Piece*>(out + at[u]) = v[u];
+    }
+  }
 }
 
 // Waits until the blocks that this wavefront has copied are there, of whose later accesses `after` are at least on
@@ -343,7 +364,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void k_adapter_up(AdapterArgs p, int
   const int ms = (int)min(at.end - first, (int64_t)kUpRows), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n0 = (blockIdx.x % (unsigned)chunks) * steps * kUpCols, n1 = min(n0 + steps * kUpCols, ns);
   const int e = adapter_of(p, at.group);
-  if (e < 0) return copy_base<E>(p, first, ms, n0, n1 - n0, ns);
+  if (e < 0) return copy_base<E, kBy>(p, first, ms, n0, n1 - n0, ns);
   const W w{static_cast<const E*>(kForm == kForward ? p.b : p.a) + (int64_t)e * p.q * ns, ns, p.q};
   const float scale = kForm == kForward ? scale_of(p, e) : 1.f;
 
@@ -425,7 +446,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void k_adapter_up_few(AdapterArgs p)
   const int64_t first = at.first + (blockIdx.x / (unsigned)tiles_n - at.before) * 16;
   const int ms = (int)min(at.end - first, (int64_t)16), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int e = adapter_of(p, at.group), n_all = (blockIdx.x % (unsigned)tiles_n) * wide;
-  if (e < 0) return copy_base<E>(p, first, ms, n_all, min(ns - n_all, wide), ns);
+  if (e < 0) return copy_base<E, kBy>(p, first, ms, n_all, min(ns - n_all, wide), ns);
   const int n0 = n_all + wave * kUpCols;
   if (n0 >= ns) return;
   const W w{static_cast<const E*>(kForm == kForward ? p.b : p.a) + (int64_t)e * p.q * ns, ns, p.q};

@@ -179,6 +179,25 @@ def test_large_adapters_of_whole_numbers_are_exact(dev, counts, index, n, o, i, 
     assert torch.equal(c.da, da.float()) and torch.equal(c.db, db.float())
 
 
+@pytest.mark.parametrize("counts,o", [([1, 2], 8), ([40, 70], 8), ([40, 70], 72), ([130, 1], 1001), ([300, 5], 1096), ([1100, 900], 9224)])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_rows_without_an_adapter_are_the_base_bit_by_bit(dev, counts, o, shift):
+    """Also what is not finite there, whatever x holds; without a base zeros; in place nothing changes."""
+    gen, r, q = rng_of(o), sum(counts) + 2, 16
+    bits = torch.randint(-32768, 32768, (r, o), generator=gen).short()
+    base = torch.zeros(r * o + shift, dtype=torch.int16, device=dev)[shift:].view(r, o).copy_(bits).view(BF16)
+    x, a, b = torch.full((r, 24), float("nan"), dtype=BF16, device=dev), torch.ones(2, q, 24, dtype=BF16, device=dev), torch.ones(2, o, q, dtype=BF16, device=dev)
+    where = {"offsets": offsets_of(counts).to(dev), "index": torch.full((2,), -1, dtype=torch.int32, device=dev)}
+    mine = r - 2
+    for given, want in ((base, bits), (None, torch.zeros_like(bits))):
+        y, h = torch.full((r, o), 7.0, dtype=BF16, device=dev), torch.full((r, q), 7.0, device=dev)
+        B.adapter_forward(x, a, b, h, y, base=given, **where)
+        assert torch.equal(y[:mine].view(torch.int16).cpu(), want[:mine]) and not h[:mine].any()
+        assert (y[mine:] == 7).all() and (h[mine:] == 7).all()
+    B.adapter_forward(x, a, b, h, base, base=base, **where)
+    assert torch.equal(base.view(torch.int16).cpu(), bits)
+
+
 @pytest.mark.parametrize("shift", [1, 3, 4])
 @pytest.mark.parametrize("q", [5, 16, 72])
 def test_addresses_of_any_element_alignment(dev, shift, q):
