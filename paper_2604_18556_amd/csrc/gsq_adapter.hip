@@ -10,6 +10,7 @@
 
 #include "gsq_adapter.h"
 #include "gsq_split.hpp"
+#include "gsq_walk.h"
 
 namespace gsq {
 namespace {
@@ -506,42 +507,37 @@ struct AdapterSlabs {
   const AdapterArgs& p;
   int e, s0 = 0;
   uint64_t mine = 0;           // segments from s0 on that are left
-  int64_t at = 0, end = 0;     // rows of the present segment that are left
-  int64_t skip;                // slabs to the next
-  bool more = true;
+  SlabWalk walk;
 
-  __device__ __forceinline__ AdapterSlabs(const AdapterArgs& args, int adapter, int wave) : p(args), e(adapter), skip(wave) {
+  __device__ __forceinline__ AdapterSlabs(const AdapterArgs& args, int adapter, int wave) : p(args), e(adapter), walk(wave) {
     if (!p.index) {
-      if (e < p.rows.groups) group_rows(p.rows, e, at, end);
+      if (e < p.rows.groups) enter(e);
     } else {
       look();
     }
+  }
+  __device__ __forceinline__ void enter(int segment) {
+    int64_t first, end;
+    group_rows(p.rows, segment, first, end);
+    walk.enter(first, end);
   }
   __device__ __forceinline__ void look() {
     const int lane = threadIdx.x & 63, s = min(s0 + lane, p.rows.groups - 1);
     mine = __ballot(s0 + lane < p.rows.groups && p.index[s] == e);
   }
-  // The next slab: its first row and how many it has.
+  // The next slab: its first row and how many it has.  Once there is none, there is none again.
   __device__ __forceinline__ bool next(int64_t& first, int& rows) {
-    while (true) {
-      const int64_t left = (end - at + kWeightRows - 1) / kWeightRows;
-      if (skip < left) {
-        first = at + skip * kWeightRows;
-        rows = (int)min(end - first, (int64_t)kWeightRows);
-        at = first;
-        skip = blockDim.x >> 6;
-        return true;
-      }
-      skip -= left;
+    while (!walk.take(kWeightRows, blockDim.x >> 6, first, rows)) {
       if (!p.index) return false;
       while (!mine) {
         s0 += 64;
         if (s0 >= p.rows.groups) return false;
         look();
       }
-      group_rows(p.rows, s0 + __builtin_ctzll(mine), at, end);
+      enter(s0 + __builtin_ctzll(mine));
       mine &= mine - 1;
     }
+    return true;
   }
 };
 
@@ -661,6 +657,10 @@ __global__ __launch_bounds__(64 * kSplitWaves) void k_adapter_weights(AdapterArg
     has_odd = use(odd, own + kWeightSlab, has_even);
   }
 
+  // no copy is on its way any more when the sums take the slabs' place
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  wait_vm<0>();
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
   // the wavefronts' sums, added in their order; a lane has rows 4 (lane / 16) + i of the rank, and of block c column
   // 16 c + lane % 16
   const float scale = of_a ? 1.f : scale_of(p, e);
