@@ -210,13 +210,15 @@ __global__ __launch_bounds__(64) void k_route(RouteArgs p) {
     sum += w[n];
   }
   if (p.renormalise) total = sum_lanes<LANES>(sum);
-  const double by = wrong != 0.f ? (double)__builtin_nanf("") : total > 0.0 ? (double)p.scale / total : 0.0;
+  // the share first: scale / total would overflow where a bias chooses experts whose scores are subnormal
+  const double by = wrong != 0.f ? (double)__builtin_nanf("") : total > 0.0 ? (double)p.scale : 0.0;
+  if (!(total > 0.0)) total = 1.0;
 #pragma unroll
   for (int n = 0; n < TIMES; ++n) {
     const int i = lane + n * LANES;
     if (live && i < p.K) {
       p.experts[token * p.K + i] = s_chosen[sub][i];
-      p.weights[token * p.K + i] = (float)(w[n] * by);
+      p.weights[token * p.K + i] = (float)(w[n] / total * by);
     }
   }
 }

@@ -207,6 +207,33 @@ def test_route_keys_that_32_bits_do_not_tell_apart(dev):
     assert route(r, logits, None, dev)[0].tolist() == [[1, 0], [2, 1]]
 
 
+@pytest.mark.parametrize("times", [1, 1200])
+@pytest.mark.parametrize("score,scale", [(SOFT, 1.5), (SIG, 2.5)], ids=["softmax", "sigmoid"])
+def test_route_weights_of_subnormal_scores(dev, score, scale, times):
+    """A bias chooses experts whose scores in 64 bits are below the smallest normal one: weights are still their shares.
+    One expert's is the scale itself.  Others: scores of at least 2^-1041 are whole numbers of 2^-1074, off by up to two of
+    them, 2^-32 of a score, here and in the reference: 2^-30 of a share with the sum's, beside half a step of fp32."""
+    low = 720.0 if score == SOFT else 709.0
+    logits = torch.tensor([[low, 0.0, 0.25, -0.5, 1.0, 0.0, 0.0, 0.0], [0.0, 3.0, -0.25, -1.0, low, 0.5, 0.0, 0.0]]) - low
+    if score == SIG:
+        logits = logits.clamp_min(-709.5)
+    bias = torch.tensor([0.0, 9.0, 8.0, 7.0, 0.0, 6.0, 0.0, 0.0])
+    logits = logits.repeat(times, 1)
+    for k in (1, 2, 4):
+        r = R(8, k, score=score, scale=scale)
+        ids, w = route(r, logits, bias, dev)
+        idr, wr = route_ref(r, logits, bias)
+        assert torch.equal(ids, idr) and ids[0].tolist() == [1, 2, 3, 5][:k]
+        assert torch.isfinite(w).all() and ((w.double() - wr).abs() <= wr * (U + 2.0 ** -30)).all()
+        if k == 1:
+            assert (w == scale).all()
+    if score == SOFT:                              # the smallest score that there is, and none at all
+        r = R(8, 1, scale=scale)
+        for down, want in ((744.0, scale), (800.0, 0.0)):
+            _, w = route(r, torch.cat((logits[:1, :1] * 0 + down, logits[:1, 1:] * 0), 1).repeat(times, 1), bias, dev)
+            assert (w == want).all()
+
+
 def test_route_from_any_address(dev):
     gen = rng_of(4)
     for e in (33, 64, 255):
