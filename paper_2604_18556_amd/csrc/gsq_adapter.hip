@@ -152,15 +152,17 @@ template <class T>
 __device__ __forceinline__ void split_hidden(const float* row, int k, int q, float by, typename T::frag& hi,
                                              typename T::frag& lo) {
   using E = typename T::elem;
+  // the largest of 16 bits: what is finite and would be rounded beyond it (bf16) has its rest in the second part, as have
+  // infinities and NaN, whole
+  constexpr float kTop = T::kDtype == GSQ_DT_FP16 ? 65504.f : 0x1.fep127f;
   float v[8];
   load_hidden(row, k + 8 * ((threadIdx.x & 63) >> 4), q, v);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float x = v[i] * by;
-    const E h = (E)x;
+    const E h = (E)__builtin_amdgcn_fmed3f(x, -kTop, kTop);
     hi[i] = h;
-    // of what is not finite there is no second part
-    lo[i] = (E)(__builtin_isfinite((float)h) ? x - (float)h : 0.f);
+    lo[i] = (E)(x - (float)h);
   }
 }
 

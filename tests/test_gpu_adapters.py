@@ -319,6 +319,33 @@ def test_values_that_are_not_finite_stay_where_they_belong(dev, q, dtype):
         assert torch.equal(got.cpu()[2][torch.isfinite(want[2])], want[2][torch.isfinite(want[2])].float())
 
 
+@pytest.mark.parametrize("rows,q", [(1, 8), (5, 200), (70, 8), (70, 40), (70, 200)])
+def test_hidden_between_the_largest_of_16_bits_and_of_32(dev, rows, q):
+    """hidden = +-2^127 (2 - 2^-9) is finite, but rounded to bf16 it would not be.  Its two parts are exact, and so are y and
+    dx: +-255.75 before the base."""
+    n = 24
+    x = torch.zeros(rows, n, dtype=torch.float64)
+    x[::2, :2], x[1::2, :2] = 1.0, -1.0
+    a = torch.zeros(1, q, n, dtype=torch.float64)
+    a[0, q - 1, 0], a[0, q - 1, 1] = 2.0 ** 127 * (2 - 2.0 ** -7), 1.5 * 2.0 ** 119
+    b = torch.zeros(1, n, q, dtype=torch.float64)
+    b[0, 3, q - 1], b[0, 5, q - 1] = 2.0 ** -120, -(2.0 ** -121)
+    base = torch.full((rows, n), 7.0).double()
+    base[::2, 3], base[1::2, 3] = -256.0, 256.0
+    args = (torch.tensor([0, rows]), None, None, base, base)
+    ref = Ref(x, x, a, b, *args)
+    c = Case(dev, BF16, x, x, a, b, *args)
+    B.adapter_forward(c.x, c.a, c.b, c.h, c.y, base=c.base, **c.where)
+    assert torch.equal(c.h.cpu(), ref.h.float()) and c.h.abs().amax() == 2.0 ** 127 * (2 - 2.0 ** -9)
+    assert torch.equal(c.y.cpu(), ref.y.to(BF16)) and (ref.y[:, 3].abs() == 0.25).all()
+    # the other way round: B has the large values, A the small ones
+    bt, at = a.transpose(1, 2).contiguous(), b.transpose(1, 2).contiguous()
+    ref = Ref(x, x, at, bt, *args)
+    c = Case(dev, BF16, x, x, at, bt, *args)
+    B.adapter_input_grad(c.dy, c.a, c.b, c.dh, c.dx, base=c.dbase, **c.where)
+    assert torch.equal(c.dh.cpu(), ref.dh.float()) and torch.equal(c.dx.cpu(), ref.dx.to(BF16))
+
+
 def test_wrong_offsets_and_indexes_touch_nothing_outside(dev):
     gen, o, i, q, r = rng_of(8), 24, 40, 8, 20
     x, dy, a, b = whole((r, i), gen), whole((r, o), gen), whole((2, q, i), gen, 1), whole((2, o, q), gen, 1)
