@@ -76,8 +76,8 @@ typedef struct {
 } gsq_exchange;
 
 /* out[slots[t, k]] = x[t].  x: T x C, slots: int32 T x K, out: R x C.  Slots outside 0 .. R - 1 name no row; rows
- * that no slot names are left as they were.  Slots have to be distinct: a row that several name gets one of
- * theirs.  The gradient of x is gsq_combine_rows of the rows' gradients without weights. */
+ * that no slot names are left as they were.  Slots of different tokens have to be distinct: each value of a row
+ * that several name is that of one of them, not always the same one. */
 gsq_status gsq_dispatch_rows(const gsq_exchange* g, const void* x, const int32_t* slots, void* out,
                              hipStream_t stream);
 
@@ -88,8 +88,8 @@ gsq_status gsq_combine_rows(const gsq_exchange* g, const void* rows, const int32
                             void* out, hipStream_t stream);
 
 /* Its gradients from dout (T x C): drows[slots[t, k]] = weights[t, k] dout[t] (R x C in dtype; rows that no slot
- * names are left as they were, slots have to be distinct) and dweights[t, k] = sum_c dout[t, c]
- * rows[slots[t, k], c] (fp32 T x K; 0 for a slot that names no row). */
+ * names are left as they were; slots have to be distinct, as above, those of one token too) and dweights[t, k] =
+ * sum_c dout[t, c] rows[slots[t, k], c] (fp32 T x K; 0 for a slot that names no row). */
 gsq_status gsq_combine_rows_grad(const gsq_exchange* g, const void* dout, const void* rows, const int32_t* slots,
                                  const float* weights, void* drows, float* dweights, hipStream_t stream);
 

@@ -459,6 +459,40 @@ def test_exchanges_that_no_cache_holds(dev, t, k, c):
     assert ((y.double() - ref).abs() <= err + half_step(BF16) * (ref.abs() + err) + smallest(BF16)).all()
 
 
+@pytest.mark.parametrize("c", [5, 40, 1001, 7168])
+def test_rows_that_several_slots_name(dev, c):
+    """Each value of such a row is one of theirs; other rows, sums and the weights' gradients are as ever."""
+    gen, t, n = rng_of(c), 300, 900
+    slots = torch.arange(2 * t, dtype=torch.int32).view(t, 2)
+    slots[7] = 500                                 # twice by one token, and by token 250
+    slots[100:200, 0] = 700                        # by a hundred
+    slots[250, 1] = 3                              # by token 1 too
+    x, rows, w = torch.randn(t, c, generator=gen), torch.randn(n, c, generator=gen), torch.randn(t, 2, generator=gen)
+    sd, out = slots.to(dev), torch.full((n, c), 7.0, device=dev)
+    B.dispatch_rows(x.to(dev), sd, out)
+    out = out.cpu()
+    for row in (3, 500, 700):
+        tokens = (slots == row).any(1).nonzero().flatten()
+        assert (out[row] == x[tokens]).any(0).all()
+    ref = torch.full((n, c), 7.0)
+    ref[slots.flatten().long()] = x.repeat_interleave(2, 0)
+    alone = torch.ones(n, dtype=torch.bool)
+    alone[[3, 500, 700]] = False
+    assert torch.equal(out[alone], ref[alone])
+    y, drows, dw = torch.empty(t, c, device=dev), torch.full((n, c), 7.0, device=dev), torch.empty(t, 2, device=dev)
+    B.combine_rows(rows.to(dev), sd, y, weights=w.to(dev))
+    want, mag, picked = combine_ref(rows, slots, w)
+    assert ((y.cpu().double() - want).abs() <= 3 * U * mag + U * want.abs() + smallest(FP32)).all()
+    B.combine_rows_grad(x.to(dev), rows.to(dev), sd, w.to(dev), drows, dw)
+    prod = picked * x.double()[:, None]
+    assert ((dw.cpu().double() - prod.sum(-1)).abs() <= c * 2 * U * prod.abs().sum(-1)).all()
+    drows = drows.cpu().double()
+    for row in (3, 500, 700):
+        token, place = (slots == row).nonzero(as_tuple=True)
+        each = w[token, place, None].double() * x[token].double()
+        assert ((drows[row] - each).abs() <= each.abs() * 2 * U + smallest(FP32)).any(0).all()
+
+
 def test_exchange_gradients_are_differences(dev):
     """f = <dy, combine(rows, w)> is linear in each: with small whole numbers its differences are exact."""
     gen, t, k, c = rng_of(3), 6, 3, 40
