@@ -18,10 +18,10 @@
  * rank is padded with zeros.
  *
  * Stream, device pointers, status codes and gsq_last_error() are as gsq.h says, addresses, overlapping calls and
- * reproducibility as gsq_products.h does; nothing is allocated, synchronised or kept.  Sums are in fp32, and
- * hidden enters the second product with 16 bits of mantissa at least, so that y and dx are rounded once.  What is not
- * finite stays in its rows of y and dx, and in its adapter's gradients; where the formulas have an infinity there may
- * be NaN.
+ * reproducibility as gsq_products.h does; nothing is allocated, synchronised or kept.  Sums are in fp32, and y and dx
+ * are rounded once: hidden enters the second product off by no more than 2^-16 of each value (bf16), or by 2^-22 of it
+ * and 2^-36 of the row's largest (fp16).  What is not finite stays in its rows of y and dx, and in its adapter's
+ * gradients; where the formulas have an infinity there may be NaN.
  */
 #ifndef GSQ_ADAPTERS_H
 #define GSQ_ADAPTERS_H

@@ -216,7 +216,8 @@ inline SumsPlan plan_sums(int64_t rows, int64_t groups, int O, int I, bool tight
 }
 
 // How ids are brought into order: by one workgroup, or chunk by chunk, of which there are at most 128, so that a
-// workgroup counts over all of them itself.  The chunks' counts fit into a quarter of the ids' places.  `waves`
+// workgroup counts over all of them itself.  The chunks' counts, kept in the ids' places until these are known, take less
+// than a quarter of them and one chunk's: about half at most, with two chunks of which the second is short.  `waves`
 // wavefronts count, with a histogram each in LDS (64 KB in all).
 struct OrderPlan {
   int threads, waves, chunks;

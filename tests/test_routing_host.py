@@ -184,3 +184,31 @@ int main() {
                     str(exe)], check=True, capture_output=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
+
+
+def test_counts_of_the_order_fit_the_ids_places(tmp_path):
+    """Less than a quarter of the places and one chunk's counts, whatever the last chunk holds."""
+    src = tmp_path / "plan.cpp"
+    src.write_text(r'''
+#include <cstdio>
+#include "gsq_plan.h"
+int main() {
+  using namespace gsq;
+  double most = 0;
+  for (int g : {1, 2, 3, 7, 64, 100, 255, 256, 257, 1000, 2047, 2048, 2049, 3000, 4095, 4096})
+    for (int64_t n = 8193; n <= ((int64_t)1 << 30); n += n < 17000 ? 1 : n / 7 + 1) {
+      const OrderPlan p = plan_order(n, g);
+      if (p.chunks == 1) continue;
+      const int64_t words = (int64_t)p.chunks * g;
+      most = std::max(most, (double)words / n);
+      if (4 * words >= n + 4 * g || words > n) { std::printf("%lld ids, %d groups: %lld\n", (long long)n, g, (long long)words); return 1; }
+    }
+  if (most < 0.49 || most > 0.51) { std::printf("%f\n", most); return 1; }
+  return 0;
+}
+''')
+    exe = tmp_path / "plan"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", os.path.join(ROOT, "paper_2604_18556_amd", "csrc"), str(src), "-o",
+                    str(exe)], check=True, capture_output=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout
