@@ -3,7 +3,7 @@
 //
 // A product through a low rank is two products whose inner results are small: hidden goes to memory in fp32 (the gradients
 // need it again), and both kernels of a call are bound by reading x and by reading and writing y, not by the matrix cores
-// (busy 0.03 and 0.10 of the time at 4096 rows, 4096 -> 64 -> 14336: 20 us for A x, 58 us for y).
+// (busy 0.03 and 0.09 of the time at 4096 rows, 4096 -> 64 -> 14336: 20 us for A x, 58 us for y).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -351,10 +351,12 @@ __device__ __forceinline__ void wait_blocks(int after) {
 
 // Panels of 64 rows (16 to a wavefront) and `steps` times 64 columns.  A panel's hidden stays in registers as long as its
 // rank fits KS blocks.  While a step is multiplied, the matrix of the next is on its way to LDS, and the base of the next
-// two to registers.  4096 rows of 14336 with a base at rank 64: 58 us, 235 MB of base and y at 4.1 TB/s (a copy of as much
-// takes 45).  With cold caches 60, and 116 with the matrix read by each wavefront for itself, 92 from LDS but 32 bytes of
-// a row stored at a time, 80 with 64, 78 with whole lines that the caches keep.  Twice the columns at a step, a panel's
-// workgroups on neighbouring columns at each step, and each XCD on columns of its own changed nothing or cost a tenth.
+// two to registers; but before a step's base enters its sums everything that is on its way is waited for, as the built
+// code cannot count on the younger loads, which stand under lane masks.  4096 rows of 14336 with a base at rank 64: 58 us,
+// 235 MB of base and y at 4.1 TB/s (a copy of as much takes 45), waiting half of the time.  With cold caches 60, and 116
+// with the matrix read by each wavefront for itself, 92 from LDS but 32 bytes of a row stored at a time, 80 with 64, 78
+// with whole lines that the caches keep.  Twice the columns at a step, a panel's workgroups on neighbouring columns at
+// each step, and each XCD on columns of its own changed nothing or cost a tenth.
 template <class T, int kForm, int KS, bool kCopied, int kBy>
 __global__ __launch_bounds__(64 * kUpWaves) void k_adapter_up(AdapterArgs p, int steps, int chunks) {
   using E = typename T::elem;
@@ -495,12 +497,14 @@ __global__ __launch_bounds__(64 * kUpWaves) void k_adapter_up_few(AdapterArgs p)
 
 // ------------------------------------------------------------------ dA, dB: sums over an adapter's rows
 // The instructions' rows are the rank, their columns those of x (or dy), and both run across their arrays.  x comes to
-// LDS in slabs of 32 rows, two of them for each wavefront so that one is on its way while the other is used, and is read
-// by transposing reads; a lane reads its eight hidden values of a column itself.
+// LDS in slabs of 32 rows, two of them for each wavefront, and is read by transposing reads; a lane reads its eight hidden
+// values of a column itself.  Two slabs are asked for at first; later a slab is asked for while the one before is
+// multiplied, and waited for right after, copies and all, as hidden goes to registers on several ways that meet.
 // fp32 instructions would need no transposing, but take five times as long as the bf16 ones of the exact parts that
 // hidden is split into, three of 8 bits (fp16 x: two parts, of whose products those below 2^-24 of the whole are left out).
-// 4096 rows of 4096 + 14336 columns in four adapters of rank 32: 45 us, 0.15 GB at 3.4 TB/s (92 by fp32 instructions, with
+// 4096 rows of 4096 + 14336 columns in four adapters of rank 32: 43 us, 0.15 GB at 3.5 TB/s (92 by fp32 instructions, with
 // 64-row slabs one at a time 50); the largest adapter has half of the rows, and the rounds of workgroups end unevenly.
+// One adapter has a workgroup for each 128 columns only: 8192 rows of 4096 + 4096 at rank 16 61 us.
 constexpr int kWeightCols = 128, kWeightBlocks = kWeightCols / 16;
 constexpr int kWeightRows = 32, kWeightSlab = kWeightRows * kWeightCols * 2;
 

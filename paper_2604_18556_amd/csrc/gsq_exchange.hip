@@ -2,10 +2,12 @@
 // gradients of the sum.
 //
 // All three are bound by memory.  A lane has 16 bytes of a token's row and asks for those of eight of its rows (two,
-// where a token has no more: 16384 rows of 4096 of one token each there and back 135 us by eights) at once; a wavefront
-// belongs to one token (rows of more than 512 bytes) and has the slots in scalar registers, so that nothing in the way
-// of the loads is divided.  The last 16 bytes of a row overlap those before where its length is no multiple of them;
-// addresses may be any, as loads and stores of 16 bytes need no alignment.
+// where a token has no more: 16384 rows of 4096 of one token each there and back 135 us by eights) at once.  What a token
+// has not of the eight is read as the first row, which the caches hold: 16384 rows of 7168 summed by eights 43 us, 6.1 TB/s,
+// by sixes 45, by fours 54, by threes 65, 4.8 TB/s, by twos 57.  A wavefront belongs to one token (rows of more than 512
+// bytes) and has the slots in scalar registers, so that nothing in the way of the loads is divided.  The last 16 bytes of a
+// row overlap those before where its length is no multiple of them; addresses may be any, as loads and stores of 16 bytes
+// need no alignment.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

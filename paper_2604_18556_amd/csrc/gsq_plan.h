@@ -134,7 +134,9 @@ inline RowsPlan plan_packed(int64_t rows, int64_t groups, int O, int blocks, boo
 }
 
 // hidden and dhidden of the adapters: rows times a matrix of `rank` columns by wavefronts that share the sum, at the
-// costs of plan_rows.
+// costs of plan_rows, which were fitted there to eight of them; tiles of 16 x 16 have up to sixteen here.  (Those are taken
+// only where they number far fewer than a launch of sixteen wavefronts holds: of more rows 64 x 16 is cheaper, of a rank
+// beyond 16 16 x 64.)
 inline RowsPlan plan_adapter(int64_t rows, int64_t segments, int rank, int slabs, bool tight) {
   const TileCost aligned[] = {{64, 64, 1, 0.165, 0.22}, {64, 16, 1, 0.1, 0.115}, {16, 64, 1, 0.06, 0.1}, {16, 16, 0.5, 0.02, 0.055}};
   const TileCost loose[] = {{64, 64, 1, 0.17, 0.42}, {64, 16, 1, 0.1, 0.21}, {16, 64, 1, 0.07, 0.15}, {16, 16, 0.5, 0.025, 0.08}};

@@ -1,4 +1,4 @@
-"""The rules of the adapters that the host can run: how wavefronts share the slabs of an adapter's rows."""
+"""The rules of the adapters that the host can run: how wavefronts share the slabs of an adapter's rows, and tiles."""
 import os
 import subprocess
 
@@ -80,6 +80,30 @@ int main() {
       }
       if (want != got) { std::printf("not all: %d waves\n", waves); return 1; }
     }
+  return 0;
+}
+''')
+
+
+def test_chosen_tiles_fit_a_launch(tmp_path):
+    """The rule reckons with up to eight wavefronts to a tile; those of 16 x 16 have up to sixteen."""
+    run(tmp_path, r'''
+#include <cstdio>
+#include "gsq_plan.h"
+using namespace gsq;
+int main() {
+  for (int64_t rows = 1; rows <= (int64_t)1 << 29; rows += rows < 64 ? 1 : rows / 19 + 1)
+    for (int64_t segments : {1, 2, 3, 16, 100, 1000, 10000, 65535})
+      for (int rank : {1, 8, 16, 17, 32, 48, 64, 65, 80, 128, 129, 200, 320, 511, 512})
+        for (int slabs : {1, 2, 3, 5, 8, 16, 64, 1000, 32768})
+          for (bool tight : {true, false}) {
+            const RowsPlan p = plan_adapter(rows, segments, rank, slabs, tight);
+            const int waves = std::min(slabs, p.height == 16 && p.width == 16 ? 16 : 8);   // one for each slab at most
+            if (p.height && !fits_launch(most_panels(rows, segments, p.height) * tiles_of(rank, p.width), 64 * waves)) {
+              std::printf("%lld rows, %lld segments, rank %d\n", (long long)rows, (long long)segments, rank);
+              return 1;
+            }
+          }
   return 0;
 }
 ''')
